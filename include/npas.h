@@ -253,6 +253,62 @@ int npas_stack_num_launches(const npas_stack *s);
 int npas_stack_describe(const npas_stack *s, int N, int64_t *rows_host, int max_rows);
 void npas_stack_free(npas_stack *s);
 
+/* ---- a decoder block around its linear layers ------------------------------
+ * What a transformer's decoder block needs between projections that run as npas_fc_sparse (block-based pruning) or npas_fc_mxfp4:
+ * norms with gate and residual, a paged cache of keys and values, attention of one new token a sequence.  Rows are tokens; a
+ * row is contiguous, rows lie `.._stride` elements apart (slices of a joined projection need no copy).  Pointers need the
+ * alignment of their element type, the two caches 16 bytes.  Sums, norms and softmax statistics are held in fp32; a result is
+ * rounded to the storage type once.  Nothing allocates or synchronises; lengths, positions and page tables are read on the
+ * device, so a captured HIP graph may be replayed with new ones. */
+
+/* The end of one block and the start of the next, one pass over the rows:
+ *   p = branch * post_weight / sqrt(mean(branch^2) + eps)     (post_weight NULL: p = branch)
+ *   h_out = residual_scale * h + gate * p                     (gate NULL: 1; branch NULL: h_out = residual_scale * h)
+ *   n_out = h_out * pre_weight / sqrt(mean(h_out^2) + eps)    (from the unrounded h_out; pre_weight and n_out both NULL: not formed)
+ * branch, h, h_out, n_out [T][D] in storage type dt, contiguous; weights fp32 [D].  gate: storage type, row t at gate + t * gate_stride
+ * (0: one row for all tokens).  h_out may be h, n_out may be branch; no other overlap. */
+int npas_gated_residual_norm(const void *branch_dev, const void *h_dev, const void *gate_dev, int64_t gate_stride,
+                             const float *post_weight_dev, const float *pre_weight_dev, float residual_scale, float eps,
+                             void *h_out_dev, void *n_out_dev, int T, int D, npas_dtype dt, void *hip_stream);
+
+/* A paged cache, described by the caller on every call (the library keeps nothing): keys and values
+ * [pages][kv_heads][page_size][head_dim] in 16-bit storage (dt is NPAS_BF16 or NPAS_F16); token j of sequence s lies in page
+ * page_table[s * table_stride + j / page_size] at row j % page_size.  A table entry outside 0 .. pages - 1 means "not in the
+ * cache": nothing is written there, attention leaves those tokens out.  head_dim: a multiple of 8, at most 256. */
+typedef struct {
+    void *k_dev, *v_dev;
+    const int32_t *page_table_dev;
+    int dtype, pages, page_size, kv_heads, head_dim;
+    int sequences, table_stride;
+} npas_kv_cache;
+
+typedef enum { NPAS_ROTATE_HALVES = 0, NPAS_ROTATE_PAIRS = 1 } npas_rotation;
+
+/* Rotation of queries and keys by their positions, keys and values into the cache: token t (of T) belongs to sequence sequence_dev[t]
+ * (NULL: t itself) and stands at position_dev[t].  In the first rot_dim elements of a head the pair (a, b) = (x[i], x[i + rot_dim / 2])
+ * (HALVES) or (x[2 i], x[2 i + 1]) (PAIRS) becomes (a cos - b sin, b cos + a sin) with cos = cos_sin[position][i], sin =
+ * cos_sin[position][rot_dim / 2 + i], fp32 [positions][rot_dim]; the rest is copied.  rot_dim 0: no rotation (cos_sin NULL).
+ * q [T] rows of heads * head_dim -> q_out [T][heads][head_dim] (both NULL: keys and values only; q_out may be q where q_stride
+ * is heads * head_dim); k, v [T] rows of kv_heads * head_dim.
+ * A token whose position is negative or at or past `positions` (where rot_dim > 0), or whose sequence is none of the cache's, is padding: it
+ * leaves the cache as it is, its q_out row is zeros.  One whose page is not in the cache is not stored.  Two tokens of a call at one
+ * place of the cache: undefined which stays. */
+int npas_kv_append(const npas_kv_cache *cache, const void *q_dev, int64_t q_stride, const void *k_dev, int64_t k_stride,
+                   const void *v_dev, int64_t v_stride, void *q_out_dev, int T, int heads, const int32_t *sequence_dev,
+                   const int32_t *position_dev, const float *cos_sin_dev, int positions, int rot_dim, npas_rotation kind,
+                   void *hip_stream);
+
+/* Attention of one new token a sequence over the cache: for sequence s and head h (reading the keys of head h / (heads / kv_heads))
+ *   y[s][h] = sum_j p_j v_j,  p = softmax_j(scale * q[s][h] . k_j),  max(0, n - window) <= j < n, j in the cache,
+ * n = length_dev[s] cut to 0 .. min(max_length, table_stride * page_size); window 0: no window.  Where no j is left, y is zero.
+ * lse_dev (nullable, fp32 [sequences][heads]): log sum_j exp(scale * q . k_j), -inf where no j is left.
+ * q: row s at q + s * q_stride, heads * head_dim long; y [sequences][heads][head_dim].  Long sequences are cut over workgroups whose
+ * partial results are joined through the workspace (16-byte aligned, npas_paged_attention_workspace_bytes, which may be 0). */
+size_t npas_paged_attention_workspace_bytes(const npas_kv_cache *cache, int heads, int max_length);
+int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t q_stride, void *y_dev, float *lse_dev, int heads,
+                         const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev,
+                         size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

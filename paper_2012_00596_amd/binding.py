@@ -11,13 +11,15 @@ _CSRC = os.path.join(_HERE, "csrc")
 _LIB = os.path.join(_HERE, "libnpas.so")
 _CALLS = os.path.join(_HERE, "_pycalls.so")  # CPython entry points of the run calls, linked to libnpas.so
 SOURCES = ["pack.cpp", "api.cpp", "kernels.hip", "spatial_direct_kernel.hip", "small_channel_rows_kernel.hip", "small_kernels.hip", "block_kernels.hip",
-           "inverted_residual_kernel.hip", "pointwise_stream_kernel.hip", "bottleneck_tail_kernel.hip", "noalloc.hip"]
+           "inverted_residual_kernel.hip", "pointwise_stream_kernel.hip", "bottleneck_tail_kernel.hip", "noalloc.hip",
+           "decoder.cpp", "decoder_kernels.hip", "paged_attention_kernel.hip"]
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "npas.h")
 
 F32, BF16, F16 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_RELU6, ACT_HARDSWISH = 0, 1, 2, 3
 SCHEME_BLOCK_PUNCHED, SCHEME_FC_BLOCK, SCHEME_PATTERN, SCHEME_DEPTHWISE = 0, 1, 2, 3
 LAYER_CONV, LAYER_FC, LAYER_MAXPOOL3X3S2, LAYER_GLOBAL_AVGPOOL, LAYER_DEPTHWISE3X3 = 0, 1, 2, 3, 4
+ROTATE_HALVES, ROTATE_PAIRS = 0, 1
 STACK_FUSE_POINTWISE = 1
 STACK_FUSE_INVERTED_RESIDUAL = 2
 STACK_FUSE_CONV_MAXPOOL = 4
@@ -32,6 +34,7 @@ EXPORTS = [
     "npas_maxpool3x3s2", "npas_global_avgpool", "npas_stack_create", "npas_stack_workspace_bytes",
     "npas_run_stack", "npas_stack_num_launches", "npas_stack_free", "npas_stack_describe", "npas_debug_set_switches",
     "npas_run_stack_static", "npas_debug_launch_empty", "npas_debug_device_kernel", "npas_debug_direct_plan",
+    "npas_gated_residual_norm", "npas_kv_append", "npas_paged_attention_workspace_bytes", "npas_paged_attention",
 ]
 STATIC_WORKSPACE_BYTES = 32 << 20
 DESCRIBE_COLS = 11
@@ -48,7 +51,7 @@ def build(force: bool = True) -> str:
     import sysconfig
     from concurrent.futures import ThreadPoolExecutor
     srcs = [os.path.join(_CSRC, s) for s in SOURCES]
-    deps = srcs + [os.path.join(_CSRC, "npas_internal.h"), os.path.join(_CSRC, "device_util.h"), HEADER]
+    deps = srcs + [os.path.join(_CSRC, "npas_internal.h"), os.path.join(_CSRC, "device_util.h"), os.path.join(_CSRC, "decoder_internal.h"), HEADER]
     calls = os.path.join(_CSRC, "pycalls.cpp")
     if not force and os.path.exists(_LIB) and os.path.exists(_CALLS) and \
             all(os.path.getmtime(_LIB) >= os.path.getmtime(d) for d in deps) and os.path.getmtime(_CALLS) >= os.path.getmtime(calls):
@@ -75,6 +78,12 @@ def build(force: bool = True) -> str:
 class LayerDesc(C.Structure):
     _fields_ = [("kind", C.c_int), ("packed", C.c_void_p), ("stride", C.c_int), ("pad", C.c_int),
                 ("act", C.c_int), ("src", C.c_int), ("res", C.c_int), ("bias_dev", C.c_void_p)]
+
+
+class KvCacheDesc(C.Structure):
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("page_table_dev", C.c_void_p), ("dtype", C.c_int), ("pages", C.c_int),
+                ("page_size", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("sequences", C.c_int),
+                ("table_stride", C.c_int)]
 
 
 _lib = None
@@ -120,6 +129,12 @@ def lib():
         L.npas_debug_direct_plan.argtypes = [vp, ip, ip, ip, ip, ip, C.POINTER(ip)]
         L.npas_debug_set_switches.argtypes = [C.c_char_p, ip]
         L.npas_debug_set_switches.restype = None
+        i64, cache = C.c_int64, C.POINTER(KvCacheDesc)
+        L.npas_gated_residual_norm.argtypes = [vp, vp, vp, i64, vp, vp, C.c_float, C.c_float, vp, vp, ip, ip, ip, vp]
+        L.npas_kv_append.argtypes = [cache, vp, i64, vp, i64, vp, i64, vp, ip, ip, vp, vp, vp, ip, ip, ip, vp]
+        L.npas_paged_attention_workspace_bytes.argtypes = [cache, ip, ip]
+        L.npas_paged_attention_workspace_bytes.restype = C.c_size_t
+        L.npas_paged_attention.argtypes = [cache, vp, i64, vp, vp, ip, vp, ip, ip, C.c_float, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -361,3 +376,77 @@ class Stack:
 
     def run(self, x, y, N, workspace, workspace_bytes, stream=None):
         (_calls or _load_calls()).run_stack(self, x, y, N, workspace, workspace_bytes, stream)
+
+
+# ---- a decoder block around its linear layers ----------------------------------
+
+def _rows(t, width):
+    """(device pointer, elements from row to row) of rows of `width` elements: a tensor whose rows are contiguous (a slice of a joined
+    projection, [rows][width] or [rows][heads][head_dim]), or the address of contiguous rows."""
+    if t is None or isinstance(t, int):
+        return t, width
+    inner = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        assert size == 1 or stride == inner, "rows are not contiguous"
+        inner *= size
+    assert inner == width, f"rows of {inner} elements, {width} expected"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+
+
+class KvCache:
+    """A paged cache of keys and values: k, v [pages][kv_heads][page_size][head_dim] (16-bit), page_table int32 [sequences][pages of the
+    longest]; keeps the tensors alive.  dtype: BF16 or F16."""
+
+    def __init__(self, k, v, page_table, dtype):
+        assert k.dim() == 4 and tuple(k.shape) == tuple(v.shape), "keys and values are [pages][kv_heads][page_size][head_dim]"
+        assert page_table.dim() == 2 and page_table.element_size() == 4 and not page_table.is_floating_point(), "page_table is int32"
+        self.k, self.v, self.page_table, self.dtype = k, v, page_table, dtype
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.sequences = page_table.shape[0]
+        self.desc = KvCacheDesc(_dev(k), _dev(v), _dev(page_table), dtype, self.pages, self.page_size, self.kv_heads, self.head_dim,
+                                self.sequences, page_table.shape[1])
+        self.handle = C.c_void_p(C.addressof(self.desc))
+
+
+def gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate=None, post_weight=None, pre_weight=None, residual_scale=1.0, eps=1e-6,
+                        stream=None):
+    """Norm of a block's output, its gate, the scaled residual and the norm before the next block (npas_gated_residual_norm).  gate: one
+    row [D] or [1][D] for all tokens, or a row a token [T][D] (its rows may be a slice's)."""
+    g, gs = None, 0
+    if gate is not None and not isinstance(gate, int):
+        if gate.dim() == 1 or gate.shape[0] == 1:
+            g = _dev(gate)
+            assert gate.numel() == D, "gate is [D], [1][D] or [T][D]"
+        else:
+            assert gate.shape[0] == T, "gate is [D], [1][D] or [T][D]"
+            g, gs = _rows(gate, D)
+    elif gate is not None:
+        g, gs = gate, D
+    _check(lib().npas_gated_residual_norm(_dev(branch), _dev(h), g, gs, _dev(post_weight), _dev(pre_weight), residual_scale, eps,
+                                          _dev(h_out), _dev(n_out), T, D, dtype, stream))
+
+
+def kv_append(cache, q, k, v, q_out, T, heads, positions, sequences=None, cos_sin=None, rot_dim=0, kind=ROTATE_HALVES, stream=None):
+    """Rotates queries and keys and writes keys and values into the paged cache (npas_kv_append).  q, k, v: rows of T tokens, slices of a
+    joined projection allowed; positions, sequences int32 [T]; cos_sin fp32 [positions][rot_dim]."""
+    D = cache.head_dim
+    qp, qs = _rows(q, heads * D)
+    kp, ks = _rows(k, cache.kv_heads * D)
+    vp, vs = _rows(v, cache.kv_heads * D)
+    count = 0
+    if cos_sin is not None and rot_dim:
+        count = cos_sin.shape[0]
+        assert cos_sin.shape[1] == rot_dim, "cos_sin is [positions][rot_dim]"
+    _check(lib().npas_kv_append(cache.desc, qp, qs, kp, ks, vp, vs, _dev(q_out), T, heads, _dev(sequences), _dev(positions),
+                                _dev(cos_sin), count, rot_dim, kind, stream))
+
+
+def paged_attention_workspace_bytes(cache, heads, max_length):
+    return int(lib().npas_paged_attention_workspace_bytes(cache.desc, heads, max_length))
+
+
+def paged_attention(cache, q, y, heads, lengths, max_length, scale, window=0, lse=None, workspace=None, workspace_bytes=0, stream=None):
+    """Attention of one new token a sequence over the paged cache (npas_paged_attention); lengths int32 [sequences]."""
+    qp, qs = _rows(q, heads * cache.head_dim)
+    _check(lib().npas_paged_attention(cache.desc, qp, qs, _dev(y), _dev(lse), heads, _dev(lengths), max_length, window, scale,
+                                      _dev(workspace), workspace_bytes, stream))

@@ -1,0 +1,284 @@
+// Decoder-block kernels that move rows once: norm / gate / residual / norm, and the append of rotated keys and values to a
+// paged cache.
+#include <type_traits>
+
+#include "decoder_internal.h"
+#include "device_util.h"
+
+namespace npas {
+
+// Eight consecutive elements as fp32 and back, at the alignment of one element: global loads and stores of 16 bytes need no more on
+// this architecture.  n < 8: the first n, zeros behind them.
+struct __attribute__((packed, aligned(2))) Words16 {
+    uint32_t w[4];
+};
+struct __attribute__((packed, aligned(4))) Floats8 {
+    float f[8];
+};
+template <int DT> __device__ __forceinline__ void load8(const void *p, size_t i, int n, float (&v)[8])
+{
+    if (n >= 8) {
+        if constexpr (DT == NPAS_F32) {
+            const Floats8 x = *reinterpret_cast<const Floats8 *>(reinterpret_cast<const float *>(p) + i);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = x.f[k];
+        } else {
+            const Words16 x = *reinterpret_cast<const Words16 *>(reinterpret_cast<const uint16_t *>(p) + i);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = from_storage<DT>((uint16_t)(x.w[k >> 1] >> (k & 1) * 16));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < n ? ld_act<DT>(p, i + k) : 0.f;
+    }
+}
+template <int DT> __device__ __forceinline__ void store8(void *p, size_t i, int n, const float (&v)[8])
+{
+    if (n >= 8) {
+        if constexpr (DT == NPAS_F32) {
+            Floats8 x;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x.f[k] = v[k];
+            *reinterpret_cast<Floats8 *>(reinterpret_cast<float *>(p) + i) = x;
+        } else {
+            Words16 x;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x.w[k] = pack2<DT>(v[2 * k], v[2 * k + 1]);
+            *reinterpret_cast<Words16 *>(reinterpret_cast<uint16_t *>(p) + i) = x;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+            if (k < n) st_act<DT>(p, i + k, v[k]);
+    }
+}
+
+// Sum over a row's WPR waves, the same in every lane; the waves' sums are added in their order.
+template <int WPR> __device__ __forceinline__ float row_sum(float v, float *part)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if constexpr (WPR > 1) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) v += part[w];
+    }
+    return v;
+}
+
+// One pass over a row that stays in registers: WPR waves a row (four rows a workgroup where one wave is a row), NV vectors of 8
+// elements a thread.
+template <int DT, int NV, int WPR> __global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void gated_residual_norm_kernel(NormArgs a)
+{
+    constexpr int THREADS = 64 * WPR;
+    __shared__ float part[2][WPR];
+    const int row = WPR == 1 ? (int)(blockIdx.x * 4 + (threadIdx.x >> 6)) : (int)blockIdx.x;
+    const int tid = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
+    if (WPR == 1 && row >= a.T) return;
+    const size_t at = (size_t)row * a.D;
+    float b[NV][8], h[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = (tid + j * THREADS) * 8, n = a.D - i;
+        load8<DT>(a.h, at + i, n, h[j]);
+        if (a.branch) load8<DT>(a.branch, at + i, n, b[j]);
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) b[j][k] = 0.f;
+    }
+    if (a.branch) {
+        float r = 1.f;
+        if (a.post) {
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s = fmaf(b[j][k], b[j][k], s);
+            r = 1.f / sqrtf(row_sum<WPR>(s, part[0]) * a.inv_d + a.eps);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = (tid + j * THREADS) * 8, n = a.D - i;
+            float w[8], g[8];
+            if (a.post) {
+                load8<NPAS_F32>(a.post, i, n, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) b[j][k] *= r * w[k];
+            }
+            if (a.gate) {
+                load8<DT>(a.gate, (size_t)row * a.gate_stride + i, n, g);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) b[j][k] *= g[k];
+            }
+        }
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            h[j][k] = fmaf(a.scale, h[j][k], b[j][k]);
+            s = fmaf(h[j][k], h[j][k], s);
+        }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = (tid + j * THREADS) * 8;
+        store8<DT>(a.h_out, at + i, a.D - i, h[j]);
+    }
+    if (!a.pre) return;
+    const float r = 1.f / sqrtf(row_sum<WPR>(s, part[1]) * a.inv_d + a.eps);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = (tid + j * THREADS) * 8, n = a.D - i;
+        float w[8];
+        load8<NPAS_F32>(a.pre, i, n, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] *= h[j][k] * r;
+        store8<DT>(a.n_out, at + i, n, w);
+    }
+}
+
+// Rows too long for registers: three walks over the row, the last of which forms h_out again and writes it (h_out may be h).
+template <int DT> __global__ __launch_bounds__(1024) void gated_residual_norm_long_kernel(NormArgs a)
+{
+    __shared__ float part[2][16];
+    const int row = blockIdx.x;
+    const size_t at = (size_t)row * a.D;
+    float r = 1.f;
+    if (a.branch && a.post) {
+        float s = 0.f;
+        for (int i = threadIdx.x; i < a.D; i += 1024) {
+            const float b = ld_act<DT>(a.branch, at + i);
+            s = fmaf(b, b, s);
+        }
+        r = 1.f / sqrtf(row_sum<16>(s, part[0]) * a.inv_d + a.eps);
+    }
+    auto value = [&](int i) {
+        float b = a.branch ? ld_act<DT>(a.branch, at + i) : 0.f;
+        if (a.branch && a.post) b *= r * a.post[i];
+        if (a.branch && a.gate) b *= ld_act<DT>(a.gate, (size_t)row * a.gate_stride + i);
+        return fmaf(a.scale, ld_act<DT>(a.h, at + i), b);
+    };
+    float q = 1.f;
+    if (a.pre) {
+        float s = 0.f;
+        for (int i = threadIdx.x; i < a.D; i += 1024) {
+            const float h = value(i);
+            s = fmaf(h, h, s);
+        }
+        q = 1.f / sqrtf(row_sum<16>(s, part[1]) * a.inv_d + a.eps);
+    }
+    for (int i = threadIdx.x; i < a.D; i += 1024) {
+        const float h = value(i);
+        st_act<DT>(a.h_out, at + i, h);
+        if (a.pre) st_act<DT>(a.n_out, at + i, a.pre[i] * (h * q));
+    }
+}
+
+template <typename F> static void with_dtype(int dt, F &&f)
+{
+    if (dt == NPAS_F32) f(std::integral_constant<int, NPAS_F32>{});
+    else if (dt == NPAS_BF16) f(std::integral_constant<int, NPAS_BF16>{});
+    else f(std::integral_constant<int, NPAS_F16>{});
+}
+
+int launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return NPAS_OK;
+    set_error("%s launch failed: %s", what, hipGetErrorString(e));
+    return NPAS_E_HIP;
+}
+
+int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream)
+{
+    hipStream_t st = (hipStream_t)stream;
+    with_dtype(dt, [&](auto dtc) {
+        constexpr int DT = decltype(dtc)::value;
+        const dim3 rows((unsigned)a.T), quads((unsigned)((a.T + 3) / 4));
+        if (a.D <= 512) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 1>), quads, dim3(256), 0, st, a);
+        else if (a.D <= 1024) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 1>), quads, dim3(256), 0, st, a);
+        else if (a.D <= 2048) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 4>), rows, dim3(256), 0, st, a);
+        else if (a.D <= 4096) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 4>), rows, dim3(256), 0, st, a);
+        else if (a.D <= 8192) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 8>), rows, dim3(512), 0, st, a);
+        else if (a.D <= 16384) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 16>), rows, dim3(1024), 0, st, a);
+        else hipLaunchKernelGGL((gated_residual_norm_long_kernel<DT>), rows, dim3(1024), 0, st, a);
+    });
+    return launched("gated residual norm");
+}
+
+// ---- append to the paged cache -------------------------------------------------
+
+// One workgroup a token.  A unit is VL consecutive elements: rotated in themselves (PAIRS), rotated with their partners rot_dim / 2
+// further on (halves), or copied (the rest of a rotated head, the values).  Queries first, then keys, then values.
+template <int DT, int VL, bool PAIRS> __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a)
+{
+    const int t = blockIdx.x, D = a.c.head_dim, half = a.rot_dim / 2;
+    const int s = a.sequence ? a.sequence[t] : t, pos = a.position[t];
+    const bool token = (uint32_t)s < (uint32_t)a.c.sequences && pos >= 0 && (a.rot_dim == 0 || pos < a.positions);
+    const int column = token ? pos / a.c.page_size : 0, slot = token ? pos - column * a.c.page_size : 0;
+    const int page = token && column < a.c.table_stride ? a.c.table[(size_t)s * a.c.table_stride + column] : -1;
+    const bool stored = (uint32_t)page < (uint32_t)a.c.pages;
+    const size_t row0 = stored ? (size_t)page * a.c.kv_heads * a.c.page_size + slot : 0; // cache row of the first head
+    const float *cs = a.cos_sin + (size_t)(token ? pos : 0) * a.rot_dim;
+    const int rot_units = (PAIRS ? a.rot_dim : half) / VL, head_units = rot_units + (D - a.rot_dim) / VL, value_units = D / VL;
+    const int nq = a.q ? a.heads * head_units : 0, nk = a.c.kv_heads * head_units, nv = a.c.kv_heads * value_units;
+    for (int u = threadIdx.x; u < nq + nk + nv; u += 256) {
+        const bool is_q = u < nq, is_v = u >= nq + nk;
+        if (!is_q && !stored) break;
+        const int w = is_q ? u : is_v ? u - nq - nk : u - nq, per = is_v ? value_units : head_units, head = w / per, j = w - head * per;
+        const bool rotated = !is_v && j < rot_units;
+        const int d = is_v ? j * VL : rotated ? j * VL : a.rot_dim + (j - rot_units) * VL;
+        const void *src = is_q ? a.q : is_v ? a.v : a.k;
+        void *dst = is_q ? a.q_out : is_v ? a.c.v : a.c.k;
+        const size_t in = (size_t)t * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (size_t)head * D + d;
+        const size_t out = (is_q ? ((size_t)t * a.heads + head) * D : (row0 + (size_t)head * a.c.page_size) * D) + d;
+        float x[8], p[8];
+        load8<DT>(src, in, VL, x);
+        if (!PAIRS && rotated) load8<DT>(src, in + half, VL, p);
+        if (!token) { // only queries come here
+#pragma unroll
+            for (int k = 0; k < VL; ++k) x[k] = p[k] = 0.f;
+        } else if (PAIRS && rotated) {
+#pragma unroll
+            for (int k = 0; k < VL / 2; ++k) {
+                const float c = cs[d / 2 + k], n = cs[half + d / 2 + k], u0 = x[2 * k], u1 = x[2 * k + 1];
+                x[2 * k] = u0 * c - u1 * n;
+                x[2 * k + 1] = u1 * c + u0 * n;
+            }
+        } else if (rotated) {
+#pragma unroll
+            for (int k = 0; k < VL; ++k) {
+                const float c = cs[d + k], n = cs[half + d + k], u0 = x[k], u1 = p[k];
+                x[k] = u0 * c - u1 * n;
+                p[k] = u1 * c + u0 * n;
+            }
+        }
+        store8<DT>(dst, out, VL, x);
+        if (!PAIRS && rotated) store8<DT>(dst, out + half, VL, p);
+    }
+}
+
+int launch_kv_append(int dt, const AppendArgs &a, void *stream)
+{
+    hipStream_t st = (hipStream_t)stream;
+    auto pick = [&](auto dtc) {
+        constexpr int DT = decltype(dtc)::value;
+        const dim3 grid((unsigned)a.T), block(256);
+        // vectors of 8 where a pair's elements, or the two halves' vectors, start at multiples of 8 (the head's rest then does too)
+        if (a.pairs) {
+            if (a.rot_dim % 8 == 0) hipLaunchKernelGGL((kv_append_kernel<DT, 8, true>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((kv_append_kernel<DT, 2, true>), grid, block, 0, st, a);
+        } else {
+            if (a.rot_dim % 16 == 0) hipLaunchKernelGGL((kv_append_kernel<DT, 8, false>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((kv_append_kernel<DT, 1, false>), grid, block, 0, st, a);
+        }
+    };
+    if (dt == NPAS_BF16) pick(std::integral_constant<int, NPAS_BF16>{});
+    else pick(std::integral_constant<int, NPAS_F16>{});
+    return launched("cache append");
+}
+
+} // namespace npas
