@@ -51,6 +51,7 @@ extern "C" {
 
 typedef struct npas_packed npas_packed; /* one packed layer */
 typedef struct npas_stack npas_stack;   /* a wired list of layers */
+typedef struct npas_mxfp4 npas_mxfp4;   /* one linear layer in microscaled 4-bit floats */
 
 typedef enum { NPAS_F32 = 0, NPAS_BF16 = 1, NPAS_F16 = 2 } npas_dtype;
 /* ReLU6 = min(max(v, 0), 6); hard-swish (what Phase 1 of the framework puts in place of swish,
@@ -308,6 +309,32 @@ size_t npas_paged_attention_workspace_bytes(const npas_kv_cache *cache, int head
 int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t q_stride, void *y_dev, float *lse_dev, int heads,
                          const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev,
                          size_t workspace_bytes, void *hip_stream);
+
+/* ---- linear layers in microscaled 4-bit floats -------------------------------
+ * Rows are cut into blocks of 32 consecutive elements (the last may be partial: as if zeros followed).  A block has one power of two 2^e,
+ * e = floor(log2(largest magnitude)) - 2 (at least -127), kept as the byte e + 127, and per element the 4-bit float (sign, two
+ * exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) nearest to x / 2^e, ties to the even code, at most 6.  An all-zero
+ * block has byte 0; a block that holds an infinity or a NaN has byte 255 and stands for NaN throughout.
+ * codes [rows][16 * ceil(K / 32)]: two elements a byte, the lower four bits first; scales [rows][ceil(K / 32)]. */
+int npas_mxfp4_quantize(const void *x_dev, int64_t x_stride, void *codes_dev, void *scales_dev, int rows, int K, npas_dtype dt,
+                        void *hip_stream);
+/* The values that codes and scales stand for, y [rows][K] in storage type dt (a value that dt cannot hold is rounded). */
+int npas_mxfp4_dequantize(const void *codes_dev, const void *scales_dev, void *y_dev, int rows, int K, npas_dtype dt,
+                          void *hip_stream);
+
+/* FC weights W[OUT][IN] (storage type dt; one that is not finite is refused with NPAS_E_SHAPE) in microscaled 4-bit floats, blocks along IN.  Release with npas_mxfp4_free. */
+int npas_pack_fc_mxfp4(const void *w_host, int OUT, int IN, npas_dtype dt, void *hip_stream, npas_mxfp4 **out);
+/* info[0..7] = { dtype, OUT, IN, blocks of a row, device_ready, device-format bytes, reserved, reserved }. */
+int npas_mxfp4_info(const npas_mxfp4 *p, int64_t info[8]);
+/* The codes and scales of the packed weights, laid out as npas_mxfp4_quantize writes them, to caller's HOST buffers (either may be NULL). */
+int npas_mxfp4_export(const npas_mxfp4 *p, uint8_t *codes_host, uint8_t *scales_host);
+void npas_mxfp4_free(npas_mxfp4 *p);
+/* y[b][o] = act(bias[o] + sum_i Wq[o][i] xq[b][i]): x [B][IN] (row b at x + b * x_stride, the handle's storage type) is quantised to
+ * microscaled 4-bit floats, blocks along IN, and multiplied by the packed weights on the matrix cores with fp32 accumulation;
+ * y [B][OUT] contiguous, bias fp32 [OUT], nullable.  The workspace (16-byte aligned) holds the quantised activations. */
+size_t npas_fc_mxfp4_workspace_bytes(const npas_mxfp4 *p, int B);
+int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void *y_dev, int B, const void *bias_dev, npas_act act,
+                  void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -12,7 +12,8 @@ _LIB = os.path.join(_HERE, "libnpas.so")
 _CALLS = os.path.join(_HERE, "_pycalls.so")  # CPython entry points of the run calls, linked to libnpas.so
 SOURCES = ["pack.cpp", "api.cpp", "kernels.hip", "spatial_direct_kernel.hip", "small_channel_rows_kernel.hip", "small_kernels.hip", "block_kernels.hip",
            "inverted_residual_kernel.hip", "pointwise_stream_kernel.hip", "bottleneck_tail_kernel.hip", "noalloc.hip",
-           "decoder.cpp", "decoder_kernels.hip", "paged_attention_kernel.hip"]
+           "decoder.cpp", "decoder_kernels.hip", "paged_attention_kernel.hip", "mxfp4.cpp", "mxfp4_kernels.hip"]
+HEADERS = ["npas_internal.h", "device_util.h", "decoder_internal.h", "mxfp4_internal.h", "row_vectors.h"]
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "npas.h")
 
 F32, BF16, F16 = 0, 1, 2
@@ -35,6 +36,8 @@ EXPORTS = [
     "npas_run_stack", "npas_stack_num_launches", "npas_stack_free", "npas_stack_describe", "npas_debug_set_switches",
     "npas_run_stack_static", "npas_debug_launch_empty", "npas_debug_device_kernel", "npas_debug_direct_plan",
     "npas_gated_residual_norm", "npas_kv_append", "npas_paged_attention_workspace_bytes", "npas_paged_attention",
+    "npas_mxfp4_quantize", "npas_mxfp4_dequantize", "npas_pack_fc_mxfp4", "npas_mxfp4_info", "npas_mxfp4_export", "npas_mxfp4_free",
+    "npas_fc_mxfp4_workspace_bytes", "npas_fc_mxfp4",
 ]
 STATIC_WORKSPACE_BYTES = 32 << 20
 DESCRIBE_COLS = 11
@@ -51,7 +54,7 @@ def build(force: bool = True) -> str:
     import sysconfig
     from concurrent.futures import ThreadPoolExecutor
     srcs = [os.path.join(_CSRC, s) for s in SOURCES]
-    deps = srcs + [os.path.join(_CSRC, "npas_internal.h"), os.path.join(_CSRC, "device_util.h"), os.path.join(_CSRC, "decoder_internal.h"), HEADER]
+    deps = srcs + [os.path.join(_CSRC, h) for h in HEADERS] + [HEADER]
     calls = os.path.join(_CSRC, "pycalls.cpp")
     if not force and os.path.exists(_LIB) and os.path.exists(_CALLS) and \
             all(os.path.getmtime(_LIB) >= os.path.getmtime(d) for d in deps) and os.path.getmtime(_CALLS) >= os.path.getmtime(calls):
@@ -135,6 +138,16 @@ def lib():
         L.npas_paged_attention_workspace_bytes.argtypes = [cache, ip, ip]
         L.npas_paged_attention_workspace_bytes.restype = C.c_size_t
         L.npas_paged_attention.argtypes = [cache, vp, i64, vp, vp, ip, vp, ip, ip, C.c_float, vp, C.c_size_t, vp]
+        L.npas_mxfp4_quantize.argtypes = [vp, i64, vp, vp, ip, ip, ip, vp]
+        L.npas_mxfp4_dequantize.argtypes = [vp, vp, vp, ip, ip, ip, vp]
+        L.npas_pack_fc_mxfp4.argtypes = [vp, ip, ip, ip, vp, C.POINTER(vp)]
+        L.npas_mxfp4_info.argtypes = [vp, vp]
+        L.npas_mxfp4_export.argtypes = [vp, vp, vp]
+        L.npas_mxfp4_free.argtypes = [vp]
+        L.npas_mxfp4_free.restype = None
+        L.npas_fc_mxfp4_workspace_bytes.argtypes = [vp, ip]
+        L.npas_fc_mxfp4_workspace_bytes.restype = C.c_size_t
+        L.npas_fc_mxfp4.argtypes = [vp, vp, i64, vp, ip, vp, ip, vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -450,3 +463,60 @@ def paged_attention(cache, q, y, heads, lengths, max_length, scale, window=0, ls
     qp, qs = _rows(q, heads * cache.head_dim)
     _check(lib().npas_paged_attention(cache.desc, qp, qs, _dev(y), _dev(lse), heads, _dev(lengths), max_length, window, scale,
                                       _dev(workspace), workspace_bytes, stream))
+
+
+# ---- linear layers in microscaled 4-bit floats ----------------------------------
+
+def mxfp4_quantize(x, codes, scales, M, K, dtype, stream=None):
+    """Rows x [M][K] (they may be a slice's) to codes uint8 [M][16 ceil(K / 32)] and scale bytes uint8 [M][ceil(K / 32)]."""
+    xp, xs = _rows(x, K)
+    _check(lib().npas_mxfp4_quantize(xp, xs, _dev(codes), _dev(scales), M, K, dtype, stream))
+
+
+def mxfp4_dequantize(codes, scales, y, M, K, dtype, stream=None):
+    """The values that codes and scales stand for, y [M][K]."""
+    _check(lib().npas_mxfp4_dequantize(_dev(codes), _dev(scales), _dev(y), M, K, dtype, stream))
+
+
+class Mxfp4:
+    """Owner of one npas_mxfp4 handle: FC weights in microscaled 4-bit floats."""
+
+    def __init__(self, handle):
+        self.handle = handle
+        v = self.info()
+        self.OUT, self.IN = v["OUT"], v["IN"]
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            lib().npas_mxfp4_free(self.handle)
+            self.handle = None
+
+    def info(self):
+        v = np.zeros(8, dtype=np.int64)
+        _check(lib().npas_mxfp4_info(self.handle, _host(v)))
+        return dict(zip(["dtype", "OUT", "IN", "blocks", "device_ready", "device_bytes"], (int(x) for x in v)))
+
+    def export(self):
+        """Codes uint8 [OUT][16 blocks] and scale bytes uint8 [OUT][blocks], laid out as mxfp4_quantize writes them."""
+        i = self.info()
+        codes = np.zeros((i["OUT"], i["blocks"] * 16), dtype=np.uint8)
+        scales = np.zeros((i["OUT"], i["blocks"]), dtype=np.uint8)
+        _check(lib().npas_mxfp4_export(self.handle, _host(codes), _host(scales)))
+        return {"codes": codes, "scales": scales}
+
+    def workspace_bytes(self, B):
+        return int(lib().npas_fc_mxfp4_workspace_bytes(self.handle, B))
+
+
+def pack_fc_mxfp4(w, dtype, stream=None):
+    """w: NumPy [OUT][IN] in storage type (float32, or uint16 bits)."""
+    h = C.c_void_p()
+    assert w.ndim == 2 and w.dtype == _np_storage(dtype)
+    _check(lib().npas_pack_fc_mxfp4(_host(w), w.shape[0], w.shape[1], dtype, stream, C.byref(h)))
+    return Mxfp4(h)
+
+
+def fc_mxfp4(packed, x, y, B, bias=None, act=ACT_NONE, workspace=None, workspace_bytes=0, stream=None):
+    """y [B][OUT] = act(bias + x W^T) with both factors in microscaled 4-bit floats; x [B][IN] (its rows may be a slice's)."""
+    xp, xs = _rows(x, packed.IN)
+    _check(lib().npas_fc_mxfp4(packed.handle, xp, xs, _dev(y), B, _dev(bias), act, _dev(workspace), workspace_bytes, stream))

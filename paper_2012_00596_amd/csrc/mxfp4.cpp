@@ -1,0 +1,261 @@
+// C-ABI calls of the linear layers in microscaled 4-bit floats: packing on the host, argument checks, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <new>
+
+#include "mxfp4_internal.h"
+
+using namespace npas;
+
+namespace {
+
+bool misaligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+int check_dtype(int dt)
+{
+    if (dt == NPAS_F32 || dt == NPAS_BF16 || dt == NPAS_F16) return NPAS_OK;
+    set_error("unknown storage type %d", dt);
+    return NPAS_E_DTYPE;
+}
+
+float f16_value(uint16_t h)
+{
+    const int e = h >> 10 & 31, m = h & 1023;
+    const float v = e == 31 ? (m ? NAN : INFINITY) : e ? std::ldexp((float)(m | 1024), e - 25) : std::ldexp((float)m, -24);
+    return h & 0x8000 ? -v : v;
+}
+
+float element(const void *w, size_t i, int dt)
+{
+    if (dt == NPAS_F32) return ((const float *)w)[i];
+    const uint16_t b = ((const uint16_t *)w)[i];
+    if (dt == NPAS_F16) return f16_value(b);
+    const uint32_t u = (uint32_t)b << 16;
+    float v;
+    memcpy(&v, &u, 4);
+    return v;
+}
+
+// One block of n <= 32 values to 16 bytes of codes and the scale byte; false where a value is not finite.
+bool encode_block(const float *v, int n, uint8_t codes[16], uint8_t *scale)
+{
+    uint32_t top = 0;
+    for (int i = 0; i < n; ++i) {
+        uint32_t u;
+        memcpy(&u, v + i, 4);
+        top = std::max(top, u & 0x7fffffffu);
+    }
+    const int e = (int)(top >> 23);
+    if (e == 255) return false;
+    *scale = (uint8_t)(e > 2 ? e - 2 : 0);
+    const double inv = std::ldexp(1.0, 127 - *scale);
+    memset(codes, 0, 16);
+    for (int i = 0; i < n; ++i) {
+        const double a = std::fabs((double)v[i] * inv);
+        // between two neighbouring values the even code takes the middle
+        const unsigned c = (a > 0.25) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0);
+        codes[i >> 1] |= (uint8_t)((c | (std::signbit(v[i]) ? 8u : 0u)) << (i & 1) * 4);
+    }
+    return true;
+}
+
+int upload(npas_mxfp4 *p, void *hip_stream)
+{
+    int ndev = 0, dev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0 || hipGetDevice(&dev) != hipSuccess) {
+        (void)hipGetLastError();
+        return NPAS_OK; // host-only handle: export works, run calls fail loudly
+    }
+    const size_t images = (size_t)p->groups * p->steps * 4096, words = (size_t)p->groups * p->quads * 256;
+    std::vector<uint8_t> blob(images + words * 4, 0);
+    uint8_t *sc = blob.data() + images;
+    for (int o = 0; o < p->OUT; ++o) {
+        const int g = o >> 6, r = (o & 63) >> 2, j = o & 3;
+        for (int b = 0; b < p->blocks; ++b) {
+            const int step = b >> 2, lane = (b & 3) * 16 + r;
+            memcpy(&blob[(((size_t)g * p->steps + step) * 4 + j) * 1024 + lane * 16], &p->codes[((size_t)o * p->blocks + b) * 16], 16);
+            sc[((((size_t)g * p->quads + (step >> 2)) * 4 + j) * 64 + lane) * 4 + (step & 3)] = p->scales[(size_t)o * p->blocks + b];
+        }
+    }
+    void *ptr = nullptr;
+    hipError_t e = hipMalloc(&ptr, blob.size());
+    if (e != hipSuccess) {
+        set_error("hipMalloc(%zu) failed: %s", blob.size(), hipGetErrorString(e));
+        return NPAS_E_HIP;
+    }
+    // on the caller's stream; the source is a local buffer, so wait for the copy before it goes away
+    e = hipMemcpyAsync(ptr, blob.data(), blob.size(), hipMemcpyHostToDevice, (hipStream_t)hip_stream);
+    if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)hip_stream);
+    if (e != hipSuccess) {
+        (void)hipFree(ptr);
+        set_error("hipMemcpy to device failed: %s", hipGetErrorString(e));
+        return NPAS_E_HIP;
+    }
+    p->device = dev;
+    p->blob = ptr;
+    p->bytes = blob.size();
+    p->images = ptr;
+    p->image_scales = (const uint32_t *)((const uint8_t *)ptr + images);
+    return NPAS_OK;
+}
+
+int check_rows(const void *a, const void *b, const void *c, int rows, int K, int dt)
+{
+    if (!a || !b || !c) {
+        set_error("NULL argument");
+        return NPAS_E_NULL;
+    }
+    if (int rc = check_dtype(dt)) return rc;
+    if (rows <= 0 || K <= 0 || K > 1 << 24) {
+        set_error("bad shape rows=%d K=%d", rows, K);
+        return NPAS_E_SHAPE;
+    }
+    return NPAS_OK;
+}
+
+// Activations in the workspace: images of 16 rows, then their scale words.
+size_t image_bytes(const npas_mxfp4 *p, int B) { return (size_t)((B + 15) / 16) * p->steps * 1024; }
+
+} // namespace
+
+extern "C" {
+
+int npas_mxfp4_quantize(const void *x_dev, int64_t x_stride, void *codes_dev, void *scales_dev, int rows, int K, npas_dtype dt,
+                        void *hip_stream)
+{
+    if (int rc = check_rows(x_dev, codes_dev, scales_dev, rows, K, dt)) return rc;
+    if (x_stride < K || x_stride > (int64_t)1 << 40 || misaligned(x_dev, dtype_size(dt)) || misaligned(codes_dev, 4)) {
+        set_error("row stride %lld of %d elements, or a pointer that is not aligned (x to its element, codes to 4 bytes)", (long long)x_stride, K);
+        return NPAS_E_SHAPE;
+    }
+    QuantizeArgs a{x_dev, (uint8_t *)codes_dev, (uint8_t *)scales_dev, x_stride, rows, K, (K + 31) / 32, 0, 0};
+    return launch_mxfp4_quantize(dt, a, hip_stream);
+}
+
+int npas_mxfp4_dequantize(const void *codes_dev, const void *scales_dev, void *y_dev, int rows, int K, npas_dtype dt,
+                          void *hip_stream)
+{
+    if (int rc = check_rows(codes_dev, scales_dev, y_dev, rows, K, dt)) return rc;
+    if (misaligned(y_dev, dtype_size(dt)) || misaligned(codes_dev, 4)) {
+        set_error("a pointer that is not aligned (y to its element, codes to 4 bytes)");
+        return NPAS_E_SHAPE;
+    }
+    DequantizeArgs a{(const uint8_t *)codes_dev, (const uint8_t *)scales_dev, y_dev, rows, K, (K + 31) / 32};
+    return launch_mxfp4_dequantize(dt, a, hip_stream);
+}
+
+int npas_pack_fc_mxfp4(const void *w_host, int OUT, int IN, npas_dtype dt, void *hip_stream, npas_mxfp4 **out)
+{
+    if (!w_host || !out) {
+        set_error("NULL argument (w_host=%p out=%p)", w_host, (void *)out);
+        return NPAS_E_NULL;
+    }
+    *out = nullptr;
+    if (OUT <= 0 || IN <= 0 || OUT > 1 << 24 || IN > 1 << 24) {
+        set_error("bad shape OUT=%d IN=%d", OUT, IN);
+        return NPAS_E_SHAPE;
+    }
+    if (int rc = check_dtype(dt)) return rc;
+    try {
+        std::unique_ptr<npas_mxfp4> p(new npas_mxfp4);
+        p->dtype = dt; p->OUT = OUT; p->IN = IN;
+        p->blocks = (IN + 31) / 32; p->steps = (p->blocks + 3) / 4; p->quads = (p->steps + 3) / 4; p->groups = (OUT + 63) / 64;
+        p->codes.resize((size_t)OUT * p->blocks * 16);
+        p->scales.resize((size_t)OUT * p->blocks);
+        float v[32];
+        for (int o = 0; o < OUT; ++o)
+            for (int b = 0; b < p->blocks; ++b) {
+                const int n = std::min(32, IN - b * 32);
+                for (int i = 0; i < n; ++i) v[i] = element(w_host, (size_t)o * IN + b * 32 + i, dt);
+                const size_t at = (size_t)o * p->blocks + b;
+                if (!encode_block(v, n, &p->codes[at * 16], &p->scales[at])) {
+                    set_error("a weight of output %d, inputs %d .. %d, is not finite", o, b * 32, b * 32 + n - 1);
+                    return NPAS_E_SHAPE;
+                }
+            }
+        if (int rc = upload(p.get(), hip_stream)) return rc;
+        *out = p.release();
+        return NPAS_OK;
+    } catch (const std::bad_alloc &) {
+        set_error("out of host memory packing %d x %d weights", OUT, IN);
+        return NPAS_E_SHAPE;
+    }
+}
+
+int npas_mxfp4_info(const npas_mxfp4 *p, int64_t info[8])
+{
+    if (!p || !info) {
+        set_error("NULL argument");
+        return NPAS_E_NULL;
+    }
+    const int64_t v[8] = {p->dtype, p->OUT, p->IN, p->blocks, p->device >= 0, (int64_t)p->bytes, 0, 0};
+    memcpy(info, v, sizeof(v));
+    return NPAS_OK;
+}
+
+int npas_mxfp4_export(const npas_mxfp4 *p, uint8_t *codes_host, uint8_t *scales_host)
+{
+    if (!p) {
+        set_error("NULL handle");
+        return NPAS_E_NULL;
+    }
+    if (codes_host) memcpy(codes_host, p->codes.data(), p->codes.size());
+    if (scales_host) memcpy(scales_host, p->scales.data(), p->scales.size());
+    return NPAS_OK;
+}
+
+void npas_mxfp4_free(npas_mxfp4 *p)
+{
+    if (!p) return;
+    if (p->blob) (void)hipFree(p->blob);
+    delete p;
+}
+
+size_t npas_fc_mxfp4_workspace_bytes(const npas_mxfp4 *p, int B)
+{
+    if (!p || B <= 0) return 0;
+    return image_bytes(p, B) + (size_t)((B + 15) / 16) * p->quads * 256;
+}
+
+int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void *y_dev, int B, const void *bias_dev, npas_act act,
+                  void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    if (!p || !x_dev || !y_dev) {
+        set_error("NULL argument (handle=%p x_dev=%p y_dev=%p)", (const void *)p, x_dev, y_dev);
+        return NPAS_E_NULL;
+    }
+    if (B <= 0 || x_stride < p->IN || x_stride > (int64_t)1 << 40 || (double)((B + 15) / 16) * p->groups > 2147483647.0 ||
+        (double)((B + 15) / 16) * p->steps > 2147483647.0) {
+        set_error("bad shape B=%d, row stride %lld of %d elements", B, (long long)x_stride, p->IN);
+        return NPAS_E_SHAPE;
+    }
+    if (!valid_act(act)) {
+        set_error("unknown activation %d", (int)act);
+        return NPAS_E_SHAPE;
+    }
+    if (misaligned(x_dev, dtype_size(p->dtype)) || misaligned(y_dev, dtype_size(p->dtype)) || misaligned(bias_dev, 4)) {
+        set_error("a pointer is not aligned to its element type");
+        return NPAS_E_SHAPE;
+    }
+    const size_t need = npas_fc_mxfp4_workspace_bytes(p, B);
+    if (need && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 16))) {
+        set_error("the layer needs %zu bytes of workspace at a multiple of 16 for %d rows, got %zu at %p", need, B, workspace_bytes, workspace_dev);
+        return NPAS_E_WORKSPACE;
+    }
+    if (p->device < 0) {
+        set_error("packed layer has no device copy (packed on a machine without a GPU)");
+        return NPAS_E_HIP;
+    }
+    uint8_t *images = (uint8_t *)workspace_dev, *words = images + image_bytes(p, B);
+    QuantizeArgs q{x_dev, images, words, x_stride, B, p->IN, p->blocks, p->steps, p->quads};
+    if (int rc = launch_mxfp4_quantize_images(p->dtype, q, hip_stream)) return rc;
+    FcMxArgs a{images, (const uint32_t *)words, p->images, p->image_scales, (const float *)bias_dev, y_dev, B, p->OUT, p->steps, p->quads,
+               p->groups, (B + 15) / 16, act};
+    return launch_fc_mxfp4(p->dtype, a, hip_stream);
+}
+
+} // extern "C"

@@ -1,0 +1,305 @@
+"""Microscaled 4-bit floats through the C ABI: codes and scales bit for bit against the definition, products against 64-bit sums of
+the values that the codes stand for; and what is refused.
+
+Tolerance of a product: a sum of IN exact terms in fp32, at worst added one after another (one instruction's 128 terms, then the
+instructions), so (128 + IN / 128) 2^-24 of the terms' magnitudes, and the storage type's rounding of the result."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import paper_2012_00596_amd as npas
+from workloads import dtypes
+
+U = {npas.F32: 2.0 ** -24, npas.BF16: 2.0 ** -8, npas.F16: 2.0 ** -11}
+TINY = {npas.F32: 2.0 ** -149, npas.BF16: 2.0 ** -133, npas.F16: 2.0 ** -25}
+GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+DT = [npas.F32, npas.BF16, npas.F16]
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available(), "GPU tests need a GPU"
+    return t
+
+
+def reference(x):
+    """(codes [M][16 blocks], scales [M][blocks]) of x (float64 values of a storage type); NaN blocks have scale 255, codes 0."""
+    M, K = x.shape
+    nb = -(-K // 32)
+    b = np.zeros((M, nb * 32))
+    b[:, :K] = x
+    b = b.reshape(M, nb, 32)
+    bad = ~np.isfinite(b).all(-1)
+    top = np.where(bad, 0.0, np.abs(np.where(np.isfinite(b), b, 0)).max(-1))
+    e = np.where(top > 0, np.frexp(top)[1] - 3, -127)
+    e = np.maximum(e, -127)
+    r = np.abs(np.where(bad[..., None], 0.0, b)) * np.exp2(-e.astype(np.float64))[..., None]
+    dist = np.abs(r[..., None] - GRID)                              # nearest value; of two equally near ones the even code
+    near = dist == dist.min(-1, keepdims=True)
+    code = np.where(near[..., ::2].any(-1), near[..., ::2].argmax(-1) * 2, near[..., 1::2].argmax(-1) * 2 + 1).astype(np.uint8)
+    code |= (np.signbit(b) & ~bad[..., None]).astype(np.uint8) << 3
+    packed = code[..., ::2] | code[..., 1::2] << 4
+    return packed.reshape(M, nb * 16), np.where(bad, 255, e + 127).astype(np.uint8)
+
+
+def values(codes, scales, K):
+    """float64 values [M][K] of codes and scales."""
+    M = codes.shape[0]
+    c = np.stack([codes & 15, codes >> 4], -1).reshape(M, -1, 32)
+    v = GRID[c & 7] * np.where(c & 8, -1.0, 1.0) * np.exp2(scales.astype(np.float64) - 127)[..., None]
+    v = np.where((scales == 255)[..., None], np.nan, v)
+    return v.reshape(M, -1)[:, :K]
+
+
+def sample(seed, shape, dt, kind="wide"):
+    """(storage, float64 values): magnitudes over many powers of two, ties of the grid among them."""
+    rng = np.random.default_rng(seed)
+    v = rng.standard_normal(shape)
+    if kind == "wide":
+        v = v * np.exp2(rng.integers(-6, 7, shape))
+        v[..., ::7] = np.round(v[..., ::7] * 4) / 4                  # multiples of 1/4: many fall between two codes
+        v[..., ::11] = 0
+    return dtypes.quantize(v, dt)
+
+
+def edge_rows(dt):
+    """Blocks that a type's range puts at the edge: zeros, smallest and largest numbers, ties, infinities, NaN, -0."""
+    big, small = {npas.F32: (3.4e38, 2.0 ** -149), npas.BF16: (3.3e38, 2.0 ** -133), npas.F16: (65504.0, 2.0 ** -24)}[dt]
+    rows = np.zeros((12, 64))
+    rows[1, 3], rows[1, 40] = big, -big
+    rows[2, :] = small * np.arange(64)
+    rows[3, :32] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 6.5, 5.5, -0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5.0, -7.0] + [4.0] * 14
+    rows[4, 5] = np.inf
+    rows[5, 33] = np.nan
+    rows[6, 0], rows[6, 1] = -np.inf, np.nan
+    rows[7, :] = -0.0
+    rows[8, :] = 2.0 ** -14
+    rows[9, :32] = np.ldexp(1.0, -10) * np.arange(32)
+    rows[10, 0], rows[10, 1:] = 1.0, small
+    rows[11, :] = -1e-3
+    return dtypes.quantize(rows, dt)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("OUT,IN", [(1, 1), (3, 31), (64, 32), (65, 33), (7, 130), (130, 513), (16, 1024)])
+def test_packed_weights_bit_exact(dt, OUT, IN):
+    store, exact = sample(OUT + IN, (OUT, IN), dt)
+    p = npas.pack_fc_mxfp4(store, dt)
+    codes, scales = reference(exact)
+    e = p.export()
+    np.testing.assert_array_equal(e["scales"], scales)
+    np.testing.assert_array_equal(e["codes"], codes)
+    i = p.info()
+    assert (i["OUT"], i["IN"], i["dtype"], i["blocks"]) == (OUT, IN, dt, -(-IN // 32))
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_packed_weights_at_the_edges_of_the_type(dt):
+    store, exact = edge_rows(dt)
+    finite = np.isfinite(exact).all(1)
+    e = npas.pack_fc_mxfp4(np.ascontiguousarray(store[finite]), dt).export()
+    codes, scales = reference(exact[finite])
+    np.testing.assert_array_equal(e["scales"], scales)
+    np.testing.assert_array_equal(e["codes"], codes)
+    for r in np.flatnonzero(~finite):
+        with pytest.raises(npas.NpasError) as err:
+            npas.pack_fc_mxfp4(np.ascontiguousarray(store[r:r + 1]), dt)
+        assert err.value.code == npas.E_SHAPE and "not finite" in str(err.value)
+
+
+def test_refusals():
+    L, h = npas.lib(), ctypes.c_void_p()
+    w = np.ones((4, 40), np.float32)
+    ptr = w.ctypes.data
+    for args, code in [((None, 4, 40, 0, None, ctypes.byref(h)), npas.E_NULL), ((ptr, 4, 40, 0, None, None), npas.E_NULL),
+                       ((ptr, 0, 40, 0, None, ctypes.byref(h)), npas.E_SHAPE), ((ptr, 4, -1, 0, None, ctypes.byref(h)), npas.E_SHAPE),
+                       ((ptr, 2 ** 25, 40, 0, None, ctypes.byref(h)), npas.E_SHAPE), ((ptr, 4, 40, 5, None, ctypes.byref(h)), npas.E_DTYPE)]:
+        assert L.npas_pack_fc_mxfp4(*args) == code
+    p = npas.pack_fc_mxfp4(w, npas.F32)
+    need = p.workspace_bytes(3)
+    good = [p.handle, 64, 40, 128, 3, None, 0, 256, need, None]
+    for at, value, code in [(0, None, npas.E_NULL), (1, None, npas.E_NULL), (3, None, npas.E_NULL), (2, 39, npas.E_SHAPE), (4, 0, npas.E_SHAPE),
+                            (6, 9, npas.E_SHAPE), (1, 66, npas.E_SHAPE), (5, 66, npas.E_SHAPE)] + \
+            ([(7, None, npas.E_WORKSPACE), (7, 264, npas.E_WORKSPACE), (8, need - 1, npas.E_WORKSPACE)] if need else []):
+        args = list(good)
+        args[at] = value
+        assert L.npas_fc_mxfp4(*args) == code, (at, value)
+    if not p.info()["device_ready"]:
+        assert L.npas_fc_mxfp4(*good) == npas.E_HIP
+    for f, good in ((L.npas_mxfp4_quantize, [64, 40, 128, 256, 3, 40, npas.BF16, None]),):
+        for at, value, code in [(0, None, npas.E_NULL), (2, None, npas.E_NULL), (3, None, npas.E_NULL), (1, 39, npas.E_SHAPE), (4, 0, npas.E_SHAPE),
+                                (5, 0, npas.E_SHAPE), (6, 3, npas.E_DTYPE), (0, 65, npas.E_SHAPE), (2, 130, npas.E_SHAPE)]:
+            args = list(good)
+            args[at] = value
+            assert f(*args) == code, (at, value)
+    good = [64, 128, 256, 3, 40, npas.BF16, None]
+    for at, value, code in [(0, None, npas.E_NULL), (1, None, npas.E_NULL), (2, None, npas.E_NULL), (3, 0, npas.E_SHAPE), (4, -1, npas.E_SHAPE),
+                            (5, 7, npas.E_DTYPE), (0, 66, npas.E_SHAPE), (2, 257, npas.E_SHAPE)]:
+        args = list(good)
+        args[at] = value
+        assert L.npas_mxfp4_dequantize(*args) == code, (at, value)
+    assert L.npas_mxfp4_info(None, None) == npas.E_NULL and L.npas_mxfp4_export(None, None, None) == npas.E_NULL
+    assert L.npas_fc_mxfp4_workspace_bytes(None, 3) == 0
+
+
+def _dev(torch, store, dt):
+    a = np.ascontiguousarray(store)
+    return torch.from_numpy(a).cuda() if dt == npas.F32 else torch.from_numpy(a.view(np.int16)).cuda()
+
+
+def _td(torch, dt):
+    return torch.float32 if dt == npas.F32 else torch.int16
+
+
+def _f64(t, dt):
+    a = t.cpu().numpy()
+    return dtypes.storage_to_f64(a if dt == npas.F32 else a.view(np.uint16), dt)
+
+
+@gpu
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 32), (3, 31), (5, 33), (2, 257), (17, 1280), (3, 2049), (200, 96), (1, 20000)])
+def test_quantize_and_back(torch, dt, M, K):
+    store, exact = sample(M * 7 + K, (M, K), dt)
+    codes, scales = reference(exact)
+    nb = -(-K // 32)
+    c = torch.full((M, nb * 16), 0xA5, dtype=torch.uint8, device="cuda")
+    s = torch.full((M, nb), 0xA5, dtype=torch.uint8, device="cuda")
+    npas.mxfp4_quantize(_dev(torch, store, dt), c, s, M, K, dt)
+    np.testing.assert_array_equal(s.cpu().numpy(), scales)
+    np.testing.assert_array_equal(c.cpu().numpy(), codes)
+    y = torch.full((M * K + 1,), 7, dtype=_td(torch, dt), device="cuda")
+    npas.mxfp4_dequantize(c, s, y[:M * K].reshape(M, K), M, K, dt)
+    want = dtypes.quantize(values(codes, scales, K), dt)[1]
+    np.testing.assert_array_equal(_f64(y[:M * K].reshape(M, K), dt), want)
+    assert float(y[M * K]) == 7
+
+
+@gpu
+@pytest.mark.parametrize("dt", DT)
+def test_quantize_edges_of_the_type(torch, dt):
+    store, exact = edge_rows(dt)
+    codes, scales = reference(exact)
+    M, K = exact.shape
+    c, s = torch.empty((M, 32), dtype=torch.uint8, device="cuda"), torch.empty((M, 2), dtype=torch.uint8, device="cuda")
+    npas.mxfp4_quantize(_dev(torch, store, dt), c, s, M, K, dt)
+    np.testing.assert_array_equal(s.cpu().numpy(), scales)
+    number = np.repeat(scales != 255, 16, 1)
+    np.testing.assert_array_equal(c.cpu().numpy()[number], codes[number])
+    y = torch.empty((M, K), dtype=_td(torch, dt), device="cuda")
+    npas.mxfp4_dequantize(c, s, y, M, K, dt)
+    want, got = values(codes, scales, K), _f64(y, dt)
+    np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    np.testing.assert_array_equal(got[ok], want[ok])
+
+
+@gpu
+def test_quantize_rows_of_a_wider_tensor_at_odd_alignment(torch):
+    dt, M, K = npas.BF16, 9, 75
+    store, exact = sample(3, (M, 200), dt)
+    wide = _dev(torch, store, dt)
+    codes, scales = reference(exact[:, 101:101 + K])
+    c, s = torch.empty((M, 48), dtype=torch.uint8, device="cuda"), torch.empty((M, 3), dtype=torch.uint8, device="cuda")
+    npas.mxfp4_quantize(wide[:, 101:101 + K], c, s, M, K, dt)
+    np.testing.assert_array_equal(s.cpu().numpy(), scales)
+    np.testing.assert_array_equal(c.cpu().numpy(), codes)
+
+
+def _act(v, act):
+    if act == npas.ACT_RELU:
+        return np.maximum(v, 0)
+    if act == npas.ACT_RELU6:
+        return np.clip(v, 0, 6)
+    return v * np.clip(v + 3, 0, 6) / 6 if act == npas.ACT_HARDSWISH else v
+
+
+def _product(torch, seed, B, IN, OUT, dt, bias=True, act=npas.ACT_NONE, x=None):
+    xs, x64 = sample(seed, (B, IN), dt) if x is None else x
+    ws, w64 = sample(seed + 1, (OUT, IN), dt, "plain")
+    p = npas.pack_fc_mxfp4(ws, dt)
+    b = np.random.default_rng(seed).standard_normal(OUT).astype(np.float32) if bias else None
+    need = p.workspace_bytes(B)
+    work = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    outs = []
+    for again in range(2):
+        y = torch.full((B * OUT + 1,), 77, dtype=_td(torch, dt), device="cuda")
+        npas.fc_mxfp4(p, _dev(torch, xs, dt), y[:B * OUT].reshape(B, OUT), B, None if b is None else torch.from_numpy(b).cuda(), act,
+                      work, need)
+        assert float(y[B * OUT]) == 77
+        outs.append(y)
+    assert torch.equal(outs[0], outs[1]) or dt == npas.F32
+    xq, wq = values(*reference(x64), IN), values(*reference(w64), IN)
+    ref, mag = xq @ wq.T, np.abs(xq) @ np.abs(wq).T
+    if b is not None:
+        ref, mag = ref + b, mag + np.abs(b)
+    got = _f64(outs[0][:B * OUT].reshape(B, OUT), dt)
+    want = _act(ref, act)
+    grow = 3.0 if act == npas.ACT_HARDSWISH else 1.0           # the activation's slope is at most 1.5, its own three roundings
+    nan = np.isnan(want)
+    np.testing.assert_array_equal(np.isnan(got), nan)
+    bad = np.abs(got - want) > U[dt] * np.abs(want) + TINY[dt] + grow * (128 + IN / 128) * 2.0 ** -24 * mag
+    assert not bad[~nan].any(), f"{bad[~nan].sum()} of {bad.size} off, worst {np.abs(got - want)[~nan].max()}"
+
+
+FC = [(1, 1, 1), (1, 32, 64), (2, 33, 5), (3, 128, 65), (16, 127, 63), (17, 640, 130), (1, 4096, 512), (5, 1000, 333), (33, 1280, 1000),
+      (64, 513, 256), (100, 2050, 96), (200, 384, 700), (257, 1024, 513), (300, 100, 1030), (520, 4224, 264)]
+
+
+@gpu
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("B,IN,OUT", FC)
+def test_product(torch, dt, B, IN, OUT):
+    print(f"fc_mxfp4 B={B} IN={IN} OUT={OUT} dtype={dt}", flush=True)
+    _product(torch, B + IN + OUT, B, IN, OUT, dt, bias=OUT % 2 == 1)
+
+
+@gpu
+@pytest.mark.parametrize("act", [npas.ACT_RELU, npas.ACT_RELU6, npas.ACT_HARDSWISH])
+@pytest.mark.parametrize("B", [3, 150])
+def test_product_activations(torch, act, B):
+    _product(torch, 5, B, 300, 200, npas.BF16, act=act)
+
+
+@gpu
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("B", [12, 96])
+def test_product_of_rows_at_the_edges_of_the_type(torch, dt, B):
+    """Zeros, the smallest numbers, infinities and NaN: a block with one of the latter makes its row NaN and no other."""
+    store, exact = edge_rows(dt)
+    keep = [0, 2, 3, 4, 5, 6, 7, 8, 9, 11]                      # without the largest numbers, whose sums overflow
+    store, exact = np.tile(store[keep], (B // 10 + 1, 1))[:B], np.tile(exact[keep], (B // 10 + 1, 1))[:B]
+    _product(torch, 9, B, 64, 70, dt, x=(store, exact))
+
+
+@gpu
+def test_product_rows_of_a_wider_tensor_on_a_side_stream_and_in_a_graph(torch):
+    dt, B, IN, OUT = npas.BF16, 40, 200, 90
+    ws, w64 = sample(21, (OUT, IN), dt, "plain")
+    p = npas.pack_fc_mxfp4(ws, dt)
+    need = p.workspace_bytes(B)
+    work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    wide = torch.zeros((B, IN + 31), dtype=torch.int16, device="cuda")
+    y = torch.empty((B, OUT), dtype=torch.int16, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        npas.fc_mxfp4(p, wide[:, 31:], y, B, workspace=work, workspace_bytes=need, stream=side.cuda_stream)
+    wq = values(*reference(w64), IN)
+    for i in range(3):
+        xs, x64 = sample(30 + i, (B, IN + 31), dt)
+        wide.copy_(_dev(torch, xs, dt))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        xq = values(*reference(x64[:, 31:]), IN)
+        ref, mag = xq @ wq.T, np.abs(xq) @ np.abs(wq).T
+        replayed = y.clone()
+        assert (np.abs(_f64(y, dt) - ref) <= U[dt] * np.abs(ref) + TINY[dt] + 130 * 2.0 ** -24 * mag).all()
+        y.zero_()
+        torch.cuda.synchronize()
+        npas.fc_mxfp4(p, wide[:, 31:], y, B, workspace=work, workspace_bytes=need, stream=side.cuda_stream)
+        side.synchronize()
+        assert torch.equal(y, replayed)
