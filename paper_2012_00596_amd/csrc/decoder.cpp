@@ -36,6 +36,32 @@ int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
     return NPAS_OK;
 }
 
+// How a launch cuts the tokens: about kTarget workgroups in all where lengths reach max_length, at least kMinChunk tokens each.
+struct Cuts {
+    int chunk, splits;
+    size_t stat_at, bytes; // (maximum, sum) pairs lie behind the sums; bytes: for any window
+};
+constexpr long kTarget = 2048, kMinChunk = 256;
+Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
+{
+    const long room = (long)c.table_stride * c.page_size, longest = max_length < room ? max_length : room;
+    const long n = window > 0 && window < longest ? window : longest;
+    const long group = heads / c.kv_heads, pairs = (long)c.sequences * c.kv_heads * ((group + 15) / 16);
+    long chunk = (n * pairs + kTarget - 1) / kTarget;
+    if (chunk < kMinChunk) chunk = kMinChunk;
+    if (chunk < (n + kMaxSplits - 1) / kMaxSplits) chunk = (n + kMaxSplits - 1) / kMaxSplits;
+    chunk = (chunk + 127) / 128 * 128;
+    // cuts are at least kMinChunk tokens and a share 1 / (kTarget / pairs) of the tokens each
+    long most = (longest + kMinChunk - 1) / kMinChunk, share = (kTarget + pairs - 1) / pairs;
+    most = most < share ? most : share;
+    most = most < kMaxSplits ? most : kMaxSplits;
+    Cuts k{(int)chunk, (int)((n + chunk - 1) / chunk), 0, 0};
+    const size_t rows = (size_t)c.sequences * heads;
+    k.stat_at = rows * k.splits * c.head_dim * 4;
+    if (most > 1) k.bytes = rows * most * (c.head_dim * 4 + 8);
+    return k;
+}
+
 bool bad_stride(int64_t stride, int64_t row) { return stride < row || stride > (int64_t)1 << 40; }
 
 } // namespace
@@ -109,7 +135,7 @@ size_t npas_paged_attention_workspace_bytes(const npas_kv_cache *cache, int head
 {
     CacheArgs c;
     if (max_length <= 0 || check_cache(cache, heads, &c)) return 0;
-    return 0;
+    return plan_cuts(c, heads, max_length, 0).bytes;
 }
 
 int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t q_stride, void *y_dev, float *lse_dev, int heads,
@@ -131,13 +157,17 @@ int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t 
         set_error("a pointer is not aligned to its element type");
         return NPAS_E_SHAPE;
     }
-    const size_t need = npas_paged_attention_workspace_bytes(cache, heads, max_length);
+    const Cuts cuts = plan_cuts(a.c, heads, max_length, window);
+    const size_t need = cuts.bytes;
     if (need && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 16))) {
         set_error("paged attention needs %zu bytes of workspace at a multiple of 16, got %zu at %p", need, workspace_bytes, workspace_dev);
         return NPAS_E_WORKSPACE;
     }
     a.q = q_dev; a.y = y_dev; a.lse = lse_dev; a.q_stride = q_stride; a.length = length_dev;
     a.heads = heads; a.max_length = max_length; a.window = window; a.scale = scale;
+    a.chunk = cuts.chunk; a.splits = cuts.splits;
+    a.part = (float *)workspace_dev;
+    a.part_stat = (float2 *)((uint8_t *)workspace_dev + cuts.stat_at);
     return launch_paged_attention(cache->dtype, a, hip_stream);
 }
 

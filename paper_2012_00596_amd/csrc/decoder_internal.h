@@ -1,6 +1,8 @@
 // Kernel argument blocks and launchers of the decoder-block operators (norm with gate and residual, paged cache,
 // attention of one token).
 #pragma once
+#include <hip/hip_runtime.h>
+
 #include <cstddef>
 #include <cstdint>
 
@@ -43,7 +45,12 @@ struct AttentionArgs {
     const int32_t *length;
     int heads, max_length, window;
     float scale;
+    // cuts of `chunk` tokens; more than one: unnormalised sums [sequence][head][cut][head_dim] and (maximum, sum) of each
+    int chunk, splits;
+    float *part;
+    float2 *part_stat;
 };
+constexpr int kMaxSplits = 512;
 
 int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream);
 int launch_kv_append(int dt, const AppendArgs &a, void *stream);

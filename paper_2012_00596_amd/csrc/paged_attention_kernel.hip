@@ -1,4 +1,5 @@
-// Attention of one new token a sequence over the paged cache.
+// Attention of one new token a sequence over the paged cache: a split kernel that walks the tokens once with running maximum and
+// sum, and a joining kernel for sequences that were cut over several workgroups.
 #include <type_traits>
 
 #include "decoder_internal.h"
@@ -6,61 +7,297 @@
 
 namespace npas {
 
-// One workgroup a (sequence, head): four waves take the tokens in turn, a lane four elements of the head; running maximum and sum per
-// wave, joined at the end.
-template <int DT> __global__ __launch_bounds__(256) void paged_attention_kernel(AttentionArgs a)
+constexpr uint32_t kAbsent = 0xffffffffu;
+constexpr int kRows = 2048; // tokens whose cache rows are looked up at once
+
+// The tokens of sequence s that take part: [first, first + count).
+__device__ __forceinline__ void token_range(const AttentionArgs &a, int s, int &first, int &count)
 {
-    __shared__ float sm[4], sl[4], so[4][256];
-    const int s = blockIdx.x / a.heads, head = blockIdx.x - s * a.heads, kv = head / (a.heads / a.c.kv_heads), D = a.c.head_dim;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d0 = lane * 4;
     const long room = (long)a.c.table_stride * a.c.page_size;
     int n = max(0, min(a.length[s], a.max_length));
     if (n > room) n = (int)room;
-    const int first = a.window > 0 ? max(0, n - a.window) : 0;
-    float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
+    first = a.window > 0 ? max(0, n - a.window) : 0;
+    count = n - first;
+}
+
+// One workgroup a (sequence, key head, 16 of its query heads, cut): its four waves take tiles of 32 tokens in turn.
+// Both products run on 16 x 16 x 32 matrix instructions with the query heads as columns, so that a key or value is read once for all
+// heads of its group.  Scores: row operand = keys as they lie in the cache (lane 16 q + r: token r, 8 elements), result register i of
+// lane 16 q + n = token 4 q + i, head n.  The weights are the second product's column operand as they stand, if its 32 tokens are
+// counted so that quarter q holds tokens 4 q .. 4 q + 3 of both 16-token tiles; its row operand, values by element, comes from rows of
+// the cache read whole (lane 16 q + r: VW consecutive elements of those eight tokens) and turned round in registers, two elements an
+// instruction: row r of tile j is element VW r + j.  Nothing passes through LDS but the cache rows of the tokens.
+// The weights go in as two 16-bit numbers, high part and remainder: the matrix cores have time for both (the kernel waits for memory),
+// and the result is then as good as with 32-bit weights.
+template <int DT, int NC, bool FULL> __global__ __launch_bounds__(256, NC <= 4 ? 2 : 1) void paged_attention_kernel(AttentionArgs a)
+{
+    constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
+    constexpr int PITCH = DP + 4;
+    __shared__ __align__(16) uint32_t rows[kRows];
+    __shared__ float sm[4][16], sl[4][16];
+    __shared__ __align__(16) float so[4 * 16 * PITCH];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, D = FULL ? DP : a.c.head_dim;
+    const int group = a.heads / a.c.kv_heads, head_tiles = (group + 15) >> 4;
+    uint32_t id = blockIdx.x;
+    const int kv = id % a.c.kv_heads;
+    id /= a.c.kv_heads;
+    const int h0 = id % head_tiles * 16; // first of the group's heads here
+    id /= head_tiles;
+    const int split = id % a.splits, s = id / a.splits;
+    int first, count;
+    token_range(a, s, first, count);
+    const long from = (long)split * a.chunk;
+    if (from >= count && (split > 0 || a.splits > 1)) return;
+    const int t0 = first + (int)from, cnt = min(a.chunk, count - (int)from);
+    const bool real = h0 + r < group;
+    uint4 qf[NC];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) q[k] = d0 + k < D ? a.scale * ld_act<DT>(a.q, (size_t)s * a.q_stride + (size_t)head * D + d0 + k) : 0.f;
-    for (int j = first + wave; j < n; j += 4) {
-        const int column = j / a.c.page_size, page = a.c.table[(size_t)s * a.c.table_stride + column];
-        if ((uint32_t)page >= (uint32_t)a.c.pages) continue;
-        const size_t row = (((size_t)page * a.c.kv_heads + kv) * a.c.page_size + (j - column * a.c.page_size)) * D;
-        float x = 0.f;
-        if (d0 < D)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x = fmaf(q[k], ld_act<DT>(a.c.k, row + d0 + k), x);
-#pragma unroll
-        for (int w = 32; w; w >>= 1) x += __shfl_xor(x, w);
-        const float top = fmaxf(m, x), c = m == -INFINITY ? 0.f : expf(m - top), p = x == -INFINITY ? 0.f : expf(x - top);
-        l = l * c + p;
-        if (d0 < D)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o[k] = o[k] * c + p * ld_act<DT>(a.c.v, row + d0 + k);
-        m = top;
+    for (int c = 0; c < NC; ++c) {
+        const int d = 32 * c + 8 * q;
+        qf[c] = make_uint4(0, 0, 0, 0);
+        if (real && d < D) {
+            struct __attribute__((packed, aligned(2))) Words { uint32_t w[4]; };
+            const Words x = *reinterpret_cast<const Words *>(reinterpret_cast<const uint16_t *>(a.q) + (size_t)s * a.q_stride +
+                                                             (size_t)(kv * group + h0 + r) * D + d);
+            qf[c] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+        }
     }
-    if (lane == 0) {
-        sm[wave] = m;
-        sl[wave] = l;
+    const uint8_t *kb = reinterpret_cast<const uint8_t *>(a.c.k), *vb = reinterpret_cast<const uint8_t *>(a.c.v);
+    const uint32_t row_bytes = (uint32_t)D * 2;
+    const float to2 = a.scale * 1.4426950408889634f; // scores in powers of two
+    f32x4 o[VW] = {};
+    float m = -INFINITY, l = 0.f;
+
+    struct Tile {
+        uint4 k[2][NC];
+        uint32_t v[8][VP * VD];
+        uint32_t absent;
+    };
+    auto load = [&](int tile, Tile &t) {
+        const uint32_t *at = rows + tile * 32;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t row = at[16 * h + r];
+            const uint8_t *p = kb + (uint64_t)(row == kAbsent ? 0u : row) * row_bytes;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int d = 32 * c + 8 * q;
+                if (FULL || d < D) t.k[h][c] = *reinterpret_cast<const uint4 *>(p + 2 * d);
+                else t.k[h][c] = make_uint4(0, 0, 0, 0);
+            }
+        }
+        t.absent = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint4 four = *reinterpret_cast<const uint4 *>(at + 16 * h + 4 * q);
+            const uint32_t row[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool none = row[i] == kAbsent;
+                if (none) t.absent |= 1u << (4 * h + i);
+                const uint8_t *p = vb + (uint64_t)(none ? 0u : row[i]) * row_bytes;
+#pragma unroll
+                for (int e = 0; e < VP; ++e) {
+                    const int d = VW * r + 8 * e;
+                    const uint8_t *x = p + 2 * (FULL || d < D ? d : 0); // elements past the head: their results are not kept
+                    uint32_t *v = &t.v[4 * h + i][e * VD];
+                    if constexpr (VD == 4) {
+                        const uint4 w = *reinterpret_cast<const uint4 *>(x);
+                        v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+                    } else {
+                        const uint2 w = *reinterpret_cast<const uint2 *>(x);
+                        v[0] = w.x, v[1] = w.y;
+                    }
+                }
+            }
+        }
+    };
+    auto compute = [&](const Tile &t) {
+        f32x4 c0 = {}, c1 = {};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            c0 = mfma16<DT>(t.k[0][c], qf[c], c0);
+            c1 = mfma16<DT>(t.k[1][c], qf[c], c1);
+        }
+        float x[8], top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = t.absent >> i & 1 ? -INFINITY : (i < 4 ? c0[i] : c1[i - 4]) * to2;
+            top = fmaxf(top, x[i]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > m)) {
+            const float now = fmaxf(m, top), c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= c;
+#pragma unroll
+            for (int j = 0; j < VW; ++j) o[j] *= c;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p0 = __builtin_amdgcn_exp2f(x[2 * i] - base), p1 = __builtin_amdgcn_exp2f(x[2 * i + 1] - base);
+            l += p0 + p1;
+            hi[i] = pack2<DT>(p0, p1);
+            lo[i] = pack2<DT>(p0 - from_storage<DT>((uint16_t)hi[i]), p1 - from_storage<DT>((uint16_t)(hi[i] >> 16)));
+        }
+        const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        uint32_t keep[8]; // an absent token's row is another's: it must not bring in an infinity or a NaN
+#pragma unroll
+        for (int i = 0; i < 8; ++i) keep[i] = t.absent >> i & 1 ? 0u : 0xffffffffu;
+#pragma unroll
+        for (int w = 0; w < VW / 2; ++w) {
+            uint32_t v[8], even[4], odd[4];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = t.v[i][w] & keep[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                even[i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x05040100u);
+                odd[i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07060302u);
+            }
+            const uint4 ve = make_uint4(even[0], even[1], even[2], even[3]), vo = make_uint4(odd[0], odd[1], odd[2], odd[3]);
+            o[2 * w] = mfma16<DT>(ve, ph, o[2 * w]);
+            o[2 * w + 1] = mfma16<DT>(vo, ph, o[2 * w + 1]);
+            o[2 * w] = mfma16<DT>(ve, pl, o[2 * w]);
+            o[2 * w + 1] = mfma16<DT>(vo, pl, o[2 * w + 1]);
+        }
+    };
+
+    for (int base = 0; base < cnt; base += kRows) {
+        const int here = min(kRows, cnt - base), tiles = (here + 31) >> 5;
+        if (base) __syncthreads();
+        for (int i = threadIdx.x; i < tiles * 32; i += 256) {
+            uint32_t row = kAbsent;
+            if (i < here) {
+                const uint32_t j = (uint32_t)(t0 + base + i), column = j / (uint32_t)a.c.page_size;
+                const uint32_t page = (uint32_t)a.c.table[(size_t)s * a.c.table_stride + column];
+                if (page < (uint32_t)a.c.pages) row = (page * a.c.kv_heads + kv) * a.c.page_size + (j - column * a.c.page_size);
+            }
+            rows[i] = row;
+        }
+        __syncthreads();
+        if (wave < tiles) {
+            Tile now, next;
+            load(wave, now);
+            for (int tile = wave; tile < tiles; tile += 4) {
+                if (tile + 4 < tiles) load(tile + 4, next);
+                compute(now);
+                now = next;
+            }
+        }
+    }
+
+    // Join of the four waves: maxima, then rescaled sums, in the waves' order.
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (q == 0) {
+        sm[wave][r] = m;
+        sl[wave][r] = l;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) so[wave][d0 + k] = o[k];
+    for (int i = 0; i < 4; ++i) {
+        float *p = so + (wave * 16 + r) * PITCH + VW * (4 * q + i);
+#pragma unroll
+        for (int j = 0; j < VW; j += 4) *reinterpret_cast<float4 *>(p + j) = make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]);
+    }
     __syncthreads();
-    const int d = threadIdx.x;
-    const float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-    float sum = 0.f, y = 0.f;
-    for (int w = 0; w < 4; ++w) {
-        const float c = sm[w] == -INFINITY ? 0.f : expf(sm[w] - top);
-        sum += c * sl[w];
-        y += c * so[w][d];
+    for (int u = threadIdx.x; u < 16 * (DP / 4); u += 256) {
+        const int n = u / (DP / 4), d = (u - n * (DP / 4)) * 4;
+        if (h0 + n >= group || d >= D) continue;
+        const int head = kv * group + h0 + n;
+        const float top = fmaxf(fmaxf(sm[0][n], sm[1][n]), fmaxf(sm[2][n], sm[3][n]));
+        float sum = 0.f;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float c = sm[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][n] - top);
+            const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + n) * PITCH + d);
+            sum += c * sl[w][n];
+            y.x += c * v.x, y.y += c * v.y, y.z += c * v.z, y.w += c * v.w;
+        }
+        const size_t row = (size_t)s * a.heads + head;
+        if (a.splits > 1) {
+            *reinterpret_cast<float4 *>(a.part + (row * a.splits + split) * D + d) = y;
+            if (d == 0) a.part_stat[row * a.splits + split] = make_float2(top, sum);
+        } else {
+            const float inv = sum != 0.f ? 1.f / sum : 0.f;
+            uint16_t *out = reinterpret_cast<uint16_t *>(a.y) + row * D + d;
+            const float v[4] = {y.x * inv, y.y * inv, y.z * inv, y.w * inv};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) out[k] = to_storage<DT>(v[k]);
+            if (d == 0 && a.lse) a.lse[row] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        }
     }
-    if (d < D) st_act<DT>(a.y, ((size_t)s * a.heads + head) * D + d, sum != 0.f ? y / sum : 0.f);
-    if (d == 0 && a.lse) a.lse[(size_t)s * a.heads + head] = sum != 0.f ? top + logf(sum) : -INFINITY;
+}
+
+// One workgroup a (sequence, head): the cuts' sums, rescaled to the largest maximum and added, four at a time side by side.
+template <int DT> __global__ __launch_bounds__(256) void paged_attention_join_kernel(AttentionArgs a)
+{
+    __shared__ float weight[kMaxSplits], part[4], total[4];
+    __shared__ __align__(16) float so[4][256];
+    const int s = blockIdx.x / a.heads, D = a.c.head_dim, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d = lane * 4;
+    const size_t row = blockIdx.x;
+    int first, count;
+    token_range(a, s, first, count);
+    const int cuts = (count + a.chunk - 1) / a.chunk;
+    const float2 *stat = a.part_stat + row * a.splits;
+    float m = -INFINITY;
+    for (int i = threadIdx.x; i < cuts; i += 256) m = fmaxf(m, stat[i].x);
+#pragma unroll
+    for (int w = 32; w; w >>= 1) m = fmaxf(m, __shfl_xor(m, w));
+    if (lane == 0) part[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    float l = 0.f;
+    for (int i = threadIdx.x; i < cuts; i += 256) {
+        const float2 x = stat[i];
+        const float c = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
+        weight[i] = c;
+        l += c * x.y;
+    }
+#pragma unroll
+    for (int w = 32; w; w >>= 1) l += __shfl_xor(l, w);
+    if (lane == 0) total[wave] = l;
+    __syncthreads();
+    l = total[0] + total[1] + total[2] + total[3];
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (d < D)
+        for (int i = wave; i < cuts; i += 4) {
+            const float c = weight[i];
+            const float4 v = *reinterpret_cast<const float4 *>(a.part + (row * a.splits + i) * D + d);
+            y.x += c * v.x, y.y += c * v.y, y.z += c * v.z, y.w += c * v.w;
+        }
+    *reinterpret_cast<float4 *>(&so[wave][d]) = y;
+    __syncthreads();
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    if ((int)threadIdx.x < D)
+        reinterpret_cast<uint16_t *>(a.y)[row * D + threadIdx.x] =
+            to_storage<DT>((so[0][threadIdx.x] + so[1][threadIdx.x] + so[2][threadIdx.x] + so[3][threadIdx.x]) * inv);
+    if (threadIdx.x == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 int launch_paged_attention(int dt, const AttentionArgs &a, void *stream)
 {
-    const dim3 grid((unsigned)(a.c.sequences * a.heads)), block(256);
-    if (dt == NPAS_BF16) hipLaunchKernelGGL((paged_attention_kernel<NPAS_BF16>), grid, block, 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL((paged_attention_kernel<NPAS_F16>), grid, block, 0, (hipStream_t)stream, a);
+    hipStream_t st = (hipStream_t)stream;
+    const int group = a.heads / a.c.kv_heads;
+    const dim3 grid((unsigned)((size_t)a.c.sequences * a.splits * ((group + 15) / 16) * a.c.kv_heads));
+    auto pick = [&](auto dtc) {
+        constexpr int DT = decltype(dtc)::value;
+        auto run = [&](auto ncc) {
+            constexpr int NC = decltype(ncc)::value;
+            if (a.c.head_dim == 32 * NC) hipLaunchKernelGGL((paged_attention_kernel<DT, NC, true>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((paged_attention_kernel<DT, NC, false>), grid, dim3(256), 0, st, a);
+        };
+        if (a.c.head_dim <= 64) run(std::integral_constant<int, 2>{});
+        else if (a.c.head_dim <= 128) run(std::integral_constant<int, 4>{});
+        else run(std::integral_constant<int, 8>{});
+        if (a.splits > 1)
+            hipLaunchKernelGGL((paged_attention_join_kernel<DT>), dim3((unsigned)(a.c.sequences * a.heads)), dim3(256), 0, st, a);
+    };
+    if (dt == NPAS_BF16) pick(std::integral_constant<int, NPAS_BF16>{});
+    else pick(std::integral_constant<int, NPAS_F16>{});
     return launched("paged attention");
 }
 
