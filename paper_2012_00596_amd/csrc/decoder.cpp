@@ -36,26 +36,38 @@ int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
     return NPAS_OK;
 }
 
-// How a launch cuts the tokens: about kTarget workgroups in all where lengths reach max_length, at least kMinChunk tokens each.
+// How a launch cuts the tokens.  A pair is a sequence's key head (with up to 16 of its query heads): one workgroup a pair and cut.
+//   - Up to 128 tokens a wave (1024 where eight waves are used, 512 otherwise) one cut: the joining launch costs more (3.7 us on the device
+//     and 2.4 to issue) than the few rounds it would save: 16 pairs of 777 tokens 8.8 us in one cut, 9.6 in four.
+//   - Eight waves where every workgroup has a compute unit to itself anyway (that case: 8.8 us, with four waves 9.4); with more workgroups
+//     four, two of them on a compute unit (512 pairs of up to 8192 tokens: 227 us, with eight 244).
+//   - Longer ones in 512 workgroups (the two on each compute unit: 131071 tokens of 4 pairs 55 us, in 2048 workgroups 64, most of it the
+//     join), at least 256 tokens each; and at most 4096 tokens, so that a long sequence in a ragged batch does not run alone at the end.
 struct Cuts {
-    int chunk, splits;
-    size_t stat_at, bytes; // (maximum, sum) pairs lie behind the sums; bytes: for any window
+    int chunk, splits, waves;
+    size_t stat_at, bytes; // (maximum, sum) pairs lie behind the sums; bytes: enough for any window
 };
-constexpr long kTarget = 2048, kMinChunk = 256;
 Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
 {
+    constexpr long kWorkgroups = 512, kLeast = 256, kMost = 4096;
     const long room = (long)c.table_stride * c.page_size, longest = max_length < room ? max_length : room;
     const long n = window > 0 && window < longest ? window : longest;
     const long group = heads / c.kv_heads, pairs = (long)c.sequences * c.kv_heads * ((group + 15) / 16);
-    long chunk = (n * pairs + kTarget - 1) / kTarget;
-    if (chunk < kMinChunk) chunk = kMinChunk;
+    Cuts k{};
+    k.waves = c.head_dim <= 128 && pairs <= 256 && n <= 1024 ? 8 : 4;
+    long chunk = (n * pairs + kWorkgroups - 1) / kWorkgroups;
+    if (chunk > kMost) chunk = kMost;
+    if (chunk < kLeast) chunk = kLeast;
     if (chunk < (n + kMaxSplits - 1) / kMaxSplits) chunk = (n + kMaxSplits - 1) / kMaxSplits;
+    if (n <= 128 * k.waves) chunk = n;
     chunk = (chunk + 127) / 128 * 128;
-    // cuts are at least kMinChunk tokens and a share 1 / (kTarget / pairs) of the tokens each
-    long most = (longest + kMinChunk - 1) / kMinChunk, share = (kTarget + pairs - 1) / pairs;
-    most = most < share ? most : share;
-    most = most < kMaxSplits ? most : kMaxSplits;
-    Cuts k{(int)chunk, (int)((n + chunk - 1) / chunk), 0, 0};
+    k.chunk = (int)chunk;
+    k.splits = (int)((n + chunk - 1) / chunk);
+    // the most cuts that any window can lead to: each has kLeast tokens, and kMost or the pair's share of the workgroups
+    const long share = (kWorkgroups + pairs - 1) / pairs, capped = (longest + kMost - 1) / kMost;
+    long most = (longest + kLeast - 1) / kLeast;
+    if (most > (share > capped ? share : capped)) most = share > capped ? share : capped;
+    if (most > kMaxSplits) most = kMaxSplits;
     const size_t rows = (size_t)c.sequences * heads;
     k.stat_at = rows * k.splits * c.head_dim * 4;
     if (most > 1) k.bytes = rows * most * (c.head_dim * 4 + 8);
@@ -165,7 +177,7 @@ int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t 
     }
     a.q = q_dev; a.y = y_dev; a.lse = lse_dev; a.q_stride = q_stride; a.length = length_dev;
     a.heads = heads; a.max_length = max_length; a.window = window; a.scale = scale;
-    a.chunk = cuts.chunk; a.splits = cuts.splits;
+    a.chunk = cuts.chunk; a.splits = cuts.splits; a.waves = cuts.waves;
     a.part = (float *)workspace_dev;
     a.part_stat = (float2 *)((uint8_t *)workspace_dev + cuts.stat_at);
     return launch_paged_attention(cache->dtype, a, hip_stream);

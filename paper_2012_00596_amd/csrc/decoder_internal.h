@@ -46,7 +46,7 @@ struct AttentionArgs {
     int heads, max_length, window;
     float scale;
     // cuts of `chunk` tokens; more than one: unnormalised sums [sequence][head][cut][head_dim] and (maximum, sum) of each
-    int chunk, splits;
+    int chunk, splits, waves; // waves of a workgroup, 4 or 8
     float *part;
     float2 *part_stat;
 };

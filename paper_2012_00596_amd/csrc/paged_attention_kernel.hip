@@ -29,13 +29,13 @@ __device__ __forceinline__ void token_range(const AttentionArgs &a, int s, int &
 // instruction: row r of tile j is element VW r + j.  Nothing passes through LDS but the cache rows of the tokens.
 // The weights go in as two 16-bit numbers, high part and remainder: the matrix cores have time for both (the kernel waits for memory),
 // and the result is then as good as with 32-bit weights.
-template <int DT, int NC, bool FULL> __global__ __launch_bounds__(256, NC <= 4 ? 2 : 1) void paged_attention_kernel(AttentionArgs a)
+template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * NW, NW == 8 || NC <= 4 ? 2 : 1) void paged_attention_kernel(AttentionArgs a)
 {
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
     constexpr int PITCH = DP + 4;
     __shared__ __align__(16) uint32_t rows[kRows];
-    __shared__ float sm[4][16], sl[4][16];
-    __shared__ __align__(16) float so[4 * 16 * PITCH];
+    __shared__ float sm[NW][16], sl[NW][16];
+    __shared__ __align__(16) float so[NW * 16 * PITCH];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, D = FULL ? DP : a.c.head_dim;
     const int group = a.heads / a.c.kv_heads, head_tiles = (group + 15) >> 4;
     uint32_t id = blockIdx.x;
@@ -168,7 +168,7 @@ template <int DT, int NC, bool FULL> __global__ __launch_bounds__(256, NC <= 4 ?
     for (int base = 0; base < cnt; base += kRows) {
         const int here = min(kRows, cnt - base), tiles = (here + 31) >> 5;
         if (base) __syncthreads();
-        for (int i = threadIdx.x; i < tiles * 32; i += 256) {
+        for (int i = threadIdx.x; i < tiles * 32; i += 64 * NW) {
             uint32_t row = kAbsent;
             if (i < here) {
                 const uint32_t j = (uint32_t)(t0 + base + i), column = j / (uint32_t)a.c.page_size;
@@ -181,8 +181,8 @@ template <int DT, int NC, bool FULL> __global__ __launch_bounds__(256, NC <= 4 ?
         if (wave < tiles) {
             Tile now, next;
             load(wave, now);
-            for (int tile = wave; tile < tiles; tile += 4) {
-                if (tile + 4 < tiles) load(tile + 4, next);
+            for (int tile = wave; tile < tiles; tile += NW) {
+                if (tile + NW < tiles) load(tile + NW, next);
                 compute(now);
                 now = next;
             }
@@ -203,15 +203,16 @@ template <int DT, int NC, bool FULL> __global__ __launch_bounds__(256, NC <= 4 ?
         for (int j = 0; j < VW; j += 4) *reinterpret_cast<float4 *>(p + j) = make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]);
     }
     __syncthreads();
-    for (int u = threadIdx.x; u < 16 * (DP / 4); u += 256) {
+    for (int u = threadIdx.x; u < 16 * (DP / 4); u += 64 * NW) {
         const int n = u / (DP / 4), d = (u - n * (DP / 4)) * 4;
         if (h0 + n >= group || d >= D) continue;
         const int head = kv * group + h0 + n;
-        const float top = fmaxf(fmaxf(sm[0][n], sm[1][n]), fmaxf(sm[2][n], sm[3][n]));
-        float sum = 0.f;
+        float top = sm[0][n], sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) top = fmaxf(top, sm[w][n]);
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float c = sm[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][n] - top);
             const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + n) * PITCH + d);
             sum += c * sl[w][n];
@@ -232,50 +233,53 @@ template <int DT, int NC, bool FULL> __global__ __launch_bounds__(256, NC <= 4 ?
     }
 }
 
-// One workgroup a (sequence, head): the cuts' sums, rescaled to the largest maximum and added, four at a time side by side.
-template <int DT> __global__ __launch_bounds__(256) void paged_attention_join_kernel(AttentionArgs a)
+// One workgroup a (sequence, head): the cuts' sums, rescaled to the largest maximum and added; LANES lanes hold a cut's row, four elements
+// each, so that 512 / LANES cuts are read side by side.
+template <int DT, int LANES> __global__ __launch_bounds__(512) void paged_attention_join_kernel(AttentionArgs a)
 {
-    __shared__ float weight[kMaxSplits], part[4], total[4];
-    __shared__ __align__(16) float so[4][256];
-    const int s = blockIdx.x / a.heads, D = a.c.head_dim, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d = lane * 4;
+    constexpr int SIDE = 512 / LANES;
+    __shared__ float weight[kMaxSplits], part[8], total[8];
+    __shared__ __align__(16) float so[SIDE][LANES * 4];
+    const int s = blockIdx.x / a.heads, D = a.c.head_dim, tid = threadIdx.x, side = tid / LANES, d = tid % LANES * 4;
     const size_t row = blockIdx.x;
     int first, count;
     token_range(a, s, first, count);
     const int cuts = (count + a.chunk - 1) / a.chunk;
-    const float2 *stat = a.part_stat + row * a.splits;
-    float m = -INFINITY;
-    for (int i = threadIdx.x; i < cuts; i += 256) m = fmaxf(m, stat[i].x);
+    const float2 x = tid < cuts ? a.part_stat[row * a.splits + tid] : make_float2(-INFINITY, 0.f); // at most kMaxSplits = 512
+    float m = x.x;
 #pragma unroll
     for (int w = 32; w; w >>= 1) m = fmaxf(m, __shfl_xor(m, w));
-    if (lane == 0) part[wave] = m;
+    if ((tid & 63) == 0) part[tid >> 6] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    float l = 0.f;
-    for (int i = threadIdx.x; i < cuts; i += 256) {
-        const float2 x = stat[i];
-        const float c = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
-        weight[i] = c;
-        l += c * x.y;
-    }
+#pragma unroll
+    for (int w = 0; w < 8; ++w) m = fmaxf(m, part[w]);
+    const float c = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
+    float l = c * x.y;
+    weight[tid] = c;
 #pragma unroll
     for (int w = 32; w; w >>= 1) l += __shfl_xor(l, w);
-    if (lane == 0) total[wave] = l;
+    if ((tid & 63) == 0) total[tid >> 6] = l;
     __syncthreads();
-    l = total[0] + total[1] + total[2] + total[3];
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) l += total[w];
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     if (d < D)
-        for (int i = wave; i < cuts; i += 4) {
-            const float c = weight[i];
+#pragma unroll 4
+        for (int i = side; i < cuts; i += SIDE) {
+            const float k = weight[i];
             const float4 v = *reinterpret_cast<const float4 *>(a.part + (row * a.splits + i) * D + d);
-            y.x += c * v.x, y.y += c * v.y, y.z += c * v.z, y.w += c * v.w;
+            y.x += k * v.x, y.y += k * v.y, y.z += k * v.z, y.w += k * v.w;
         }
-    *reinterpret_cast<float4 *>(&so[wave][d]) = y;
+    *reinterpret_cast<float4 *>(&so[side][d]) = y;
     __syncthreads();
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-    if ((int)threadIdx.x < D)
-        reinterpret_cast<uint16_t *>(a.y)[row * D + threadIdx.x] =
-            to_storage<DT>((so[0][threadIdx.x] + so[1][threadIdx.x] + so[2][threadIdx.x] + so[3][threadIdx.x]) * inv);
-    if (threadIdx.x == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (tid < D) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i) sum += so[i][tid];
+        reinterpret_cast<uint16_t *>(a.y)[row * D + tid] = to_storage<DT>(l != 0.f ? sum / l : 0.f);
+    }
+    if (tid == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 int launch_paged_attention(int dt, const AttentionArgs &a, void *stream)
@@ -287,14 +291,23 @@ int launch_paged_attention(int dt, const AttentionArgs &a, void *stream)
         constexpr int DT = decltype(dtc)::value;
         auto run = [&](auto ncc) {
             constexpr int NC = decltype(ncc)::value;
-            if (a.c.head_dim == 32 * NC) hipLaunchKernelGGL((paged_attention_kernel<DT, NC, true>), grid, dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((paged_attention_kernel<DT, NC, false>), grid, dim3(256), 0, st, a);
+            auto form = [&](auto nwc) {
+                constexpr int NW = decltype(nwc)::value;
+                if (a.c.head_dim == 32 * NC) hipLaunchKernelGGL((paged_attention_kernel<DT, NC, true, NW>), grid, dim3(64 * NW), 0, st, a);
+                else hipLaunchKernelGGL((paged_attention_kernel<DT, NC, false, NW>), grid, dim3(64 * NW), 0, st, a);
+            };
+            if constexpr (NC <= 4) {
+                if (a.waves == 8) return form(std::integral_constant<int, 8>{});
+            }
+            form(std::integral_constant<int, 4>{});
         };
         if (a.c.head_dim <= 64) run(std::integral_constant<int, 2>{});
         else if (a.c.head_dim <= 128) run(std::integral_constant<int, 4>{});
         else run(std::integral_constant<int, 8>{});
-        if (a.splits > 1)
-            hipLaunchKernelGGL((paged_attention_join_kernel<DT>), dim3((unsigned)(a.c.sequences * a.heads)), dim3(256), 0, st, a);
+        const dim3 rows((unsigned)(a.c.sequences * a.heads));
+        if (a.splits > 1 && a.c.head_dim <= 64) hipLaunchKernelGGL((paged_attention_join_kernel<DT, 16>), rows, dim3(512), 0, st, a);
+        else if (a.splits > 1 && a.c.head_dim <= 128) hipLaunchKernelGGL((paged_attention_join_kernel<DT, 32>), rows, dim3(512), 0, st, a);
+        else if (a.splits > 1) hipLaunchKernelGGL((paged_attention_join_kernel<DT, 64>), rows, dim3(512), 0, st, a);
     };
     if (dt == NPAS_BF16) pick(std::integral_constant<int, NPAS_BF16>{});
     else pick(std::integral_constant<int, NPAS_F16>{});
