@@ -166,7 +166,8 @@ def _load_calls():
         spec = importlib.util.spec_from_file_location(__package__ + "._pycalls", _CALLS)
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
-        mod.init(NpasError, C.c_void_p, _conv2d_sparse, _fc_sparse, _depthwise3x3, _run_stack)
+        mod.init(NpasError, C.c_void_p, _conv2d_sparse, _fc_sparse, _depthwise3x3, _run_stack, _gated_residual_norm, _kv_append,
+                 _paged_attention, _mxfp4_quantize, _mxfp4_dequantize, _fc_mxfp4)
         _calls = mod
     return _calls
 
@@ -421,10 +422,7 @@ class KvCache:
         self.handle = C.c_void_p(C.addressof(self.desc))
 
 
-def gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate=None, post_weight=None, pre_weight=None, residual_scale=1.0, eps=1e-6,
-                        stream=None):
-    """Norm of a block's output, its gate, the scaled residual and the norm before the next block (npas_gated_residual_norm).  gate: one
-    row [D] or [1][D] for all tokens, or a row a token [T][D] (its rows may be a slice's)."""
+def _gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate, post_weight, pre_weight, residual_scale, eps, stream):
     g, gs = None, 0
     if gate is not None and not isinstance(gate, int):
         if gate.dim() == 1 or gate.shape[0] == 1:
@@ -439,19 +437,30 @@ def gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate=None, post_we
                                           _dev(h_out), _dev(n_out), T, D, dtype, stream))
 
 
-def kv_append(cache, q, k, v, q_out, T, heads, positions, sequences=None, cos_sin=None, rot_dim=0, kind=ROTATE_HALVES, stream=None):
-    """Rotates queries and keys and writes keys and values into the paged cache (npas_kv_append).  q, k, v: rows of T tokens, slices of a
-    joined projection allowed; positions, sequences int32 [T]; cos_sin fp32 [positions][rot_dim]."""
+def gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate=None, post_weight=None, pre_weight=None, residual_scale=1.0, eps=1e-6,
+                        stream=None):
+    """Norm of a block's output, its gate, the scaled residual and the norm before the next block (npas_gated_residual_norm).  gate: one
+    row [D] or [1][D] for all tokens, or a row a token [T][D] (its rows may be a slice's)."""
+    (_calls or _load_calls()).gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate, post_weight, pre_weight, residual_scale, eps,
+                                                  stream)
+
+
+def _kv_append(cache, q, k, v, q_out, T, heads, positions, sequences, cos_sin, rot_dim, kind, stream):
     D = cache.head_dim
     qp, qs = _rows(q, heads * D)
     kp, ks = _rows(k, cache.kv_heads * D)
     vp, vs = _rows(v, cache.kv_heads * D)
-    count = 0
-    if cos_sin is not None and rot_dim:
-        count = cos_sin.shape[0]
-        assert cos_sin.shape[1] == rot_dim, "cos_sin is [positions][rot_dim]"
-    _check(lib().npas_kv_append(cache.desc, qp, qs, kp, ks, vp, vs, _dev(q_out), T, heads, _dev(sequences), _dev(positions),
-                                _dev(cos_sin), count, rot_dim, kind, stream))
+    cp, cstride = _rows(cos_sin, rot_dim)
+    assert cstride == rot_dim, "cos_sin is not contiguous"
+    count = -1 if cos_sin is None or isinstance(cos_sin, int) else cos_sin.shape[0]
+    _check(lib().npas_kv_append(cache.desc, qp, qs, kp, ks, vp, vs, _dev(q_out), T, heads, _dev(sequences), _dev(positions), cp, count,
+                                rot_dim, kind, stream))
+
+
+def kv_append(cache, q, k, v, q_out, T, heads, positions, sequences=None, cos_sin=None, rot_dim=0, kind=ROTATE_HALVES, stream=None):
+    """Rotates queries and keys and writes keys and values into the paged cache (npas_kv_append).  q, k, v: rows of T tokens, slices of a
+    joined projection allowed; positions, sequences int32 [T]; cos_sin a tensor, fp32 [positions][rot_dim]."""
+    (_calls or _load_calls()).kv_append(cache, q, k, v, q_out, T, heads, positions, sequences, cos_sin, rot_dim, kind, stream)
 
 
 def paged_attention_workspace_bytes(cache, heads, max_length):
@@ -460,6 +469,10 @@ def paged_attention_workspace_bytes(cache, heads, max_length):
 
 def paged_attention(cache, q, y, heads, lengths, max_length, scale, window=0, lse=None, workspace=None, workspace_bytes=0, stream=None):
     """Attention of one new token a sequence over the paged cache (npas_paged_attention); lengths int32 [sequences]."""
+    (_calls or _load_calls()).paged_attention(cache, q, y, heads, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream)
+
+
+def _paged_attention(cache, q, y, heads, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream):
     qp, qs = _rows(q, heads * cache.head_dim)
     _check(lib().npas_paged_attention(cache.desc, qp, qs, _dev(y), _dev(lse), heads, _dev(lengths), max_length, window, scale,
                                       _dev(workspace), workspace_bytes, stream))
@@ -469,12 +482,20 @@ def paged_attention(cache, q, y, heads, lengths, max_length, scale, window=0, ls
 
 def mxfp4_quantize(x, codes, scales, M, K, dtype, stream=None):
     """Rows x [M][K] (they may be a slice's) to codes uint8 [M][16 ceil(K / 32)] and scale bytes uint8 [M][ceil(K / 32)]."""
+    (_calls or _load_calls()).mxfp4_quantize(x, codes, scales, M, K, dtype, stream)
+
+
+def _mxfp4_quantize(x, codes, scales, M, K, dtype, stream):
     xp, xs = _rows(x, K)
     _check(lib().npas_mxfp4_quantize(xp, xs, _dev(codes), _dev(scales), M, K, dtype, stream))
 
 
 def mxfp4_dequantize(codes, scales, y, M, K, dtype, stream=None):
     """The values that codes and scales stand for, y [M][K]."""
+    (_calls or _load_calls()).mxfp4_dequantize(codes, scales, y, M, K, dtype, stream)
+
+
+def _mxfp4_dequantize(codes, scales, y, M, K, dtype, stream):
     _check(lib().npas_mxfp4_dequantize(_dev(codes), _dev(scales), _dev(y), M, K, dtype, stream))
 
 
@@ -518,5 +539,9 @@ def pack_fc_mxfp4(w, dtype, stream=None):
 
 def fc_mxfp4(packed, x, y, B, bias=None, act=ACT_NONE, workspace=None, workspace_bytes=0, stream=None):
     """y [B][OUT] = act(bias + x W^T) with both factors in microscaled 4-bit floats; x [B][IN] (its rows may be a slice's)."""
-    xp, xs = _rows(x, packed.IN)
+    (_calls or _load_calls()).fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, packed.IN)
+
+
+def _fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, IN):
+    xp, xs = _rows(x, IN)
     _check(lib().npas_fc_mxfp4(packed.handle, xp, xs, _dev(y), B, _dev(bias), act, _dev(workspace), workspace_bytes, stream))

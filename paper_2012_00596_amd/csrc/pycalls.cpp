@@ -10,7 +10,7 @@ namespace {
 
 PyObject *error_class; // NpasError(code, message), set by init()
 PyObject *c_void_p;    // ctypes.c_void_p, set by init()
-PyObject *s_handle, *s_value, *s_is_contiguous, *s_data_ptr;
+PyObject *s_handle, *s_value, *s_is_contiguous, *s_data_ptr, *s_shape, *s_stride;
 
 // The arguments of one call, converted in their order.  Once one does not convert, the later conversions do nothing.
 struct Args {
@@ -74,6 +74,61 @@ struct Args {
         return (size_t)(uintptr_t)number(PyLong_AsUnsignedLongLongMask(a[i]));
     }
 
+    float real(int i)
+    {
+        if (state != PLAIN) return 0.f;
+        if (!PyFloat_Check(a[i]) && !PyLong_Check(a[i])) {
+            other();
+            return 0.f;
+        }
+        const double v = PyFloat_AsDouble(a[i]);
+        if (v == -1.0 && PyErr_Occurred()) fail();
+        return (float)v;
+    }
+
+    // Rows of `width` elements: a tensor whose rows are contiguous, or the address of contiguous rows.  count: rows of a tensor, -1 of an address.
+    struct Rows {
+        void *p;
+        int64_t stride, count;
+    };
+    Rows rows(int i, int64_t width)
+    {
+        PyObject *o = a[i];
+        if (state != PLAIN || o == Py_None) return Rows{nullptr, width, -1};
+        if (PyLong_Check(o)) return Rows{number(PyLong_AsUnsignedLongLongMask(o)), width, -1};
+        Rows r{nullptr, width, 0};
+        PyObject *shape = PyObject_GetAttr(o, s_shape), *stride = shape ? PyObject_CallMethodNoArgs(o, s_stride) : nullptr;
+        if (!stride) fail();
+        else if (!PyTuple_Check(shape) || !PyTuple_Check(stride) || PyTuple_GET_SIZE(shape) != PyTuple_GET_SIZE(stride) || !PyTuple_GET_SIZE(shape)) other();
+        else {
+            int64_t inner = 1;
+            for (Py_ssize_t d = PyTuple_GET_SIZE(shape) - 1; d > 0 && state == PLAIN; --d) {
+                const int64_t n = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, d)), by = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, d));
+                if (n != 1 && by != inner) refuse("rows are not contiguous");
+                inner *= n;
+            }
+            if (state == PLAIN && inner != width) refuse("rows of another length than the call's");
+            r.count = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0));
+            if (r.count > 1) r.stride = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, 0));
+            if (state == PLAIN && PyErr_Occurred()) fail();
+        }
+        Py_XDECREF(shape);
+        Py_XDECREF(stride);
+        PyObject *p = state == PLAIN ? PyObject_CallMethodNoArgs(o, s_data_ptr) : nullptr;
+        if (state == PLAIN) {
+            if (!p) fail();
+            else if (PyLong_Check(p)) r.p = number(PyLong_AsUnsignedLongLongMask(p));
+            else other();
+        }
+        Py_XDECREF(p);
+        return r;
+    }
+    void refuse(const char *why)
+    {
+        PyErr_SetString(PyExc_AssertionError, why);
+        fail();
+    }
+
 private:
     void *fail()
     {
@@ -101,7 +156,7 @@ PyObject *result(int rc)
 
 // What follows the conversions: the library call without the interpreter lock, or, where an argument is of another kind, the
 // same call through ctypes (which accepts or refuses it).
-enum Call { CONV2D, FC, DEPTHWISE, STACK, CALLS };
+enum Call { CONV2D, FC, DEPTHWISE, STACK, NORM, APPEND, ATTENTION, QUANTIZE, DEQUANTIZE, FC_MXFP4, CALLS };
 PyObject *by_ctypes[CALLS]; // set by init()
 
 template <typename F> PyObject *finish(const Args &g, Call which, Py_ssize_t n, F call)
@@ -178,7 +233,117 @@ PyObject *run_stack(PyObject *, PyObject *const *a, Py_ssize_t n)
     return finish(g, STACK, n, [&] { return npas_run_stack(s, x, y, N, w, bytes, st); });
 }
 
-// init(NpasError, c_void_p, conv2d_sparse, fc_sparse, depthwise3x3, run_stack): the last four are the calls through ctypes
+// gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate, post_weight, pre_weight, residual_scale, eps, stream)
+PyObject *gated_residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 13)) return nullptr;
+    Args g{a};
+    void *branch = g.pointer(0), *h = g.pointer(1), *ho = g.pointer(2), *no = g.pointer(3);
+    const int T = g.integer(4), D = g.integer(5), dt = g.integer(6);
+    // one row [D] or [1][D] for all tokens, or a row a token
+    int64_t stride = 0;
+    void *gate = nullptr;
+    if (g.state == Args::PLAIN && a[7] != Py_None) {
+        PyObject *shape = PyLong_Check(a[7]) ? nullptr : PyObject_GetAttr(a[7], s_shape);
+        const bool flat = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 1;
+        const int64_t row = flat ? PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) : 0;
+        Py_XDECREF(shape);
+        if (PyErr_Occurred()) return nullptr;
+        if (flat) {
+            gate = g.pointer(7);
+            if (g.state == Args::PLAIN && row != D) g.refuse("gate is [D], [1][D] or [T][D]");
+        } else {
+            const Args::Rows r = g.rows(7, D);
+            gate = r.p;
+            stride = r.count == 1 ? 0 : r.stride;
+            if (g.state == Args::PLAIN && r.count >= 0 && r.count != 1 && r.count != T) g.refuse("gate is [D], [1][D] or [T][D]");
+        }
+    }
+    void *post = g.pointer(8), *pre = g.pointer(9);
+    const float scale = g.real(10), eps = g.real(11);
+    void *st = g.address(12);
+    return finish(g, NORM, n, [&] {
+        return npas_gated_residual_norm(branch, h, gate, stride, (const float *)post, (const float *)pre, scale, eps, ho, no, T, D, (npas_dtype)dt, st);
+    });
+}
+
+// kv_append(cache, q, k, v, q_out, T, heads, positions, sequences, cos_sin, rot_dim, kind, stream)
+PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 13)) return nullptr;
+    Args g{a};
+    const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
+    const int T = g.integer(5), heads = g.integer(6), rot = g.integer(10), kind = g.integer(11);
+    const int64_t D = c ? c->head_dim : 0, kv = c ? c->kv_heads : 0;
+    const Args::Rows q = g.rows(1, heads * D), k = g.rows(2, kv * D), v = g.rows(3, kv * D);
+    void *qo = g.pointer(4), *pos = g.pointer(7), *seq = g.pointer(8);
+    const Args::Rows cs = g.rows(9, rot);
+    if (g.state == Args::PLAIN && cs.stride != rot) g.refuse("cos_sin is not contiguous");
+    void *st = g.address(12);
+    return finish(g, APPEND, n, [&] {
+        return npas_kv_append(c, q.p, q.stride, k.p, k.stride, v.p, v.stride, qo, T, heads, (const int32_t *)seq, (const int32_t *)pos,
+                              (const float *)cs.p, (int)(cs.count > 0x7fffffff ? 0x7fffffff : cs.count), rot, (npas_rotation)kind, st);
+    });
+}
+
+// paged_attention(cache, q, y, heads, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 12)) return nullptr;
+    Args g{a};
+    const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
+    const int heads = g.integer(3), most = g.integer(5), window = g.integer(7);
+    const Args::Rows q = g.rows(1, (int64_t)heads * (c ? c->head_dim : 0));
+    void *y = g.pointer(2), *len = g.pointer(4);
+    const float scale = g.real(6);
+    void *lse = g.pointer(8), *w = g.pointer(9);
+    const size_t bytes = g.size(10);
+    void *st = g.address(11);
+    return finish(g, ATTENTION, n, [&] {
+        return npas_paged_attention(c, q.p, q.stride, y, (float *)lse, heads, (const int32_t *)len, most, window, scale, w, bytes, st);
+    });
+}
+
+// mxfp4_quantize(x, codes, scales, M, K, dtype, stream)
+PyObject *mxfp4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 7)) return nullptr;
+    Args g{a};
+    const int M = g.integer(3), K = g.integer(4), dt = g.integer(5);
+    const Args::Rows x = g.rows(0, K);
+    void *codes = g.pointer(1), *scales = g.pointer(2), *st = g.address(6);
+    return finish(g, QUANTIZE, n, [&] { return npas_mxfp4_quantize(x.p, x.stride, codes, scales, M, K, (npas_dtype)dt, st); });
+}
+
+// mxfp4_dequantize(codes, scales, y, M, K, dtype, stream)
+PyObject *mxfp4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 7)) return nullptr;
+    Args g{a};
+    void *codes = g.pointer(0), *scales = g.pointer(1), *y = g.pointer(2);
+    const int M = g.integer(3), K = g.integer(4), dt = g.integer(5);
+    void *st = g.address(6);
+    return finish(g, DEQUANTIZE, n, [&] { return npas_mxfp4_dequantize(codes, scales, y, M, K, (npas_dtype)dt, st); });
+}
+
+// fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, IN)
+PyObject *fc_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 10)) return nullptr;
+    Args g{a};
+    npas_mxfp4 *p = (npas_mxfp4 *)g.handle(0);
+    const Args::Rows x = g.rows(1, g.integer(9));
+    void *y = g.pointer(2);
+    const int B = g.integer(3);
+    void *b = g.pointer(4);
+    const int act = g.integer(5);
+    void *w = g.pointer(6);
+    const size_t bytes = g.size(7);
+    void *st = g.address(8);
+    return finish(g, FC_MXFP4, n, [&] { return npas_fc_mxfp4(p, x.p, x.stride, y, B, b, (npas_act)act, w, bytes, st); });
+}
+
+// init(NpasError, c_void_p, the calls through ctypes in the order of Call)
 PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (!argc(n, 2 + CALLS)) return nullptr;
@@ -198,6 +363,12 @@ PyMethodDef methods[] = {
     {"fc_sparse", (PyCFunction)(void (*)(void))fc_sparse, METH_FASTCALL, nullptr},
     {"depthwise3x3", (PyCFunction)(void (*)(void))depthwise3x3, METH_FASTCALL, nullptr},
     {"run_stack", (PyCFunction)(void (*)(void))run_stack, METH_FASTCALL, nullptr},
+    {"gated_residual_norm", (PyCFunction)(void (*)(void))gated_residual_norm, METH_FASTCALL, nullptr},
+    {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, nullptr},
+    {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, nullptr},
+    {"mxfp4_quantize", (PyCFunction)(void (*)(void))mxfp4_quantize, METH_FASTCALL, nullptr},
+    {"mxfp4_dequantize", (PyCFunction)(void (*)(void))mxfp4_dequantize, METH_FASTCALL, nullptr},
+    {"fc_mxfp4", (PyCFunction)(void (*)(void))fc_mxfp4, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycalls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -210,6 +381,8 @@ PyMODINIT_FUNC PyInit__pycalls()
     s_value = PyUnicode_InternFromString("value");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
-    if (!s_handle || !s_value || !s_is_contiguous || !s_data_ptr) return nullptr;
+    s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    if (!s_handle || !s_value || !s_is_contiguous || !s_data_ptr || !s_shape || !s_stride) return nullptr;
     return PyModule_Create(&module);
 }
