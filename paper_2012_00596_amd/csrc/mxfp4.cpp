@@ -70,15 +70,15 @@ int upload(npas_mxfp4 *p, void *hip_stream)
         (void)hipGetLastError();
         return NPAS_OK; // host-only handle: export works, run calls fail loudly
     }
-    const size_t images = (size_t)p->groups * p->steps * 4096, words = (size_t)p->groups * p->quads * 256;
+    const size_t images = (size_t)p->groups * p->steps * 2048, words = (size_t)p->groups * p->quads * 128;
     std::vector<uint8_t> blob(images + words * 4, 0);
     uint8_t *sc = blob.data() + images;
     for (int o = 0; o < p->OUT; ++o) {
-        const int g = o >> 6, r = (o & 63) >> 2, j = o & 3;
+        const int g = o >> 6, r = (o & 63) >> 1, j = o & 1;
         for (int b = 0; b < p->blocks; ++b) {
-            const int step = b >> 2, lane = (b & 3) * 16 + r;
-            memcpy(&blob[(((size_t)g * p->steps + step) * 4 + j) * 1024 + lane * 16], &p->codes[((size_t)o * p->blocks + b) * 16], 16);
-            sc[((((size_t)g * p->quads + (step >> 2)) * 4 + j) * 64 + lane) * 4 + (step & 3)] = p->scales[(size_t)o * p->blocks + b];
+            const int step = b >> 1, lane = (b & 1) * 32 + r;
+            memcpy(&blob[(((size_t)g * p->steps + step) * 2 + j) * 1024 + lane * 16], &p->codes[((size_t)o * p->blocks + b) * 16], 16);
+            sc[((((size_t)g * p->quads + (step >> 2)) * 2 + j) * 64 + lane) * 4 + (step & 3)] = p->scales[(size_t)o * p->blocks + b];
         }
     }
     void *ptr = nullptr;
@@ -117,8 +117,9 @@ int check_rows(const void *a, const void *b, const void *c, int rows, int K, int
     return NPAS_OK;
 }
 
-// Activations in the workspace: images of 16 rows, then their scale words.
-size_t image_bytes(const npas_mxfp4 *p, int B) { return (size_t)((B + 15) / 16) * p->steps * 1024; }
+// Activations in the workspace: images of 32 rows, then their scale words.
+int row_tiles(int B) { return (int)(((int64_t)B + 31) / 32); }
+size_t image_bytes(const npas_mxfp4 *p, int B) { return (size_t)row_tiles(B) * p->steps * 1024; }
 
 } // namespace
 
@@ -163,7 +164,7 @@ int npas_pack_fc_mxfp4(const void *w_host, int OUT, int IN, npas_dtype dt, void 
     try {
         std::unique_ptr<npas_mxfp4> p(new npas_mxfp4);
         p->dtype = dt; p->OUT = OUT; p->IN = IN;
-        p->blocks = (IN + 31) / 32; p->steps = (p->blocks + 3) / 4; p->quads = (p->steps + 3) / 4; p->groups = (OUT + 63) / 64;
+        p->blocks = (IN + 31) / 32; p->steps = (p->blocks + 3) / 4 * 2; p->quads = (p->steps + 3) / 4; p->groups = (OUT + 63) / 64;
         p->codes.resize((size_t)OUT * p->blocks * 16);
         p->scales.resize((size_t)OUT * p->blocks);
         float v[32];
@@ -217,8 +218,8 @@ void npas_mxfp4_free(npas_mxfp4 *p)
 
 size_t npas_fc_mxfp4_workspace_bytes(const npas_mxfp4 *p, int B)
 {
-    if (!p || B <= 0) return 0;
-    return image_bytes(p, B) + (size_t)((B + 15) / 16) * p->quads * 256;
+    if (!p || B <= 0 || fc_mxfp4_quantises(B, p->steps)) return 0;
+    return image_bytes(p, B) + (size_t)row_tiles(B) * p->quads * 256;
 }
 
 int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void *y_dev, int B, const void *bias_dev, npas_act act,
@@ -228,8 +229,8 @@ int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void
         set_error("NULL argument (handle=%p x_dev=%p y_dev=%p)", (const void *)p, x_dev, y_dev);
         return NPAS_E_NULL;
     }
-    if (B <= 0 || x_stride < p->IN || x_stride > (int64_t)1 << 40 || (double)((B + 15) / 16) * p->groups > 2147483647.0 ||
-        (double)((B + 15) / 16) * p->steps > 2147483647.0) {
+    if (B <= 0 || x_stride < p->IN || x_stride > (int64_t)1 << 40 || (double)row_tiles(B) * p->groups > 2147483647.0 ||
+        (double)row_tiles(B) * p->steps > 2147483647.0) {
         set_error("bad shape B=%d, row stride %lld of %d elements", B, (long long)x_stride, p->IN);
         return NPAS_E_SHAPE;
     }
@@ -250,11 +251,15 @@ int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void
         set_error("packed layer has no device copy (packed on a machine without a GPU)");
         return NPAS_E_HIP;
     }
-    uint8_t *images = (uint8_t *)workspace_dev, *words = images + image_bytes(p, B);
-    QuantizeArgs q{x_dev, images, words, x_stride, B, p->IN, p->blocks, p->steps, p->quads};
-    if (int rc = launch_mxfp4_quantize_images(p->dtype, q, hip_stream)) return rc;
-    FcMxArgs a{images, (const uint32_t *)words, p->images, p->image_scales, (const float *)bias_dev, y_dev, B, p->OUT, p->steps, p->quads,
-               p->groups, (B + 15) / 16, act};
+    FcMxArgs a{x_dev, x_stride, nullptr, nullptr, p->images, p->image_scales, (const float *)bias_dev, y_dev, B, p->IN, p->OUT, p->blocks, p->steps,
+               p->quads, p->groups, row_tiles(B), act};
+    if (!fc_mxfp4_quantises(B, p->steps)) {
+        uint8_t *images = (uint8_t *)workspace_dev, *words = images + image_bytes(p, B);
+        QuantizeArgs q{x_dev, images, words, x_stride, B, p->IN, p->blocks, p->steps, p->quads};
+        if (int rc = launch_mxfp4_quantize_images(p->dtype, q, hip_stream)) return rc;
+        a.x_images = images;
+        a.x_scales = (const uint32_t *)words;
+    }
     return launch_fc_mxfp4(p->dtype, a, hip_stream);
 }
 
