@@ -32,12 +32,16 @@ struct QuantizeArgs {
     uint8_t *codes, *scales; // canonical rows; or images of activations and their scale words
     int64_t x_stride;
     int rows, K, blocks, steps, quads;
+    WideDiv by_blocks; // canonical rows: of a slab of rows, see row_slab
+    int slab;
 };
 
 struct DequantizeArgs {
     const uint8_t *codes, *scales;
     void *y;
     int rows, K, blocks;
+    WideDiv by_blocks;
+    int slab;
 };
 
 struct FcMxArgs {

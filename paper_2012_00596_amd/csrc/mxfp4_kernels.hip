@@ -32,17 +32,33 @@ __device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t &scale
     return c;
 }
 
-// Canonical rows: four lanes a block, 64 blocks of one row a workgroup.
+// Canonical rows: four neighbouring lanes a block, blocks counted through all rows of a slab (blockIdx.y), so that a row that ends in the
+// middle of a workgroup leaves no lane idle; two blocks' quarters a thread, both asked for before the first is used.
+// Memory bound: 8192 x 4100 bf16 in 18 us (4.7 TB/s; a workgroup a row's piece of 64 blocks 23).
 template <int DT> __global__ __launch_bounds__(256) void mxfp4_quantize_kernel(QuantizeArgs a)
 {
-    const int row = blockIdx.x, b = blockIdx.y * 64 + (int)(threadIdx.x >> 2), part = threadIdx.x & 3, k0 = b * 32 + part * 8;
-    float v[8];
-    load8<DT>(a.x, (size_t)row * a.x_stride + k0, a.K - k0, v);
-    uint32_t scale;
-    const uint32_t c = encode8(v, scale);
-    if (b >= a.blocks) return;
-    reinterpret_cast<uint32_t *>(a.codes)[((size_t)row * a.blocks + b) * 4 + part] = c;
-    if (part == 0) a.scales[(size_t)row * a.blocks + b] = (uint8_t)scale;
+    const int row0 = blockIdx.y * a.slab, part = threadIdx.x & 3;
+    const uint32_t end = (uint32_t)min(a.slab, a.rows - row0) * a.blocks;
+    float v[2][8];
+    uint32_t n[2];
+    size_t row[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        n[i] = blockIdx.x * 128 + i * 64 + (threadIdx.x >> 2);
+        const uint32_t m = n[i] < end ? n[i] : end - 1, r = fastdiv_wide(m, a.by_blocks);
+        row[i] = row0 + r;
+        const int k0 = (int)(m - r * a.blocks) * 32 + part * 8;
+        load8<DT>(a.x, row[i] * a.x_stride + k0, a.K - k0, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t scale;
+        const uint32_t c = encode8(v[i], scale);
+        if (n[i] >= end) continue;
+        const size_t b = (size_t)row0 * a.blocks + n[i];
+        reinterpret_cast<uint32_t *>(a.codes)[b * 4 + part] = c;
+        if (part == 0) a.scales[b] = (uint8_t)scale;
+    }
 }
 
 // Operand images: a workgroup takes a step of a tile, four neighbouring lanes a block; what it writes is one image.
@@ -58,22 +74,36 @@ template <int DT> __global__ __launch_bounds__(256) void mxfp4_quantize_images_k
     if (part == 0) a.scales[(((size_t)tile * a.quads + (step >> 2)) * 64 + h * 32 + r) * 4 + (step & 3)] = (uint8_t)scale;
 }
 
+// The way back, counted through like the rows above: a thread an eight of a row.
 template <int DT> __global__ __launch_bounds__(256) void mxfp4_dequantize_kernel(DequantizeArgs a)
 {
-    const int row = blockIdx.x, b = blockIdx.y * 64 + (int)(threadIdx.x >> 2), part = threadIdx.x & 3, k0 = b * 32 + part * 8;
-    if (b >= a.blocks) return;
-    const uint32_t c = reinterpret_cast<const uint32_t *>(a.codes)[((size_t)row * a.blocks + b) * 4 + part], s = a.scales[(size_t)row * a.blocks + b];
-    const float unit = s == 255 ? __uint_as_float(0x7fc00000u) : s ? __uint_as_float(s << 23) : __uint_as_float(0x00400000u);
-    float v[8];
-#define NPAS_PAIR(i)                                                     \
-    {                                                                    \
-        const auto p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, i); \
-        v[2 * i] = p[0] * unit;                                          \
-        v[2 * i + 1] = p[1] * unit;                                      \
+    const int row0 = blockIdx.y * a.slab, part = threadIdx.x & 3;
+    const uint32_t end = (uint32_t)min(a.slab, a.rows - row0) * a.blocks;
+    uint32_t c[2], s[2], n[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        n[i] = blockIdx.x * 128 + i * 64 + (threadIdx.x >> 2);
+        const size_t b = (size_t)row0 * a.blocks + (n[i] < end ? n[i] : end - 1);
+        c[i] = reinterpret_cast<const uint32_t *>(a.codes)[b * 4 + part];
+        s[i] = a.scales[b];
     }
-    NPAS_PAIR(0) NPAS_PAIR(1) NPAS_PAIR(2) NPAS_PAIR(3)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (n[i] >= end) return;
+        const uint32_t r = fastdiv_wide(n[i], a.by_blocks);
+        const int k0 = (int)(n[i] - r * a.blocks) * 32 + part * 8;
+        const float unit = __uint_as_float(s[i] == 255 ? 0x7fc00000u : s[i] ? s[i] << 23 : 0x00400000u);
+        float v[8];
+#define NPAS_PAIR(k)                                                             \
+    {                                                                            \
+        const auto p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], 1.f, k);   \
+        v[2 * k] = p[0] * unit;                                                  \
+        v[2 * k + 1] = p[1] * unit;                                              \
+    }
+        NPAS_PAIR(0) NPAS_PAIR(1) NPAS_PAIR(2) NPAS_PAIR(3)
 #undef NPAS_PAIR
-    store8<DT>(a.y, (size_t)row * a.K + k0, a.K - k0, v);
+        store8<DT>(a.y, (size_t)(row0 + r) * a.K + k0, a.K - k0, v);
+    }
 }
 
 // ---- product --------------------------------------------------------------------
@@ -407,7 +437,7 @@ template <typename F> static int with_dtype(int dt, const char *what, F &&f)
 
 int launch_mxfp4_quantize(int dt, const QuantizeArgs &a, void *stream)
 {
-    const dim3 grid((unsigned)a.rows, (unsigned)((a.blocks + 63) / 64));
+    const dim3 grid((unsigned)(((long)a.slab * a.blocks + 127) / 128), (unsigned)((a.rows + a.slab - 1) / a.slab));
     return with_dtype(dt, "4-bit quantisation", [&](auto dtc) {
         hipLaunchKernelGGL((mxfp4_quantize_kernel<decltype(dtc)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
     });
@@ -423,7 +453,7 @@ int launch_mxfp4_quantize_images(int dt, const QuantizeArgs &a, void *stream)
 
 int launch_mxfp4_dequantize(int dt, const DequantizeArgs &a, void *stream)
 {
-    const dim3 grid((unsigned)a.rows, (unsigned)((a.blocks + 63) / 64));
+    const dim3 grid((unsigned)(((long)a.slab * a.blocks + 127) / 128), (unsigned)((a.rows + a.slab - 1) / a.slab));
     return with_dtype(dt, "4-bit dequantisation", [&](auto dtc) {
         hipLaunchKernelGGL((mxfp4_dequantize_kernel<decltype(dtc)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
     });

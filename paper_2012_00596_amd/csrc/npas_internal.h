@@ -291,6 +291,12 @@ static_assert(sizeof(SmallMJoinArgs) == 2 * sizeof(SmallMArgs), "the kernel find
 struct WideDiv {
     uint32_t magic, shift;
 };
+inline WideDiv magic_div_wide(uint32_t d)
+{
+    uint32_t shift = 0;
+    while (shift < 30 && d > 2u << shift) ++shift;
+    return WideDiv{d <= 1 ? 0u : (uint32_t)(((1ull << (32 + shift)) + d - 1) / d), shift};
+}
 
 struct RingArgs {
     const void *x;
