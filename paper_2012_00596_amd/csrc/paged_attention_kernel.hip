@@ -234,25 +234,26 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
 }
 
 // One workgroup a (sequence, head): the cuts' sums, rescaled to the largest maximum and added; LANES lanes hold a cut's row, four elements
-// each, so that 512 / LANES cuts are read side by side.
-template <int DT, int LANES> __global__ __launch_bounds__(512) void paged_attention_join_kernel(AttentionArgs a)
+// each, so that THREADS / LANES cuts are read side by side.  One wave for up to 16 cuts (2048 rows of two cuts: 3 us, with eight
+// waves 8.5), eight for more (32 rows of 128 cuts 4.8 us; 512 cuts read one after the other by four waves 37).
+template <int DT, int LANES, int THREADS> __global__ __launch_bounds__(THREADS) void paged_attention_join_kernel(AttentionArgs a)
 {
-    constexpr int SIDE = 512 / LANES;
-    __shared__ float weight[kMaxSplits], part[8], total[8];
+    constexpr int SIDE = THREADS / LANES, WAVES = THREADS / 64;
+    __shared__ float weight[THREADS], part[WAVES], total[WAVES];
     __shared__ __align__(16) float so[SIDE][LANES * 4];
     const int s = blockIdx.x / a.heads, D = a.c.head_dim, tid = threadIdx.x, side = tid / LANES, d = tid % LANES * 4;
     const size_t row = blockIdx.x;
     int first, count;
     token_range(a, s, first, count);
     const int cuts = (count + a.chunk - 1) / a.chunk;
-    const float2 x = tid < cuts ? a.part_stat[row * a.splits + tid] : make_float2(-INFINITY, 0.f); // at most kMaxSplits = 512
+    const float2 x = tid < cuts ? a.part_stat[row * a.splits + tid] : make_float2(-INFINITY, 0.f); // no more cuts than threads
     float m = x.x;
 #pragma unroll
     for (int w = 32; w; w >>= 1) m = fmaxf(m, __shfl_xor(m, w));
     if ((tid & 63) == 0) part[tid >> 6] = m;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 8; ++w) m = fmaxf(m, part[w]);
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, part[w]);
     const float c = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
     float l = c * x.y;
     weight[tid] = c;
@@ -262,7 +263,7 @@ template <int DT, int LANES> __global__ __launch_bounds__(512) void paged_attent
     __syncthreads();
     l = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) l += total[w];
+    for (int w = 0; w < WAVES; ++w) l += total[w];
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     if (d < D)
 #pragma unroll 4
@@ -273,11 +274,11 @@ template <int DT, int LANES> __global__ __launch_bounds__(512) void paged_attent
         }
     *reinterpret_cast<float4 *>(&so[side][d]) = y;
     __syncthreads();
-    if (tid < D) {
+    for (int i = tid; i < D; i += THREADS) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < SIDE; ++i) sum += so[i][tid];
-        reinterpret_cast<uint16_t *>(a.y)[row * D + tid] = to_storage<DT>(l != 0.f ? sum / l : 0.f);
+        for (int k = 0; k < SIDE; ++k) sum += so[k][i];
+        reinterpret_cast<uint16_t *>(a.y)[row * D + i] = to_storage<DT>(l != 0.f ? sum / l : 0.f);
     }
     if (tid == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
@@ -304,10 +305,16 @@ int launch_paged_attention(int dt, const AttentionArgs &a, void *stream)
         if (a.c.head_dim <= 64) run(std::integral_constant<int, 2>{});
         else if (a.c.head_dim <= 128) run(std::integral_constant<int, 4>{});
         else run(std::integral_constant<int, 8>{});
-        const dim3 rows((unsigned)(a.c.sequences * a.heads));
-        if (a.splits > 1 && a.c.head_dim <= 64) hipLaunchKernelGGL((paged_attention_join_kernel<DT, 16>), rows, dim3(512), 0, st, a);
-        else if (a.splits > 1 && a.c.head_dim <= 128) hipLaunchKernelGGL((paged_attention_join_kernel<DT, 32>), rows, dim3(512), 0, st, a);
-        else if (a.splits > 1) hipLaunchKernelGGL((paged_attention_join_kernel<DT, 64>), rows, dim3(512), 0, st, a);
+        if (a.splits == 1) return;
+        auto join = [&](auto lanesc) {
+            constexpr int LANES = decltype(lanesc)::value;
+            const dim3 rows((unsigned)(a.c.sequences * a.heads));
+            if (a.splits <= 16) hipLaunchKernelGGL((paged_attention_join_kernel<DT, LANES, 64>), rows, dim3(64), 0, st, a);
+            else hipLaunchKernelGGL((paged_attention_join_kernel<DT, LANES, kMaxSplits>), rows, dim3(kMaxSplits), 0, st, a);
+        };
+        if (a.c.head_dim <= 64) join(std::integral_constant<int, 16>{});
+        else if (a.c.head_dim <= 128) join(std::integral_constant<int, 32>{});
+        else join(std::integral_constant<int, 64>{});
     };
     if (dt == NPAS_BF16) pick(std::integral_constant<int, NPAS_BF16>{});
     else pick(std::integral_constant<int, NPAS_F16>{});
