@@ -29,7 +29,7 @@ __device__ __forceinline__ void token_range(const AttentionArgs &a, int s, int &
 // instruction: row r of tile j is element VW r + j.  Nothing passes through LDS but the cache rows of the tokens.
 // The weights go in as two 16-bit numbers, high part and remainder: the matrix cores have time for both (the kernel waits for memory),
 // and the result is then as good as with 32-bit weights.
-template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * NW, NW == 8 || NC <= 4 ? 2 : 1) void paged_attention_kernel(AttentionArgs a)
+template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * NW, NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
 {
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
     constexpr int PITCH = DP + 4;
@@ -68,39 +68,39 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
     f32x4 o[VW] = {};
     float m = -INFINITY, l = 0.f;
 
-    struct Tile {
-        uint4 k[2][NC];
-        uint32_t v[8][VP * VD];
-        uint32_t absent;
-    };
-    auto load = [&](int tile, Tile &t) {
-        const uint32_t *at = rows + tile * 32;
+    // A tile's keys and values have one place each: the next tile's keys are asked for as soon as the scores are formed, its values as soon as
+    // they have been multiplied, so that one tile is on its way all the time and the registers leave room for more waves.
+    uint4 kt[2][NC];
+    uint32_t vt[8][VP * VD], absent;
+    auto load_keys = [&](int tile) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t row = at[16 * h + r];
+            const uint32_t row = rows[tile * 32 + 16 * h + r];
             const uint8_t *p = kb + (uint64_t)(row == kAbsent ? 0u : row) * row_bytes;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int d = 32 * c + 8 * q;
-                if (FULL || d < D) t.k[h][c] = *reinterpret_cast<const uint4 *>(p + 2 * d);
-                else t.k[h][c] = make_uint4(0, 0, 0, 0);
+                if (FULL || d < D) kt[h][c] = *reinterpret_cast<const uint4 *>(p + 2 * d);
+                else kt[h][c] = make_uint4(0, 0, 0, 0);
             }
         }
-        t.absent = 0;
+    };
+    auto load_values = [&](int tile) __attribute__((always_inline)) {
+        absent = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint4 four = *reinterpret_cast<const uint4 *>(at + 16 * h + 4 * q);
+            const uint4 four = *reinterpret_cast<const uint4 *>(rows + tile * 32 + 16 * h + 4 * q);
             const uint32_t row[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool none = row[i] == kAbsent;
-                if (none) t.absent |= 1u << (4 * h + i);
+                if (none) absent |= 1u << (4 * h + i);
                 const uint8_t *p = vb + (uint64_t)(none ? 0u : row[i]) * row_bytes;
 #pragma unroll
                 for (int e = 0; e < VP; ++e) {
                     const int d = VW * r + 8 * e;
                     const uint8_t *x = p + 2 * (FULL || d < D ? d : 0); // elements past the head: their results are not kept
-                    uint32_t *v = &t.v[4 * h + i][e * VD];
+                    uint32_t *v = &vt[4 * h + i][e * VD];
                     if constexpr (VD == 4) {
                         const uint4 w = *reinterpret_cast<const uint4 *>(x);
                         v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
@@ -112,17 +112,21 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
             }
         }
     };
-    auto compute = [&](const Tile &t) {
+    // One tile; MORE: another follows.
+    auto tile_step = [&](int next, auto morec) __attribute__((always_inline)) {
+        constexpr bool MORE = decltype(morec)::value;
         f32x4 c0 = {}, c1 = {};
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            c0 = mfma16<DT>(t.k[0][c], qf[c], c0);
-            c1 = mfma16<DT>(t.k[1][c], qf[c], c1);
+            c0 = mfma16<DT>(kt[0][c], qf[c], c0);
+            c1 = mfma16<DT>(kt[1][c], qf[c], c1);
         }
+        if (MORE) load_keys(next);
+        __builtin_amdgcn_sched_barrier(0);
         float x[8], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] = t.absent >> i & 1 ? -INFINITY : (i < 4 ? c0[i] : c1[i - 4]) * to2;
+            x[i] = absent >> i & 1 ? -INFINITY : (i < 4 ? c0[i] : c1[i - 4]) * to2;
             top = fmaxf(top, x[i]);
         }
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -144,18 +148,18 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
             lo[i] = pack2<DT>(p0 - from_storage<DT>((uint16_t)hi[i]), p1 - from_storage<DT>((uint16_t)(hi[i] >> 16)));
         }
         const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        uint32_t keep[8]; // an absent token's row is another's: it must not bring in an infinity or a NaN
+        if (__any(absent != 0)) // an absent token's row is another's: it must not bring in an infinity or a NaN
 #pragma unroll
-        for (int i = 0; i < 8; ++i) keep[i] = t.absent >> i & 1 ? 0u : 0xffffffffu;
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int w = 0; w < VW / 2; ++w) vt[i][w] = absent >> i & 1 ? 0u : vt[i][w];
 #pragma unroll
         for (int w = 0; w < VW / 2; ++w) {
-            uint32_t v[8], even[4], odd[4];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = t.v[i][w] & keep[i];
+            uint32_t even[4], odd[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                even[i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x05040100u);
-                odd[i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07060302u);
+                even[i] = __builtin_amdgcn_perm(vt[2 * i + 1][w], vt[2 * i][w], 0x05040100u);
+                odd[i] = __builtin_amdgcn_perm(vt[2 * i + 1][w], vt[2 * i][w], 0x07060302u);
             }
             const uint4 ve = make_uint4(even[0], even[1], even[2], even[3]), vo = make_uint4(odd[0], odd[1], odd[2], odd[3]);
             o[2 * w] = mfma16<DT>(ve, ph, o[2 * w]);
@@ -163,6 +167,9 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
             o[2 * w] = mfma16<DT>(ve, pl, o[2 * w]);
             o[2 * w + 1] = mfma16<DT>(vo, pl, o[2 * w + 1]);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (MORE) load_values(next);
+        __builtin_amdgcn_sched_barrier(0);
     };
 
     for (int base = 0; base < cnt; base += kRows) {
@@ -179,13 +186,11 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
         }
         __syncthreads();
         if (wave < tiles) {
-            Tile now, next;
-            load(wave, now);
-            for (int tile = wave; tile < tiles; tile += NW) {
-                if (tile + NW < tiles) load(tile + NW, next);
-                compute(now);
-                now = next;
-            }
+            int tile = wave;
+            load_keys(tile);
+            load_values(tile);
+            for (; tile + NW < tiles; tile += NW) tile_step(tile + NW, std::true_type{});
+            tile_step(0, std::false_type{}); // (the last by itself: a branch around the loads would make the counted waits wait for all of them)
         }
     }
 
