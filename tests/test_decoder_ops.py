@@ -304,6 +304,10 @@ ATTENTION = [  # heads, kv heads, D, page, lengths, window, dtype, holes
 @gpu
 @pytest.mark.parametrize("case", ATTENTION, ids=str)
 def test_attention(torch, case):
+    _run_attention(torch, case)
+
+
+def _run_attention(torch, case):
     """Ragged lengths over random pages; everything that no token names is NaN, in the cache and in the workspace; queries are slices of a
     joined projection at odd alignment."""
     H, KV, D, page, lengths, window, dt, holes = case
@@ -339,6 +343,90 @@ def test_attention(torch, case):
         outs.append(y)
     assert torch.equal(outs[0], outs[1]), "two calls differ"
     _check_attention(torch, q, k, v, table, n, D ** -0.5, window, top, dt, y, lse)
+
+
+CUTS = [  # many cuts and few, every width of a head's rows; one cut of more tokens than are looked up at once
+    (8, 8, 64, 16, [6000, 70], 0, npas.F16, False), (4, 2, 256, 16, [5000, 100], 0, npas.BF16, True),
+    (16, 8, 64, 16, [2000, 1, 128, 0], 0, npas.BF16, False), (2, 2, 200, 32, [1100, 500, 257], 0, npas.F16, False),
+    (2, 1, 8, 16, [5000], 0, npas.F16, True), (12, 4, 96, 16, [3000, 2900], 1000, npas.BF16, False),
+    (17, 1, 128, 16, [700, 640], 0, npas.BF16, False), (64, 1, 64, 16, [3000], 0, npas.F16, False)]
+
+
+@gpu
+@pytest.mark.parametrize("case", CUTS, ids=str)
+def test_attention_cuts(torch, case):
+    _run_attention(torch, case)
+
+
+@gpu
+@pytest.mark.parametrize("H,KV,D,length", [(4, 2, 64, 40), (8, 2, 128, 3000)])
+def test_attention_nan_and_infinities_stay_in_their_heads(torch, H, KV, D, length):
+    """A NaN key or an infinite value reaches the heads of its group and no other; a sequence whose pages are all missing is zero."""
+    dt, S, page = npas.BF16, 3, 16
+    columns = -(-length // page)
+    k, v = (_rand(torch, 110 + i, (S * columns, KV, page, D), dt) for i in range(2))
+    q = _rand(torch, 112, (S, H, D), dt)
+    table = torch.arange(S * columns, dtype=torch.int32).reshape(S, columns)
+    n = torch.full((S,), length, dtype=torch.int32)
+    gone = table.clone()
+    gone[1] = -1
+    need = npas.paged_attention_workspace_bytes(npas.KvCache(k.cuda(), v.cuda(), table.cuda(), dt), H, length)
+    ws = torch.full((max(need, 16) // 4 + 1,), float("nan"), device="cuda")
+
+    def run(k, v, table):
+        y, lse = torch.empty((S, H, D), dtype=q.dtype, device="cuda"), torch.empty((S, H), device="cuda")
+        npas.paged_attention(npas.KvCache(k.cuda(), v.cuda(), table.cuda(), dt), q.cuda(), y, H, n.cuda(), length, D ** -0.5, lse=lse,
+                             workspace=ws, workspace_bytes=need)
+        return y.cpu(), lse.cpu()
+    clean, _ = run(k, v, table)
+    kb, vb = k.clone(), v.clone()
+    kb[table[0, columns - 1], 0, 0, 3] = float("nan")
+    vb[table[2, 0], 1, 5, 7] = float("inf")
+    y, lse = run(kb, vb, gone)
+    G = H // KV
+    assert bool(torch.isnan(y[0, :G]).all()) and torch.equal(y[0, G:], clean[0, G:])
+    assert bool((y[1] == 0).all()) and bool((lse[1] == -float("inf")).all())
+    assert bool((~torch.isfinite(y[2, G:2 * G, 7])).all())
+    others = [d for d in range(D) if d != 7]
+    assert torch.equal(y[2, G:2 * G][:, others], clean[2, G:2 * G][:, others]) and torch.equal(y[2, :G], clean[2, :G])
+
+
+@gpu
+def test_calls_by_address_and_through_ctypes(torch):
+    """The same results from tensors, from addresses of contiguous rows, and where an argument goes through ctypes."""
+    S, H, KV, D, page, dt, T = 3, 4, 2, 64, 16, npas.F16, 3
+    table = torch.arange(S * 2, dtype=torch.int32).reshape(S, 2).cuda()
+    q, kx, vx = (_rand(torch, 120 + i, (T, n, D), dt).cuda() for i, n in enumerate((H, KV, KV)))
+    pos, n = torch.tensor([0, 5, 20], dtype=torch.int32, device="cuda"), torch.tensor([1, 6, 21], dtype=torch.int32, device="cuda")
+    cs = torch.rand((32, D), device="cuda")
+    w = torch.rand(H * D, device="cuda")
+    g = _rand(torch, 125, (H * D,), dt).cuda()
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    results = []
+    for how in ("tensors", "addresses", "ctypes"):
+        k, v = (torch.zeros((S * 2, KV, page, D), dtype=torch.float16, device="cuda") for _ in range(2))
+        cache = npas.KvCache(k, v, table, dt)
+        qo, y, ho, no = (torch.zeros((T, H, D), dtype=torch.float16, device="cuda") for _ in range(4))
+        p = (lambda t: t.data_ptr()) if how == "addresses" else (lambda t: t)
+        stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream) if how == "ctypes" else torch.cuda.current_stream().cuda_stream
+        npas.kv_append(cache, p(q), p(kx), p(vx), p(qo), T, H, p(pos), cos_sin=cs, rot_dim=D, stream=stream)
+        npas.paged_attention(cache, p(qo), p(y), H, p(n), 32, 0.125, workspace=p(ws), workspace_bytes=1 << 16, stream=stream)
+        npas.gated_residual_norm(p(y), p(q), p(ho), p(no), T, H * D, dt, gate=g, post_weight=p(w), pre_weight=p(w), stream=stream)
+        codes, scales, back = torch.zeros((T, H * D // 2), dtype=torch.uint8, device="cuda"), torch.zeros((T, H * D // 32), dtype=torch.uint8, device="cuda"), torch.zeros_like(no)
+        npas.mxfp4_quantize(p(no), p(codes), p(scales), T, H * D, dt, stream)
+        npas.mxfp4_dequantize(p(codes), p(scales), p(back), T, H * D, dt, stream)
+        packed = npas.pack_fc_mxfp4(np.ones((7, H * D), np.float16).view(np.uint16), dt)
+        out = torch.zeros((T, 7), dtype=torch.float16, device="cuda")
+        npas.fc_mxfp4(packed, p(no), p(out), T, None, npas.ACT_NONE, p(ws), 1 << 16, stream)
+        torch.cuda.synchronize()
+        results.append([t.cpu() for t in (qo, k, v, y, ho, no, codes, scales, back, out)])
+    for r in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], r))
+    with pytest.raises(AssertionError):
+        npas.kv_append(cache, q[:, :, ::2], kx, vx, qo, T, H, pos)
+    with pytest.raises(npas.NpasError) as e:
+        npas.paged_attention(cache, q, y, H, n, 0, 1.0)
+    assert e.value.code == npas.E_SHAPE
 
 
 @gpu

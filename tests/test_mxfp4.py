@@ -257,6 +257,49 @@ def test_product(torch, dt, B, IN, OUT):
     _product(torch, B + IN + OUT, B, IN, OUT, dt, bias=OUT % 2 == 1)
 
 
+# Enough rows and outputs for tiles of 128 x 128 (more than 1024 pieces of 32 x 32) and of 256 x 128 (512 of them): edges in both
+# directions, one stage of 128 elements to many.
+TILES = [(700, 70, 1500), (1030, 130, 1090), (641, 300, 1664), (700, 400, 1700), (1100, 640, 1025), (700, 1000, 1501), (4000, 200, 4090),
+         (4096, 520, 4096), (3900, 1090, 4033), (8200, 33, 2051)]
+
+
+@gpu
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("B,IN,OUT", TILES)
+def test_product_in_tiles(torch, dt, B, IN, OUT):
+    print(f"fc_mxfp4 B={B} IN={IN} OUT={OUT} dtype={dt}", flush=True)
+    _product(torch, B + IN + OUT, B, IN, OUT, dt, bias=OUT % 2 == 1)
+
+
+@gpu
+@pytest.mark.parametrize("act", [npas.ACT_RELU, npas.ACT_RELU6, npas.ACT_HARDSWISH])
+@pytest.mark.parametrize("B,OUT", [(700, 1500), (4000, 4090)])
+def test_product_in_tiles_activations(torch, act, B, OUT):
+    _product(torch, 6, B, 150, OUT, npas.F16, act=act)
+
+
+@gpu
+@pytest.mark.parametrize("B", [30, 300, 1500])
+def test_rows_that_stand_for_nan_stay_nan_through_an_activation(torch, B):
+    """An infinity in a row's block makes the whole row NaN, ReLU and hard-swish pass it on, and no other row changes."""
+    dt, IN, OUT = npas.BF16, 200, 1500
+    ws, w64 = sample(41, (OUT, IN), dt, "plain")
+    p = npas.pack_fc_mxfp4(ws, dt)
+    need = p.workspace_bytes(B)
+    work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    xs, x64 = sample(42, (B, IN), dt)
+    bad = xs.copy()
+    bad[B // 2, 70] = 0x7F80
+    for act in (npas.ACT_RELU, npas.ACT_RELU6, npas.ACT_HARDSWISH):
+        y = [torch.empty((B, OUT), dtype=torch.int16, device="cuda") for _ in range(2)]
+        for x, out in zip((xs, bad), y):
+            npas.fc_mxfp4(p, _dev(torch, x, dt), out, B, None, act, work, need)
+        clean, hit = (_f64(t, dt) for t in y)
+        assert np.isnan(hit[B // 2]).all()
+        keep = np.arange(B) != B // 2
+        np.testing.assert_array_equal(clean[keep], hit[keep])
+
+
 @gpu
 @pytest.mark.parametrize("act", [npas.ACT_RELU, npas.ACT_RELU6, npas.ACT_HARDSWISH])
 @pytest.mark.parametrize("B", [3, 150])
