@@ -258,9 +258,9 @@ void npas_stack_free(npas_stack *s);
  * What a transformer's decoder block needs between projections that run as npas_fc_sparse (block-based pruning) or npas_fc_mxfp4:
  * norms with gate and residual, a paged cache of keys and values, attention of one new token a sequence.  Rows are tokens; a
  * row is contiguous, rows lie `.._stride` elements apart (slices of a joined projection need no copy).  Pointers need the
- * alignment of their element type, the two caches 16 bytes.  Sums, norms and softmax statistics are held in fp32; a result is
- * rounded to the storage type once.  Nothing allocates or synchronises; lengths, positions and page tables are read on the
- * device, so a captured HIP graph may be replayed with new ones. */
+ * alignment of their element type, the two caches 16 bytes.  Outputs overlap no input but where a call says so.  Sums, norms and
+ * softmax statistics are held in fp32; a result is rounded to the storage type once.  Nothing allocates or synchronises; lengths,
+ * positions and page tables are read on the device, so a captured HIP graph may be replayed with new ones. */
 
 /* The end of one block and the start of the next, one pass over the rows:
  *   p = branch * post_weight / sqrt(mean(branch^2) + eps)     (post_weight NULL: p = branch)
@@ -315,7 +315,8 @@ int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t 
  * e = floor(log2(largest magnitude)) - 2 (at least -127), kept as the byte e + 127, and per element the 4-bit float (sign, two
  * exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) nearest to x / 2^e, ties to the even code, at most 6.  An all-zero
  * block has byte 0; a block that holds an infinity or a NaN has byte 255 and stands for NaN throughout.
- * codes [rows][16 * ceil(K / 32)]: two elements a byte, the lower four bits first; scales [rows][ceil(K / 32)]. */
+ * codes [rows][16 * ceil(K / 32)], 4-byte aligned: two elements a byte, the lower four bits first; scales [rows][ceil(K / 32)].
+ * As above: x may be a slice (row r at x + r * x_stride), outputs overlap no input, nothing allocates or synchronises but the pack call. */
 int npas_mxfp4_quantize(const void *x_dev, int64_t x_stride, void *codes_dev, void *scales_dev, int rows, int K, npas_dtype dt,
                         void *hip_stream);
 /* The values that codes and scales stand for, y [rows][K] in storage type dt (a value that dt cannot hold is rounded). */
@@ -331,7 +332,8 @@ int npas_mxfp4_export(const npas_mxfp4 *p, uint8_t *codes_host, uint8_t *scales_
 void npas_mxfp4_free(npas_mxfp4 *p);
 /* y[b][o] = act(bias[o] + sum_i Wq[o][i] xq[b][i]): x [B][IN] (row b at x + b * x_stride, the handle's storage type) is quantised to
  * microscaled 4-bit floats, blocks along IN, and multiplied by the packed weights on the matrix cores with fp32 accumulation;
- * y [B][OUT] contiguous, bias fp32 [OUT], nullable.  The workspace (16-byte aligned) holds the quantised activations. */
+ * y [B][OUT] contiguous, bias fp32 [OUT], nullable.  A row with an infinity or a NaN gives NaN throughout, whatever the activation.
+ * The workspace (16-byte aligned, npas_fc_mxfp4_workspace_bytes, 0 for a few rows) holds the quantised activations. */
 size_t npas_fc_mxfp4_workspace_bytes(const npas_mxfp4 *p, int B);
 int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void *y_dev, int B, const void *bias_dev, npas_act act,
                   void *workspace_dev, size_t workspace_bytes, void *hip_stream);

@@ -173,6 +173,10 @@ int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t 
         return NPAS_E_SHAPE;
     }
     const Cuts cuts = plan_cuts(a.c, heads, max_length, window);
+    if ((double)a.c.sequences * cuts.splits * heads > 2147483647.0) {
+        set_error("%d sequences x %d heads x %d cuts of max_length=%d are too many workgroups", a.c.sequences, heads, cuts.splits, max_length);
+        return NPAS_E_SHAPE;
+    }
     const size_t need = cuts.bytes;
     if (need && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 16))) {
         set_error("paged attention needs %zu bytes of workspace at a multiple of 16, got %zu at %p", need, workspace_bytes, workspace_dev);

@@ -152,7 +152,7 @@ int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream)
     hipStream_t st = (hipStream_t)stream;
     with_dtype(dt, [&](auto dtc) {
         constexpr int DT = decltype(dtc)::value;
-        const dim3 rows((unsigned)a.T), quads((unsigned)((a.T + 3) / 4));
+        const dim3 rows((unsigned)a.T), quads(((unsigned)a.T + 3) / 4);
         if (a.D <= 512) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 1>), quads, dim3(256), 0, st, a);
         else if (a.D <= 1024) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 1>), quads, dim3(256), 0, st, a);
         else if (a.D <= 2048) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 4>), rows, dim3(256), 0, st, a);
@@ -168,6 +168,8 @@ int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream)
 
 // One workgroup a token.  A unit is VL consecutive elements: rotated in themselves (PAIRS), rotated with their partners rot_dim / 2
 // further on (halves), or copied (the rest of a rotated head, the values).  Queries first, then keys, then values.
+// Memory bound: 8191 tokens of 32 + 8 + 8 heads of 128, bf16, 206 MB in 32.7 us (6.3 TB/s, what is written partly stays in the Infinity
+// Cache); a decode step of 24 tokens 3.0 us.
 template <int DT, int VL, bool PAIRS> __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a)
 {
     const int t = blockIdx.x, D = a.c.head_dim, half = a.rot_dim / 2;
