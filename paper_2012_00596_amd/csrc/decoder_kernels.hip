@@ -166,11 +166,12 @@ int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream)
 
 // ---- append to the paged cache -------------------------------------------------
 
-// One workgroup a token.  A unit is VL consecutive elements: rotated in themselves (PAIRS), rotated with their partners rot_dim / 2
-// further on (halves), or copied (the rest of a rotated head, the values).  Queries first, then keys, then values.
+// One workgroup a token.  A unit is eight consecutive elements (fewer at the end of a part): rotated in themselves (PAIRS), rotated with
+// their partners rot_dim / 2 further on (halves), or copied (the rest of a rotated head, the values).  Queries first, then keys, then values.
 // Memory bound: 8191 tokens of 32 + 8 + 8 heads of 128, bf16, 206 MB in 32.7 us (6.3 TB/s, what is written partly stays in the Infinity
 // Cache); a decode step of 24 tokens 3.0 us.
-template <int DT, int VL, bool PAIRS> __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a)
+// WHOLE: every part of a head is a multiple of eight long (the checks for fewer cost 5-50 %: 2000 tokens of 64 + 8 + 8 heads 15.0 -> 23.3 us).
+template <int DT, bool PAIRS, bool WHOLE> __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a)
 {
     const int t = blockIdx.x, D = a.c.head_dim, half = a.rot_dim / 2;
     const int s = a.sequence ? a.sequence[t] : t, pos = a.position[t];
@@ -180,41 +181,45 @@ template <int DT, int VL, bool PAIRS> __global__ __launch_bounds__(256) void kv_
     const bool stored = (uint32_t)page < (uint32_t)a.c.pages;
     const size_t row0 = stored ? (size_t)page * a.c.kv_heads * a.c.page_size + slot : 0; // cache row of the first head
     const float *cs = a.cos_sin + (size_t)(token ? pos : 0) * a.rot_dim;
-    const int rot_units = (PAIRS ? a.rot_dim : half) / VL, head_units = rot_units + (D - a.rot_dim) / VL, value_units = D / VL;
+    const int rotated_part = PAIRS ? a.rot_dim : half, rot_units = (rotated_part + 7) >> 3;
+    const int head_units = rot_units + ((D - a.rot_dim + 7) >> 3), value_units = D >> 3;
     const int nq = a.q ? a.heads * head_units : 0, nk = a.c.kv_heads * head_units, nv = a.c.kv_heads * value_units;
-    for (int u = threadIdx.x; u < nq + nk + nv; u += 256) {
+    for (int u = threadIdx.x; u < nq + nk + nv; u += blockDim.x) {
         const bool is_q = u < nq, is_v = u >= nq + nk;
         if (!is_q && !stored) break;
         const int w = is_q ? u : is_v ? u - nq - nk : u - nq, per = is_v ? value_units : head_units, head = w / per, j = w - head * per;
         const bool rotated = !is_v && j < rot_units;
-        const int d = is_v ? j * VL : rotated ? j * VL : a.rot_dim + (j - rot_units) * VL;
+        const int d = is_v || rotated ? j * 8 : a.rot_dim + (j - rot_units) * 8, n = WHOLE ? 8 : min(8, (rotated ? rotated_part : D) - d);
         const void *src = is_q ? a.q : is_v ? a.v : a.k;
         void *dst = is_q ? a.q_out : is_v ? a.c.v : a.c.k;
         const size_t in = (size_t)t * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (size_t)head * D + d;
         const size_t out = (is_q ? ((size_t)t * a.heads + head) * D : (row0 + (size_t)head * a.c.page_size) * D) + d;
-        float x[8], p[8];
-        load8<DT>(src, in, VL, x);
-        if (!PAIRS && rotated) load8<DT>(src, in + half, VL, p);
+        float x[8], p[8], c[8], z[8];
+        load8<DT>(src, in, n, x);
         if (!token) { // only queries come here
 #pragma unroll
-            for (int k = 0; k < VL; ++k) x[k] = p[k] = 0.f;
-        } else if (PAIRS && rotated) {
+            for (int k = 0; k < 8; ++k) x[k] = p[k] = 0.f;
+        } else if (PAIRS && rotated) { // n is even
+            const int m = n >> 1;
 #pragma unroll
-            for (int k = 0; k < VL / 2; ++k) {
-                const float c = cs[d / 2 + k], n = cs[half + d / 2 + k], u0 = x[2 * k], u1 = x[2 * k + 1];
-                x[2 * k] = u0 * c - u1 * n;
-                x[2 * k + 1] = u1 * c + u0 * n;
+            for (int k = 0; k < 4; ++k) {
+                const float co = k < m ? cs[d / 2 + k] : 0.f, si = k < m ? cs[half + d / 2 + k] : 0.f, u0 = x[2 * k], u1 = x[2 * k + 1];
+                x[2 * k] = u0 * co - u1 * si;
+                x[2 * k + 1] = u1 * co + u0 * si;
             }
         } else if (rotated) {
+            load8<DT>(src, in + half, n, p);
+            load8<NPAS_F32>(cs, d, n, c);
+            load8<NPAS_F32>(cs, half + d, n, z);
 #pragma unroll
-            for (int k = 0; k < VL; ++k) {
-                const float c = cs[d + k], n = cs[half + d + k], u0 = x[k], u1 = p[k];
-                x[k] = u0 * c - u1 * n;
-                p[k] = u1 * c + u0 * n;
+            for (int k = 0; k < 8; ++k) {
+                const float u0 = x[k], u1 = p[k];
+                x[k] = u0 * c[k] - u1 * z[k];
+                p[k] = u1 * c[k] + u0 * z[k];
             }
         }
-        store8<DT>(dst, out, VL, x);
-        if (!PAIRS && rotated) store8<DT>(dst, out + half, VL, p);
+        store8<DT>(dst, out, n, x);
+        if (!PAIRS && rotated) store8<DT>(dst, out + half, n, p);
     }
 }
 
@@ -223,15 +228,15 @@ int launch_kv_append(int dt, const AppendArgs &a, void *stream)
     hipStream_t st = (hipStream_t)stream;
     auto pick = [&](auto dtc) {
         constexpr int DT = decltype(dtc)::value;
-        const dim3 grid((unsigned)a.T), block(256);
-        // vectors of 8 where a pair's elements, or the two halves' vectors, start at multiples of 8 (the head's rest then does too)
-        if (a.pairs) {
-            if (a.rot_dim % 8 == 0) hipLaunchKernelGGL((kv_append_kernel<DT, 8, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((kv_append_kernel<DT, 2, true>), grid, block, 0, st, a);
-        } else {
-            if (a.rot_dim % 16 == 0) hipLaunchKernelGGL((kv_append_kernel<DT, 8, false>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((kv_append_kernel<DT, 1, false>), grid, block, 0, st, a);
-        }
+        // as many waves as one pass over the token's units fills, up to four (8191 tokens of 1 + 1 + 1 heads of 64: 5.7 us, always four 10.0)
+        const int head_units = ((a.pairs ? a.rot_dim : a.rot_dim / 2) + 7) / 8 + (a.c.head_dim - a.rot_dim + 7) / 8;
+        const long units = (long)((a.q ? a.heads : 0) + a.c.kv_heads) * head_units + (long)a.c.kv_heads * (a.c.head_dim / 8);
+        const dim3 grid((unsigned)a.T), block(units <= 64 ? 64 : units <= 128 ? 128 : units <= 192 ? 192 : 256);
+        const bool whole = a.rot_dim % (a.pairs ? 8 : 16) == 0;
+        if (a.pairs && whole) hipLaunchKernelGGL((kv_append_kernel<DT, true, true>), grid, block, 0, st, a);
+        else if (a.pairs) hipLaunchKernelGGL((kv_append_kernel<DT, true, false>), grid, block, 0, st, a);
+        else if (whole) hipLaunchKernelGGL((kv_append_kernel<DT, false, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((kv_append_kernel<DT, false, false>), grid, block, 0, st, a);
     };
     if (dt == NPAS_BF16) pick(std::integral_constant<int, NPAS_BF16>{});
     else pick(std::integral_constant<int, NPAS_F16>{});
