@@ -7,39 +7,87 @@
 
 namespace npas {
 
-// A quarter of a block (8 elements) to its codes; the four lanes of a block are neighbours and agree on its scale byte.  The largest
-// magnitude is compared as bits: a NaN is above an infinity, an infinity above every number.  v times 2^-e is exact (down to the smallest
-// fp32 numbers), the conversion rounds to nearest, ties to the even code.
-__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t &scale)
+// A quarter of a block: 8 elements as they are stored (fp32: as they are, 16-bit types: four words).
+template <int DT> struct Quarter {
+    uint32_t w[DT == NPAS_F32 ? 8 : 4];
+};
+template <int DT> __device__ __forceinline__ void load_quarter(const void *p, size_t i, int n, Quarter<DT> &q)
 {
-    uint32_t top = 0;
+    if constexpr (DT == NPAS_F32) {
+        float v[8];
+        load8<DT>(p, i, n, v);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    const uint32_t e = top >> 23;
+        for (int k = 0; k < 8; ++k) q.w[k] = __float_as_uint(v[k]);
+    } else if (n >= 8) {
+        const Words16 x = *reinterpret_cast<const Words16 *>(reinterpret_cast<const uint16_t *>(p) + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q.w[k] = x.w[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = 2 * k < n ? reinterpret_cast<const uint16_t *>(p)[i + 2 * k] : 0;
+            const uint32_t hi = 2 * k + 1 < n ? reinterpret_cast<const uint16_t *>(p)[i + 2 * k + 1] : 0;
+            q.w[k] = lo | hi << 16;
+        }
+    }
+}
+
+// A quarter's codes; the four lanes of a block are neighbours and agree on its scale byte.  Magnitudes are compared as bits (16-bit types two at
+// a time): a NaN is above an infinity, an infinity above every number.  The conversions round to nearest, ties to the even code, and stop
+// at 6; x / 2^e is exact in them for 16-bit types (checked for every value with every scale that a block of it can have), as is x times
+// 2^-e in fp32 (down to the smallest numbers).
+template <int DT> __device__ __forceinline__ uint32_t encode8(const Quarter<DT> &q, uint32_t &scale)
+{
+    uint32_t e, c = 0;
+    if constexpr (DT == NPAS_F32) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = max(top, q.w[k] & 0x7fffffffu);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+        e = top >> 23;
+    } else {
+        typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, q.w[k] & 0x7fff7fffu));
+#pragma unroll
+        for (int x = 1; x < 3; ++x) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, __shfl_xor(__builtin_bit_cast(int, top), x)));
+        const uint16_t m = top[0] > top[1] ? top[0] : top[1];
+        e = (__float_as_uint(from_storage<DT>(m)) & 0x7fffffffu) >> 23;
+    }
     scale = e == 255 ? 255u : e > 2 ? e - 2 : 0u;
     if (e == 255) return 0u;
-    const float inv = __uint_as_float((254u - scale) << 23);
-    uint32_t c = 0;
-    float w[8];
+    if constexpr (DT == NPAS_F32) {
+        const float inv = __uint_as_float((254u - scale) << 23);
+        float w[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = __builtin_amdgcn_fmed3f(v[k] * inv, -6.f, 6.f);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[0], w[1], 1.f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[2], w[3], 1.f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[4], w[5], 1.f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[6], w[7], 1.f, 3);
+        for (int k = 0; k < 8; ++k) w[k] = __builtin_amdgcn_fmed3f(__uint_as_float(q.w[k]) * inv, -6.f, 6.f);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[0], w[1], 1.f, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[2], w[3], 1.f, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[4], w[5], 1.f, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, w[6], w[7], 1.f, 3);
+    } else {
+        const float unit = __uint_as_float(scale ? scale << 23 : 0x00400000u);
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+        typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+#define NPAS_PAIR(k)                                                                                                                  \
+    if constexpr (DT == NPAS_BF16) c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, q.w[k]), unit, k);     \
+    else c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(f16x2, q.w[k]), unit, k);
+        NPAS_PAIR(0) NPAS_PAIR(1) NPAS_PAIR(2) NPAS_PAIR(3)
+#undef NPAS_PAIR
+    }
     return c;
 }
 
 // Canonical rows: four neighbouring lanes a block, blocks counted through all rows of a slab (blockIdx.y), so that a row that ends in the
 // middle of a workgroup leaves no lane idle; two blocks' quarters a thread, both asked for before the first is used.
-// Memory bound: 8192 x 4100 bf16 in 15.6 us (5.4 TB/s; a workgroup a row's piece of 64 blocks 23).
+// Memory bound: 8192 x 4100 bf16 in 15 us (5.6 TB/s; a workgroup a row's piece of 64 blocks 23).
 template <int DT> __global__ __launch_bounds__(256) void mxfp4_quantize_kernel(QuantizeArgs a)
 {
     const int row0 = blockIdx.y * a.slab, part = threadIdx.x & 3;
     const uint32_t end = (uint32_t)min(a.slab, a.rows - row0) * a.blocks;
-    float v[2][8];
+    Quarter<DT> v[2];
     uint32_t n[2];
     size_t row[2];
 #pragma unroll
@@ -48,12 +96,12 @@ template <int DT> __global__ __launch_bounds__(256) void mxfp4_quantize_kernel(Q
         const uint32_t m = n[i] < end ? n[i] : end - 1, r = fastdiv_wide(m, a.by_blocks);
         row[i] = row0 + r;
         const int k0 = (int)(m - r * a.blocks) * 32 + part * 8;
-        load8<DT>(a.x, row[i] * a.x_stride + k0, a.K - k0, v[i]);
+        load_quarter<DT>(a.x, row[i] * a.x_stride + k0, a.K - k0, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         uint32_t scale;
-        const uint32_t c = encode8(v[i], scale);
+        const uint32_t c = encode8<DT>(v[i], scale);
         if (n[i] >= end) continue;
         const size_t b = (size_t)row0 * a.blocks + n[i];
         reinterpret_cast<uint32_t *>(a.codes)[b * 4 + part] = c;
@@ -67,10 +115,10 @@ template <int DT> __global__ __launch_bounds__(256) void mxfp4_quantize_images_k
 {
     const int step = blockIdx.x % a.steps, tile = blockIdx.x / a.steps, h = threadIdx.x >> 7, r = threadIdx.x >> 2 & 31, part = threadIdx.x & 3;
     const int row = tile * 32 + r, k0 = step * 64 + h * 32 + part * 8;
-    float v[8];
-    load8<DT>(a.x, (size_t)(row < a.rows ? row : 0) * a.x_stride + k0, row < a.rows ? a.K - k0 : 0, v);
+    Quarter<DT> v;
+    load_quarter<DT>(a.x, (size_t)(row < a.rows ? row : 0) * a.x_stride + k0, row < a.rows ? a.K - k0 : 0, v);
     uint32_t scale;
-    const uint32_t c = encode8(v, scale);
+    const uint32_t c = encode8<DT>(v, scale);
     reinterpret_cast<uint32_t *>(a.codes)[((size_t)tile * a.steps + step) * 256 + threadIdx.x] = c;
     if (part == 0) a.scales[(((size_t)tile * a.quads + (step >> 2)) * 64 + h * 32 + r) * 4 + (step & 3)] = (uint8_t)scale;
 }
@@ -146,12 +194,12 @@ __device__ __forceinline__ float2 group_bias(const FcMxArgs &a, int o)
 // are added through LDS, in the waves' order.  Nothing passes through LDS on the way in: all of a run's loads are asked for at once.
 // FUSED (few enough rows that quantising them again in every workgroup costs less than a launch): the workgroup brings its rows to
 // codes in LDS, four lanes a block, while its first weights are on their way.
-// One row of 4096 x 4096 4.9 us (8.9 MB: launch, one round trip to memory, the exchange of the sums; 1.8 us at the rate of a copy), 256 rows
+// One row of 4096 x 4096 4.2-4.9 us (8.9 MB: launch, one round trip to memory, the exchange of the sums; 1.8 us at the rate of a copy), 256 rows
 // of 1280 x 1000 4.0 us and 2.6 for their images.
 template <int DT, int W, int J, bool FUSED> __global__ __launch_bounds__(64 * W) void fc_mxfp4_split_kernel(FcMxArgs a)
 {
     constexpr int PARTS = 2 / J;
-    __shared__ __align__(16) uint8_t lds[W * J * 4096]; // codes and scale bytes of at most 320 steps (34 bytes each), then the sums
+    __shared__ __align__(16) uint8_t lds[W * J * 4096]; // codes and scale bytes of at most 512 steps (34 bytes each), then the sums
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
     const int part = blockIdx.x % PARTS, group = blockIdx.x / PARTS % a.groups, tile = blockIdx.x / PARTS / a.groups;
     const uint4 *x = reinterpret_cast<const uint4 *>(a.x_images) + (size_t)tile * a.steps * 64 + lane;
@@ -206,10 +254,10 @@ template <int DT, int W, int J, bool FUSED> __global__ __launch_bounds__(64 * W)
         const int quarters = a.steps * 8; // of a row, up to the last step's end
         for (int u = threadIdx.x; u < rows * quarters; u += 64 * W) {
             const int row = u / quarters, k = u - row * quarters;
-            float v[8];
-            load8<DT>(a.x, (size_t)(tile * 32 + row) * a.x_stride + k * 8, a.IN - k * 8, v);
+            Quarter<DT> v;
+            load_quarter<DT>(a.x, (size_t)(tile * 32 + row) * a.x_stride + k * 8, a.IN - k * 8, v);
             uint32_t scale;
-            const uint32_t code = encode8(v, scale);
+            const uint32_t code = encode8<DT>(v, scale);
             reinterpret_cast<uint32_t *>(lds)[row * quarters + k] = code;
             if ((k & 3) == 0) lds[(size_t)rows * a.steps * 32 + row * a.steps * 2 + (k >> 2)] = (uint8_t)scale;
         }
@@ -466,10 +514,10 @@ int launch_mxfp4_dequantize(int dt, const DequantizeArgs &a, void *stream)
     });
 }
 
-// Few elements are quantised again in every workgroup rather than by a launch of their own: bf16 rows through 4096 x 4096 in us, so / by
-// two launches: 1 row 4.2 / 6.3, 4 rows 5.7 / 6.3, 8 rows 7.4 / 6.3; through 1280 x 1000 16 rows 5.5 / 5.6, 32 rows 7.3 / 5.9; through
-// 2048 -> 8192 8 rows 5.3 / 5.7, 16 rows 7.1 / 5.7.  A launch also costs 2.4 us to issue.
-bool fc_mxfp4_quantises(int B, int steps) { return B <= 32 && (long)B * steps <= 320; }
+// Few elements are quantised again in every workgroup rather than by a launch of their own.  bf16 rows through 4096 x 4096, us replayed from a
+// graph, so / by two launches: 1 row 4.2 / 6.1, 4 rows 5.3 / 6.1, 8 rows 6.7 / 6.2, 16 rows 9.7 / 6.2; through 1280 x 1000 16 rows 4.9 / 5.4,
+// 32 rows 6.5 / 5.5; through 2048 -> 8192 8 rows 5.0 / 5.6, 16 rows 6.4 / 5.6.  A launch takes 2.4 us to issue on top.
+bool fc_mxfp4_quantises(int B, int steps) { return B <= 32 && (long)B * steps <= 512; }
 
 // Which kernel, by how many pieces of 32 rows x 32 outputs there are (us for 2048 -> 8192; sixteen waves on each piece / eight on two / tiles
 // of 128 x 128: 256 pieces 6.9 / 7.6 / 9.3, 512 8.3 / 8.4 / 10.3, 1024 12.7 / 9.3 / 10.2, 2048 22.8 / 14.7 / 10.8; for 8192 -> 1024 512
