@@ -170,19 +170,23 @@ template <int S> __device__ __forceinline__ f32x16 mfma_mx(uint4 a, uint32_t sa,
 __device__ __forceinline__ int result_row(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
 
 // The activation with NaN passed on (rows whose blocks stand for NaN stay NaN).
-struct Activation {
-    float lo, hi, shift;
-    bool product; // hard-swish: v * clamp(v + 3) / 6
-};
-__device__ __forceinline__ Activation activation_of(int act)
+template <int ACT> __device__ __forceinline__ float activate(float v)
 {
-    const bool hs = act == NPAS_ACT_HARDSWISH;
-    return Activation{act == NPAS_ACT_NONE ? -INFINITY : 0.f, hs || act == NPAS_ACT_RELU6 ? 6.f : INFINITY, hs ? 3.f : 0.f, hs};
+    if constexpr (ACT == NPAS_ACT_RELU) return v < 0.f ? 0.f : v;
+    if constexpr (ACT == NPAS_ACT_RELU6) {
+        const float w = v < 0.f ? 0.f : v;
+        return w > 6.f ? 6.f : w;
+    }
+    if constexpr (ACT == NPAS_ACT_HARDSWISH) return v * __builtin_amdgcn_fmed3f(v + 3.f, 0.f, 6.f) * (1.f / 6.f);
+    return v;
 }
-__device__ __forceinline__ float activate(float v, const Activation &a)
+// Calls f with the launch's activation as a constant: chosen once, not per value.
+template <typename F> __device__ __forceinline__ void with_activation(int act, F &&f)
 {
-    const float w = v + a.shift, r = w < a.lo ? a.lo : w > a.hi ? a.hi : w;
-    return a.product ? v * r * (1.f / 6.f) : r;
+    if (act == NPAS_ACT_NONE) f(std::integral_constant<int, NPAS_ACT_NONE>{});
+    else if (act == NPAS_ACT_RELU) f(std::integral_constant<int, NPAS_ACT_RELU>{});
+    else if (act == NPAS_ACT_RELU6) f(std::integral_constant<int, NPAS_ACT_RELU6>{});
+    else f(std::integral_constant<int, NPAS_ACT_HARDSWISH>{});
 }
 // A lane's two biases of a group.
 __device__ __forceinline__ float2 group_bias(const FcMxArgs &a, int o)
@@ -276,14 +280,15 @@ template <int DT, int W, int J, bool FUSED> __global__ __launch_bounds__(64 * W)
         for (int i = 0; i < 16; ++i)
             if (result_row(i, lane) < rows) part_sum[((wave * J + j) * 32 + result_row(i, lane)) * 32 + r] = c[j][i];
     __syncthreads();
-    const Activation act = activation_of(a.act);
     const int waves = min(W, a.quads);
-    for (int u = threadIdx.x; u < rows * 32 * J; u += 64 * W) { // consecutive threads, consecutive outputs
-        const int row = u / (32 * J), k = u % (32 * J), j = J == 2 ? k & 1 : 0, n = J == 2 ? k >> 1 : k, o = group * 64 + 2 * n + (J == 2 ? j : part);
-        float v = 0.f;
-        for (int i = 0; i < waves; ++i) v += part_sum[((i * J + j) * 32 + row) * 32 + n];
-        if (o < a.OUT) st_act<DT>(a.y, (size_t)(tile * 32 + row) * a.OUT + o, activate(v + (a.bias ? a.bias[o] : 0.f), act));
-    }
+    with_activation(a.act, [&](auto act) __attribute__((always_inline)) {
+        for (int u = threadIdx.x; u < rows * 32 * J; u += 64 * W) { // consecutive threads, consecutive outputs
+            const int row = u / (32 * J), k = u % (32 * J), j = J == 2 ? k & 1 : 0, n = J == 2 ? k >> 1 : k, o = group * 64 + 2 * n + (J == 2 ? j : part);
+            float v = 0.f;
+            for (int i = 0; i < waves; ++i) v += part_sum[((i * J + j) * 32 + row) * 32 + n];
+            if (o < a.OUT) st_act<DT>(a.y, (size_t)(tile * 32 + row) * a.OUT + o, activate<decltype(act)::value>(v + (a.bias ? a.bias[o] : 0.f)));
+        }
+    });
 }
 
 // Many rows: a workgroup of 2 x 2 waves, each RR row tiles by RC weight images, walks the stages (two steps) together.  Operand images and
@@ -436,7 +441,6 @@ template <int DT, int RR, int RC> __global__ __launch_bounds__(256, 2) void fc_m
     }
 
     // Results through the wave's own part of LDS, so that rows leave in runs of 16 bytes a lane.
-    const Activation act = activation_of(a.act);
     const int o0 = (group0 + wc * (RC / 2)) * 64, r0 = (tile0 + wr * RR) * 32, n = lane & 31;
     float2 b[RC / 2];
 #pragma unroll
@@ -448,31 +452,35 @@ template <int DT, int RR, int RC> __global__ __launch_bounds__(256, 2) void fc_m
     __syncthreads();
 #pragma unroll
     for (int i0 = 0; i0 < RR; i0 += L::PASS) {
-        auto place = [&](auto plainc) __attribute__((always_inline)) {
-            constexpr bool PLAIN = decltype(plainc)::value;
+        with_activation(a.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < L::PASS; ++i)
 #pragma unroll
                 for (int k = 0; k < 16; ++k)
 #pragma unroll
                     for (int j = 0; j < RC / 2; ++j) {
-                        float v0 = c[i0 + i][2 * j][k] + b[j].x, v1 = c[i0 + i][2 * j + 1][k] + b[j].y;
-                        if (!PLAIN) v0 = activate(v0, act), v1 = activate(v1, act);
+                        const float v0 = activate<decltype(act)::value>(c[i0 + i][2 * j][k] + b[j].x);
+                        const float v1 = activate<decltype(act)::value>(c[i0 + i][2 * j + 1][k] + b[j].y);
                         uint8_t *p = own + (i * 32 + result_row(k, lane)) * L::PITCH + (j * 64 + 2 * n) * L::ESIZE;
                         if constexpr (DT == NPAS_F32) *reinterpret_cast<float2 *>(p) = make_float2(v0, v1);
                         else *reinterpret_cast<uint32_t *>(p) = pack2<DT>(v0, v1);
                     }
-        };
-        if (a.act == NPAS_ACT_NONE) place(std::true_type{}); // (the selects of an activation on every value: 81 us instead of 72, 4096 x 4096 -> 8192)
-        else place(std::false_type{});
+        });
         constexpr int LANES = RC * 32 / 8; // lanes of a row, 8 results each
 #pragma unroll 4
         for (int u = lane; u < L::PASS * 32 * LANES; u += 64) {
             const int r = u / LANES, o = u % LANES * 8, row = r0 + i0 * 32 + r, left = a.OUT - o0 - o;
             if (row >= a.B || left <= 0) continue;
-            float v[8];
-            load8<DT>(own + r * L::PITCH, o, 8, v);
-            store8<DT>(a.y, (size_t)row * a.OUT + o0 + o, left, v);
+            const size_t at = (size_t)row * a.OUT + o0 + o;
+            const uint8_t *p = own + r * L::PITCH + o * L::ESIZE;
+            if (left >= 8) store_vectors<8 * L::ESIZE>((uint8_t *)a.y + at * L::ESIZE, p);
+            else
+#pragma unroll
+                for (int k = 0; k < 7; ++k)
+                    if (k < left) {
+                        if constexpr (DT == NPAS_F32) reinterpret_cast<uint32_t *>(a.y)[at + k] = reinterpret_cast<const uint32_t *>(p)[k];
+                        else reinterpret_cast<uint16_t *>(a.y)[at + k] = reinterpret_cast<const uint16_t *>(p)[k];
+                    }
         }
     }
 }
