@@ -260,7 +260,7 @@ void npas_mxfp4_free(npas_mxfp4 *p)
 
 size_t npas_fc_mxfp4_workspace_bytes(const npas_mxfp4 *p, int B)
 {
-    if (!p || B <= 0 || fc_mxfp4_quantises(B, p->steps)) return 0;
+    if (!p || B <= 0 || fc_mxfp4_quantises(B, p->steps, p->groups)) return 0;
     return image_bytes(p, B) + (size_t)row_tiles(B) * p->quads * 256;
 }
 
@@ -295,7 +295,7 @@ int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void
     }
     FcMxArgs a{x_dev, x_stride, nullptr, nullptr, p->images, p->image_scales, (const float *)bias_dev, y_dev, B, p->IN, p->OUT, p->blocks, p->steps,
                p->quads, p->groups, row_tiles(B), act};
-    if (!fc_mxfp4_quantises(B, p->steps)) {
+    if (!fc_mxfp4_quantises(B, p->steps, p->groups)) {
         uint8_t *images = (uint8_t *)workspace_dev, *words = images + image_bytes(p, B);
         QuantizeArgs q{x_dev, images, words, x_stride, B, p->IN, p->blocks, p->steps, p->quads, WideDiv{}, 0};
         if (int rc = launch_mxfp4_quantize_images(p->dtype, q, hip_stream)) return rc;

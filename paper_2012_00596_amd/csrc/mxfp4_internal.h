@@ -59,7 +59,7 @@ struct FcMxArgs {
 int launch_mxfp4_quantize(int dt, const QuantizeArgs &a, void *stream);
 int launch_mxfp4_quantize_images(int dt, const QuantizeArgs &a, void *stream);
 int launch_mxfp4_dequantize(int dt, const DequantizeArgs &a, void *stream);
-bool fc_mxfp4_quantises(int B, int steps); // a launch on that many rows takes them as they are
+bool fc_mxfp4_quantises(int B, int steps, int groups); // the product's launch takes its rows as they are
 int launch_fc_mxfp4(int dt, const FcMxArgs &a, void *stream);
 
 } // namespace npas

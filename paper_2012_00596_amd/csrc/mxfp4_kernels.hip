@@ -522,10 +522,17 @@ int launch_mxfp4_dequantize(int dt, const DequantizeArgs &a, void *stream)
     });
 }
 
-// Few elements are quantised again in every workgroup rather than by a launch of their own.  bf16 rows through 4096 x 4096, us replayed from a
-// graph, so / by two launches: 1 row 4.2 / 6.1, 4 rows 5.3 / 6.1, 8 rows 6.7 / 6.2, 16 rows 9.7 / 6.2; through 1280 x 1000 16 rows 4.9 / 5.4,
-// 32 rows 6.5 / 5.5; through 2048 -> 8192 8 rows 5.0 / 5.6, 16 rows 6.4 / 5.6.  A launch takes 2.4 us to issue on top.
-bool fc_mxfp4_quantises(int B, int steps) { return B <= 32 && (long)B * steps <= 512; }
+// Pieces of 32 rows x 32 outputs; with one workgroup each on 256 compute units they take (pieces + 255) / 256 rounds.
+static long pieces_of(int B, int groups) { return (long)((B + 31L) / 32) * groups * 2; }
+
+// Few elements are quantised again in every workgroup rather than by a launch of their own: what counts is how often a compute unit does it.
+// bf16, us replayed from a graph, so / by two launches: 4096 x 4096 1 row 4.2 / 6.1, 4 rows 5.3 / 6.1, 8 rows 6.7 / 6.2, 16 rows 9.7 / 6.2;
+// 1280 x 1000 16 rows 4.9 / 5.4, 32 rows 6.5 / 5.5; 2048 -> 16384 4 rows 6.0 / 6.8, 8 rows 7.1 / 6.9; 4096 -> 32000 2 rows 15.0 / 15.1, 4 rows
+// 17.8 / 15.2; 512 -> 512 512 rows 5.4 / 5.5.  A launch takes 1.6 to 2.4 us to issue on top.
+bool fc_mxfp4_quantises(int B, int steps, int groups)
+{
+    return (long)(B < 32 ? B : 32) * steps * ((pieces_of(B, groups) + 255) / 256) <= 512;
+}
 
 // Which kernel, by how many pieces of 32 rows x 32 outputs there are (us for 2048 -> 8192; sixteen waves on each piece / eight on two / tiles
 // of 128 x 128: 256 pieces 6.9 / 7.6 / 9.3, 512 8.3 / 8.4 / 10.3, 1024 12.7 / 9.3 / 10.2, 2048 22.8 / 14.7 / 10.8; for 8192 -> 1024 512
@@ -547,9 +554,10 @@ int launch_fc_mxfp4(int dt, const FcMxArgs &a, void *stream)
         constexpr bool FUSED = decltype(fc)::value;
         hipLaunchKernelGGL((fc_mxfp4_split_kernel<DT, W, J, FUSED>), dim3((unsigned)(a.tiles * a.groups * (2 / J))), dim3(64 * W), 0, (hipStream_t)stream, a);
     };
-    const long pieces = (long)a.tiles * a.groups * 2, large = (long)((a.tiles + 7) / 8) * ((a.groups + 1) / 2);
+    const long pieces = pieces_of(a.B, a.groups), large = (long)((a.tiles + 7) / 8) * ((a.groups + 1) / 2);
     return with_dtype(dt, "4-bit product", [&](auto dtc) {
-        if (!a.x_images) split(dtc, integral_constant<int, 16>{}, integral_constant<int, 1>{}, std::true_type{});
+        if (!a.x_images && pieces <= 256) split(dtc, integral_constant<int, 16>{}, integral_constant<int, 1>{}, std::true_type{});
+        else if (!a.x_images) split(dtc, integral_constant<int, 8>{}, integral_constant<int, 2>{}, std::true_type{});
         else if (pieces <= 256) split(dtc, integral_constant<int, 16>{}, integral_constant<int, 1>{}, std::false_type{});
         else if (pieces <= 1024) split(dtc, integral_constant<int, 8>{}, integral_constant<int, 2>{}, std::false_type{});
         else if (large < 512) tiled(dtc, integral_constant<int, 2>{});

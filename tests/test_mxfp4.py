@@ -145,6 +145,16 @@ def test_refusals():
     assert L.npas_fc_mxfp4_workspace_bytes(None, 3) == 0
 
 
+def test_workspace_is_checked():
+    """Many rows are quantised into the workspace: too little, misaligned or none is refused before anything is launched."""
+    L, p = npas.lib(), npas.pack_fc_mxfp4(np.ones((64, 4096), np.float32), npas.F32)
+    need = p.workspace_bytes(64)
+    assert need >= 64 * 4096 // 2
+    for ws, size in ((None, need), (264, need), (256, need - 1), (256, 0)):
+        assert L.npas_fc_mxfp4(p.handle, 64, 4096, 128, 64, None, 0, ws, size, None) == npas.E_WORKSPACE
+    assert p.workspace_bytes(1) == 0 and p.workspace_bytes(0) == 0
+
+
 def _dev(torch, store, dt):
     a = np.ascontiguousarray(store)
     return torch.from_numpy(a).cuda() if dt == npas.F32 else torch.from_numpy(a.view(np.int16)).cuda()
@@ -245,7 +255,7 @@ def _product(torch, seed, B, IN, OUT, dt, bias=True, act=npas.ACT_NONE, x=None):
     assert not bad[~nan].any(), f"{bad[~nan].sum()} of {bad.size} off, worst {np.abs(got - want)[~nan].max()}"
 
 
-FC = [(1, 1, 1), (1, 32, 64), (2, 33, 5), (3, 128, 65), (16, 127, 63), (17, 640, 130), (1, 4096, 512), (5, 1000, 333), (33, 1280, 1000),
+FC = [(2, 100, 9000), (9, 64, 20000), (70, 200, 513), (200, 90, 400), (1, 1, 1), (1, 32, 64), (2, 33, 5), (3, 128, 65), (16, 127, 63), (17, 640, 130), (1, 4096, 512), (5, 1000, 333), (33, 1280, 1000),
       (64, 513, 256), (100, 2050, 96), (200, 384, 700), (257, 1024, 513), (300, 100, 1030), (520, 4224, 264)]
 
 
