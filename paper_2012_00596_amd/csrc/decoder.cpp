@@ -37,21 +37,20 @@ int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
 }
 
 // How a launch cuts the tokens.  A pair is a sequence's key head (with up to 16 of its query heads): one workgroup a pair and cut.
-//   - Up to kSingle elements of keys a pair one cut: the joining launch takes longer to issue (2.4 us) than it saves (from call to call: 16 pairs
-//     of 777 tokens, head_dim 64, 8.7 us in one cut, 9.8 in seven; replayed from a graph 9.0 and 7.2; of 1024 tokens, head_dim 128, 14.3
-//     and 8.0 in a graph).
-//   - In that case eight waves where every workgroup has a compute unit to itself (8.7 us, with four waves 9.4); otherwise four, two
-//     workgroups on a compute unit (512 pairs of up to 8192 tokens: 227 us, with eight 244).
-//   - Longer ones in 512 workgroups (the two on each compute unit: 131071 tokens of 4 pairs 55 us, in 2048 workgroups 64), at least 128
-//     tokens each (4096 tokens of 8 pairs 8.7 us, 256 each 10.3); and at most 4096, so that a long sequence in a ragged batch does not run
-//     alone at the end (512 pairs of up to 8192: 229 us).
+//   - Up to kSingle elements of keys a pair one cut: the joining launch takes longer to issue (1.6 to 2.4 us) than it saves (from call to call: 16
+//     pairs of 777 tokens, head_dim 64, 8.0 us in one cut, 9.3 in seven; replayed from a graph 8.2 and 7.1; 128 pairs of 300 tokens,
+//     head_dim 128, in a graph 7.2 and 9.9).
+//   - In that case eight waves where every workgroup has a compute unit to itself; otherwise four, two or three workgroups on a compute unit.
+//   - Longer ones in 512 workgroups (131071 tokens of 4 pairs 54 us, in 1024 workgroups 56), at least 128 tokens each (4096 tokens of 8 pairs
+//     8.6 us, 256 each 10.3); and at most 2048, so that a long sequence in a ragged batch does not run alone at the end (512 pairs of
+//     up to 8192 tokens 227 us, in one cut 225).
 struct Cuts {
     int chunk, splits, waves;
     size_t stat_at, bytes; // (maximum, sum) pairs lie behind the sums; bytes: enough for any window
 };
 Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
 {
-    constexpr long kWorkgroups = 512, kLeast = 128, kMost = 4096, kSingle = 65536;
+    constexpr long kWorkgroups = 512, kLeast = 128, kMost = 2048, kSingle = 65536;
     const long room = (long)c.table_stride * c.page_size, longest = max_length < room ? max_length : room;
     const long n = window > 0 && window < longest ? window : longest;
     const long group = heads / c.kv_heads, pairs = (long)c.sequences * c.kv_heads * ((group + 15) / 16);

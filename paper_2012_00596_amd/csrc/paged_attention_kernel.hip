@@ -29,7 +29,7 @@ __device__ __forceinline__ void token_range(const AttentionArgs &a, int s, int &
 // instruction: row r of tile j is element VW r + j.  Nothing passes through LDS but the cache rows of the tokens.
 // The weights go in as two 16-bit numbers, high part and remainder: the matrix cores have time for both (the kernel waits for memory),
 // and the result is then as good as with 32-bit weights.
-// Memory bound: 64 sequences of up to 8192 tokens, 8 key heads of 128, 1.07 GB in 229 us (4.7 TB/s); one of 131071, 4 key heads, 55 us
+// Memory bound: 64 sequences of up to 8192 tokens, 8 key heads of 128, 1.07 GB in 227 us (4.7 TB/s); one of 131071, 4 key heads, 55 us
 // (4.9 TB/s).  Few short sequences are a chain of latencies: a launch, the length, the pages, then 1.1-1.8 us a round of tiles.
 template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * NW, NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
 {
