@@ -40,7 +40,8 @@ int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
 //   - Up to kSingle elements of keys a pair one cut: the joining launch takes longer to issue (1.6 to 2.4 us) than it saves (from call to call: 16
 //     pairs of 777 tokens, head_dim 64, 8.0 us in one cut, 9.3 in seven; replayed from a graph 8.2 and 7.1; 128 pairs of 300 tokens,
 //     head_dim 128, in a graph 7.2 and 9.9).
-//   - In that case eight waves where every workgroup has a compute unit to itself; otherwise four, two or three workgroups on a compute unit.
+//   - In that case eight waves where every workgroup has a compute unit to itself (16 pairs of 777 tokens 8.7 us, with four 9.4); otherwise four,
+//     two or three workgroups on a compute unit (512 pairs of up to 8192 tokens in one cut 227 us, with eight waves 244).
 //   - Longer ones in 512 workgroups (131071 tokens of 4 pairs 54 us, in 1024 workgroups 56), at least 128 tokens each (4096 tokens of 8 pairs
 //     8.6 us, 256 each 10.3); and at most 2048, so that a long sequence in a ragged batch does not run alone at the end (512 pairs of
 //     up to 8192 tokens 227 us, in one cut 225).
