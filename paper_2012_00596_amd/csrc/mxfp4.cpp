@@ -4,7 +4,7 @@
 #include <algorithm>
 #include <cstring>
 #include <memory>
-#include <new>
+#include <exception>
 #include <thread>
 
 #include "mxfp4_internal.h"
@@ -223,8 +223,8 @@ int npas_pack_fc_mxfp4(const void *w_host, int OUT, int IN, npas_dtype dt, void 
             if (int rc = upload(p.get(), blob, dev, hip_stream)) return rc;
         *out = p.release();
         return NPAS_OK;
-    } catch (const std::bad_alloc &) {
-        set_error("out of host memory packing %d x %d weights", OUT, IN);
+    } catch (const std::exception &e) { // no host memory for so large a layer
+        set_error("packing %d x %d weights: %s", OUT, IN, e.what());
         return NPAS_E_SHAPE;
     }
 }
