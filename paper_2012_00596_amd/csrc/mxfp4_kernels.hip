@@ -498,9 +498,15 @@ template <typename F> static int with_dtype(int dt, const char *what, F &&f)
     return NPAS_E_HIP;
 }
 
+// 128 blocks a workgroup, by slabs.  (In 64 bits: rows and a slab together pass 2^31.)
+static dim3 slab_grid(int rows, int slab, int blocks)
+{
+    return dim3((unsigned)(((long)slab * blocks + 127) / 128), (unsigned)(((long)rows + slab - 1) / slab));
+}
+
 int launch_mxfp4_quantize(int dt, const QuantizeArgs &a, void *stream)
 {
-    const dim3 grid((unsigned)(((long)a.slab * a.blocks + 127) / 128), (unsigned)((a.rows + a.slab - 1) / a.slab));
+    const dim3 grid = slab_grid(a.rows, a.slab, a.blocks);
     return with_dtype(dt, "4-bit quantisation", [&](auto dtc) {
         hipLaunchKernelGGL((mxfp4_quantize_kernel<decltype(dtc)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
     });
@@ -508,7 +514,7 @@ int launch_mxfp4_quantize(int dt, const QuantizeArgs &a, void *stream)
 
 int launch_mxfp4_quantize_images(int dt, const QuantizeArgs &a, void *stream)
 {
-    const dim3 grid((unsigned)((a.rows + 31) / 32 * a.steps));
+    const dim3 grid((unsigned)((a.rows + 31L) / 32 * a.steps));
     return with_dtype(dt, "4-bit quantisation", [&](auto dtc) {
         hipLaunchKernelGGL((mxfp4_quantize_images_kernel<decltype(dtc)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
     });
@@ -516,7 +522,7 @@ int launch_mxfp4_quantize_images(int dt, const QuantizeArgs &a, void *stream)
 
 int launch_mxfp4_dequantize(int dt, const DequantizeArgs &a, void *stream)
 {
-    const dim3 grid((unsigned)(((long)a.slab * a.blocks + 127) / 128), (unsigned)((a.rows + a.slab - 1) / a.slab));
+    const dim3 grid = slab_grid(a.rows, a.slab, a.blocks);
     return with_dtype(dt, "4-bit dequantisation", [&](auto dtc) {
         hipLaunchKernelGGL((mxfp4_dequantize_kernel<decltype(dtc)::value>), grid, dim3(256), 0, (hipStream_t)stream, a);
     });

@@ -219,6 +219,28 @@ def test_quantize_rows_of_a_wider_tensor_at_odd_alignment(torch):
     np.testing.assert_array_equal(c.cpu().numpy(), codes)
 
 
+@gpu
+def test_quantize_more_rows_than_a_slab_and_back(torch):
+    """More than 2^30 blocks: several slabs of rows, and a number of rows that passes 2^31 with a slab's added."""
+    dt, part, M, K = npas.BF16, 4096, 2 ** 30 + 8192, 1
+    store, exact = (v.reshape(part, K) for v in sample(9, (K, part), dt))
+    codes, scales = reference(exact)
+    rows = _dev(torch, store, dt)
+    x = rows.repeat(M // part, 1)
+    c, s = torch.empty((M, 16), dtype=torch.uint8, device="cuda"), torch.empty((M, 1), dtype=torch.uint8, device="cuda")
+    npas.mxfp4_quantize(x, c, s, M, K, dt)
+    want = torch.from_numpy(codes).cuda()
+    for i in range(0, M, 2 ** 26):
+        got = c[i:i + 2 ** 26].view(-1, part, 16)
+        assert bool((got == want).all()), i
+    assert bool((s.view(-1, part, 1) == torch.from_numpy(scales).cuda()).all())
+    y = torch.empty_like(x)
+    npas.mxfp4_dequantize(c, s, y, M, K, dt)
+    back = torch.empty_like(rows)
+    npas.mxfp4_dequantize(c, s, back, part, K, dt)
+    assert bool((y.view(torch.int16).view(-1, part, K) == back.view(torch.int16)).all())
+
+
 def _act(v, act):
     if act == npas.ACT_RELU:
         return np.maximum(v, 0)
