@@ -252,7 +252,7 @@ template <int DT, int LANES, int THREADS> __global__ __launch_bounds__(THREADS) 
     const size_t row = blockIdx.x;
     int first, count;
     token_range(a, s, first, count);
-    const int cuts = (count + a.chunk - 1) / a.chunk;
+    const int cuts = (int)(((uint32_t)count + (uint32_t)a.chunk - 1) / (uint32_t)a.chunk); // (count and chunk together pass 2^31)
     const float2 x = tid < cuts ? a.part_stat[row * a.splits + tid] : make_float2(-INFINITY, 0.f); // no more cuts than threads
     float m = x.x;
 #pragma unroll

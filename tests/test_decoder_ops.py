@@ -473,6 +473,27 @@ def test_append_and_attention_beyond_32_bit_offsets(torch):
 
 
 @gpu
+def test_attention_of_the_longest_length(torch):
+    """2^31 - 1 tokens: one page stands in every place of the table, so that each of its rows counts 2^16 times, the last once less."""
+    D, page, places, dt = 8, 2 ** 15, 2 ** 16, npas.F16
+    k, v = _rand(torch, 90, (1, 1, page, D), dt), (_rand(torch, 91, (1, 1, page, D), dt) + 1).half()
+    q, n = _rand(torch, 92, (1, 1, D), dt), 2 ** 31 - 1
+    cache = npas.KvCache(k.cuda(), v.cuda(), torch.zeros((1, places), dtype=torch.int32, device="cuda"), dt)
+    need = npas.paged_attention_workspace_bytes(cache, 1, n)
+    y, lse = torch.empty((1, 1, D), dtype=torch.float16, device="cuda"), torch.empty((1, 1), device="cuda")
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    npas.paged_attention(cache, q.cuda(), y, 1, torch.tensor([n], dtype=torch.int32).cuda(), n, 0.25, lse=lse, workspace=ws, workspace_bytes=need)
+    times = torch.full((page,), float(places), dtype=torch.float64)
+    times[-1] -= 1
+    p = times * torch.exp(0.25 * k[0, 0].double() @ q[0, 0].double())
+    want = p @ v[0, 0].double() / p.sum()
+    # a lane adds up to 2^18 weights in turn, a result register 2^16 products: each addition 2^-24 of what is there; then one rounding
+    bound = (2 ** 18 + 2 ** 16) * 2.0 ** -24 * (p @ v[0, 0].double().abs() / p.sum()) + 2.0 ** -11 * want.abs()
+    assert bool(((y.cpu()[0, 0].double() - want).abs() <= bound).all()), (y, want)
+    assert abs(float(lse) - float(torch.log(p.sum()))) <= 2 ** 18 * 2.0 ** -24 + 2.0 ** -20 * 24
+
+
+@gpu
 def test_step_on_a_side_stream_and_in_a_graph(torch):
     """Append, attention and norm on a stream of the caller's, captured once and replayed as positions and lengths move on; every replay
     equals the eager calls."""
