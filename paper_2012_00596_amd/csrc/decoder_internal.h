@@ -56,6 +56,8 @@ int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream);
 int launch_kv_append(int dt, const AppendArgs &a, void *stream);
 int launch_paged_attention(int dt, const AttentionArgs &a, void *stream);
 
+// Refuses what is more than a launch can have, 2^32 - 1 threads.
+int check_grid(const char *what, uint64_t workgroups, unsigned threads);
 // Reports the launch error that is pending, if any.
 int launched(const char *what);
 

@@ -147,19 +147,28 @@ int launched(const char *what)
     return NPAS_E_HIP;
 }
 
+int check_grid(const char *what, uint64_t workgroups, unsigned threads)
+{
+    if (workgroups * threads <= 0xffffffffu) return NPAS_OK;
+    set_error("%s: %llu workgroups of %u threads are more than a launch can have", what, (unsigned long long)workgroups, threads);
+    return NPAS_E_SHAPE;
+}
+
 int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream)
 {
     hipStream_t st = (hipStream_t)stream;
+    const unsigned threads = a.D <= 2048 ? 256 : a.D <= 4096 ? 512 : 1024, workgroups = a.D <= 1024 ? ((unsigned)a.T + 3) / 4 : (unsigned)a.T;
+    if (int rc = check_grid("gated residual norm", workgroups, threads)) return rc;
     with_dtype(dt, [&](auto dtc) {
         constexpr int DT = decltype(dtc)::value;
-        const dim3 rows((unsigned)a.T), quads(((unsigned)a.T + 3) / 4);
-        if (a.D <= 512) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 1>), quads, dim3(256), 0, st, a);
-        else if (a.D <= 1024) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 1>), quads, dim3(256), 0, st, a);
-        else if (a.D <= 2048) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 4>), rows, dim3(256), 0, st, a);
-        else if (a.D <= 4096) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 8>), rows, dim3(512), 0, st, a);
-        else if (a.D <= 8192) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 16>), rows, dim3(1024), 0, st, a);
-        else if (a.D <= 16384) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 16>), rows, dim3(1024), 0, st, a);
-        else hipLaunchKernelGGL((gated_residual_norm_long_kernel<DT>), rows, dim3(1024), 0, st, a);
+        const dim3 grid(workgroups), block(threads);
+        if (a.D <= 512) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 1>), grid, block, 0, st, a);
+        else if (a.D <= 1024) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 1>), grid, block, 0, st, a);
+        else if (a.D <= 2048) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 4>), grid, block, 0, st, a);
+        else if (a.D <= 4096) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 8>), grid, block, 0, st, a);
+        else if (a.D <= 8192) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 1, 16>), grid, block, 0, st, a);
+        else if (a.D <= 16384) hipLaunchKernelGGL((gated_residual_norm_kernel<DT, 2, 16>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((gated_residual_norm_long_kernel<DT>), grid, block, 0, st, a);
     });
     return launched("gated residual norm");
 }
@@ -226,12 +235,13 @@ template <int DT, bool PAIRS, bool WHOLE> __global__ __launch_bounds__(256) void
 int launch_kv_append(int dt, const AppendArgs &a, void *stream)
 {
     hipStream_t st = (hipStream_t)stream;
+    // as many waves as one pass over the token's units fills, up to four (8191 tokens of 1 + 1 + 1 heads of 64: 5.7 us, always four 10.0)
+    const int head_units = ((a.pairs ? a.rot_dim : a.rot_dim / 2) + 7) / 8 + (a.c.head_dim - a.rot_dim + 7) / 8;
+    const long units = (long)((a.q ? a.heads : 0) + a.c.kv_heads) * head_units + (long)a.c.kv_heads * (a.c.head_dim / 8);
+    const dim3 grid((unsigned)a.T), block(units <= 64 ? 64 : units <= 128 ? 128 : units <= 192 ? 192 : 256);
+    if (int rc = check_grid("cache append", grid.x, block.x)) return rc;
     auto pick = [&](auto dtc) {
         constexpr int DT = decltype(dtc)::value;
-        // as many waves as one pass over the token's units fills, up to four (8191 tokens of 1 + 1 + 1 heads of 64: 5.7 us, always four 10.0)
-        const int head_units = ((a.pairs ? a.rot_dim : a.rot_dim / 2) + 7) / 8 + (a.c.head_dim - a.rot_dim + 7) / 8;
-        const long units = (long)((a.q ? a.heads : 0) + a.c.kv_heads) * head_units + (long)a.c.kv_heads * (a.c.head_dim / 8);
-        const dim3 grid((unsigned)a.T), block(units <= 64 ? 64 : units <= 128 ? 128 : units <= 192 ? 192 : 256);
         const bool whole = a.rot_dim % (a.pairs ? 8 : 16) == 0;
         if (a.pairs && whole) hipLaunchKernelGGL((kv_append_kernel<DT, true, true>), grid, block, 0, st, a);
         else if (a.pairs) hipLaunchKernelGGL((kv_append_kernel<DT, true, false>), grid, block, 0, st, a);

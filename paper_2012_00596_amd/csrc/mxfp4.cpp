@@ -271,8 +271,8 @@ int npas_fc_mxfp4(const npas_mxfp4 *p, const void *x_dev, int64_t x_stride, void
         set_error("NULL argument (handle=%p x_dev=%p y_dev=%p)", (const void *)p, x_dev, y_dev);
         return NPAS_E_NULL;
     }
-    if (B <= 0 || x_stride < p->IN || x_stride > (int64_t)1 << 40 || (double)row_tiles(B) * p->groups > 2147483647.0 ||
-        (double)row_tiles(B) * p->steps > 2147483647.0) {
+    if (B <= 0 || x_stride < p->IN || x_stride > (int64_t)1 << 40 || (row_tiles(B) / 8 + 1.0) * (p->groups / 2 + 1.0) * 256 > 4294967295.0 ||
+        (double)row_tiles(B) * p->steps * 256 > 4294967295.0) { // (threads of its launches)
         set_error("bad shape B=%d, row stride %lld of %d elements", B, (long long)x_stride, p->IN);
         return NPAS_E_SHAPE;
     }

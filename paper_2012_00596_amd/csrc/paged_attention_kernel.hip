@@ -295,6 +295,10 @@ int launch_paged_attention(int dt, const AttentionArgs &a, void *stream)
     hipStream_t st = (hipStream_t)stream;
     const int group = a.heads / a.c.kv_heads;
     const dim3 grid((unsigned)((size_t)a.c.sequences * a.splits * ((group + 15) / 16) * a.c.kv_heads));
+    const unsigned joiners = a.splits <= 16 ? 64 : kMaxSplits; // threads of a workgroup that joins
+    if (int rc = check_grid("paged attention", grid.x, 64 * a.waves)) return rc;
+    if (a.splits > 1)
+        if (int rc = check_grid("paged attention", (uint64_t)a.c.sequences * a.heads, joiners)) return rc;
     auto pick = [&](auto dtc) {
         constexpr int DT = decltype(dtc)::value;
         auto run = [&](auto ncc) {
@@ -316,8 +320,8 @@ int launch_paged_attention(int dt, const AttentionArgs &a, void *stream)
         auto join = [&](auto lanesc) {
             constexpr int LANES = decltype(lanesc)::value;
             const dim3 rows((unsigned)(a.c.sequences * a.heads));
-            if (a.splits <= 16) hipLaunchKernelGGL((paged_attention_join_kernel<DT, LANES, 64>), rows, dim3(64), 0, st, a);
-            else hipLaunchKernelGGL((paged_attention_join_kernel<DT, LANES, kMaxSplits>), rows, dim3(kMaxSplits), 0, st, a);
+            if (joiners == 64) hipLaunchKernelGGL((paged_attention_join_kernel<DT, LANES, 64>), rows, dim3(joiners), 0, st, a);
+            else hipLaunchKernelGGL((paged_attention_join_kernel<DT, LANES, kMaxSplits>), rows, dim3(joiners), 0, st, a);
         };
         if (a.c.head_dim <= 64) join(std::integral_constant<int, 16>{});
         else if (a.c.head_dim <= 128) join(std::integral_constant<int, 32>{});

@@ -603,6 +603,19 @@ def test_norm_refuses():
         assert L.npas_gated_residual_norm(*args) == code, (at, value)
 
 
+def test_more_threads_than_a_launch_can_have_are_refused():
+    L, big = npas.lib(), 2 ** 31 - 1
+    for D in (8, 1024, 1280, 4096, 8192, 20000):
+        assert L.npas_gated_residual_norm(64, 64, None, 0, None, 64, 1.0, 1e-6, 128, 256, big, D, npas.BF16, None) == npas.E_SHAPE, D
+        assert b"threads" in L.npas_last_error()
+    assert L.npas_kv_append(_desc(), None, 0, 64, 128, 64, 128, None, big, 2, None, 64, None, 0, 0, 0, None) == npas.E_SHAPE
+    assert b"threads" in L.npas_last_error()
+    many = _desc(sequences=2 ** 22, table_stride=2 ** 12)           # 2^23 pairs of 2^16 tokens, 32 cuts each
+    need = L.npas_paged_attention_workspace_bytes(many, 4, 2 ** 16)
+    assert L.npas_paged_attention(many, 64, 256, 64, None, 4, 64, 2 ** 16, 0, 1.0, 4096, need, None) == npas.E_SHAPE
+    assert b"threads" in L.npas_last_error()
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     import torch
     k = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)

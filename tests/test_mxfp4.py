@@ -145,6 +145,15 @@ def test_refusals():
     assert L.npas_fc_mxfp4_workspace_bytes(None, 3) == 0
 
 
+def test_more_threads_than_a_launch_can_have_are_refused():
+    L = npas.lib()
+    for shape, B in (((4, 1024), 2 ** 31 - 1), ((2 ** 17, 8), 2 ** 30)):  # of the activations' quantisation, of the product
+        p = npas.pack_fc_mxfp4(np.ones(shape, np.float32), npas.F32)
+        args = p.handle, 64, shape[1], 128, B, None, 0, 256, 2 ** 60, None
+        assert L.npas_fc_mxfp4(*args) == npas.E_SHAPE
+        assert b"bad shape" in L.npas_last_error()
+
+
 def test_workspace_is_checked():
     """Many rows are quantised into the workspace: too little, misaligned or none is refused before anything is launched."""
     L, p = npas.lib(), npas.pack_fc_mxfp4(np.ones((64, 4096), np.float32), npas.F32)
