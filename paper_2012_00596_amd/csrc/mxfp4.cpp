@@ -122,6 +122,7 @@ int upload(npas_mxfp4 *p, const std::vector<uint8_t> &blob, int dev, void *hip_s
     void *ptr = nullptr;
     hipError_t e = hipMalloc(&ptr, blob.size());
     if (e != hipSuccess) {
+        (void)hipGetLastError(); // reported here, not by the next launch
         set_error("hipMalloc(%zu) failed: %s", blob.size(), hipGetErrorString(e));
         return NPAS_E_HIP;
     }
@@ -130,6 +131,7 @@ int upload(npas_mxfp4 *p, const std::vector<uint8_t> &blob, int dev, void *hip_s
     if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)hip_stream);
     if (e != hipSuccess) {
         (void)hipFree(ptr);
+        (void)hipGetLastError();
         set_error("hipMemcpy to device failed: %s", hipGetErrorString(e));
         return NPAS_E_HIP;
     }
