@@ -27,14 +27,16 @@ __device__ __forceinline__ void token_range(const AttentionArgs &a, int s, int &
 // counted so that quarter q holds tokens 4 q .. 4 q + 3 of both 16-token tiles; its row operand, values by element, comes from rows of
 // the cache read whole (lane 16 q + r: VW consecutive elements of those eight tokens) and turned round in registers, two elements an
 // instruction: row r of tile j is element VW r + j.  Nothing passes through LDS but the cache rows of the tokens.
-// The weights go in as two 16-bit numbers, high part and remainder: the matrix cores have time for both (the kernel waits for memory),
-// and the result is then as good as with 32-bit weights.
+// The weights go in as 16-bit numbers and what these leave over: three bf16 hold all 24 bits of a weight, two fp16 hold 22 and a sign, and the
+// matrix cores have time for them (the kernel waits for memory).  fp16 reaches down to 2^-24 only, so there the largest weight is 2^15: what
+// is below 2^-39 of it is lost.
 // Memory bound: 64 sequences of up to 8192 tokens, 8 key heads of 128, 1.07 GB in 227 us (4.7 TB/s); one of 131071, 4 key heads, 55 us
 // (4.9 TB/s).  Few short sequences are a chain of latencies: a launch, the length, the pages, then 1.1-1.8 us a round of tiles.
 template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * NW, NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
 {
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
-    constexpr int PITCH = DP + 4;
+    constexpr int PITCH = DP + 4, PARTS = DT == NPAS_BF16 ? 3 : 2;
+    constexpr float TOP = DT == NPAS_BF16 ? 1.f : 32768.f; // the largest weight
     __shared__ __align__(16) uint32_t rows[kRows];
     __shared__ float sm[NW][16], sl[NW][16];
     __shared__ __align__(16) float so[NW * 16 * PITCH];
@@ -141,15 +143,18 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
             for (int j = 0; j < VW; ++j) o[j] *= c;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        uint32_t hi[4], lo[4];
+        uint32_t part[PARTS][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float p0 = __builtin_amdgcn_exp2f(x[2 * i] - base), p1 = __builtin_amdgcn_exp2f(x[2 * i + 1] - base);
+            float p0 = __builtin_amdgcn_exp2f(x[2 * i] - base) * TOP, p1 = __builtin_amdgcn_exp2f(x[2 * i + 1] - base) * TOP;
             l += p0 + p1;
-            hi[i] = pack2<DT>(p0, p1);
-            lo[i] = pack2<DT>(p0 - from_storage<DT>((uint16_t)hi[i]), p1 - from_storage<DT>((uint16_t)(hi[i] >> 16)));
+#pragma unroll
+            for (int n = 0; n < PARTS; ++n) {
+                part[n][i] = pack2<DT>(p0, p1);
+                p0 -= from_storage<DT>((uint16_t)part[n][i]);
+                p1 -= from_storage<DT>((uint16_t)(part[n][i] >> 16));
+            }
         }
-        const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         if (__any(absent != 0)) // an absent token's row is another's: it must not bring in an infinity or a NaN
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -164,10 +169,12 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
                 odd[i] = __builtin_amdgcn_perm(vt[2 * i + 1][w], vt[2 * i][w], 0x07060302u);
             }
             const uint4 ve = make_uint4(even[0], even[1], even[2], even[3]), vo = make_uint4(odd[0], odd[1], odd[2], odd[3]);
-            o[2 * w] = mfma16<DT>(ve, ph, o[2 * w]);
-            o[2 * w + 1] = mfma16<DT>(vo, ph, o[2 * w + 1]);
-            o[2 * w] = mfma16<DT>(ve, pl, o[2 * w]);
-            o[2 * w + 1] = mfma16<DT>(vo, pl, o[2 * w + 1]);
+#pragma unroll
+            for (int n = 0; n < PARTS; ++n) {
+                const uint4 p = make_uint4(part[n][0], part[n][1], part[n][2], part[n][3]);
+                o[2 * w] = mfma16<DT>(ve, p, o[2 * w]);
+                o[2 * w + 1] = mfma16<DT>(vo, p, o[2 * w + 1]);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
         if (MORE) load_values(next);
@@ -220,7 +227,7 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float c = sm[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][n] - top);
+            const float c = sm[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][n] - top) * (1.f / TOP);
             const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + n) * PITCH + d);
             sum += c * sl[w][n];
             y.x += c * v.x, y.y += c * v.y, y.z += c * v.z, y.w += c * v.w;

@@ -1,0 +1,169 @@
+"""Attention of one token where a weight's last bits, or a single token, decide: scores are exact (queries are zero or one-hot), so that
+the weights' own error is all there is beside the rounding of the result.
+
+Bounds, with w = sum p |v| / sum p the magnitude of a result's terms and u = 2^-24 the roundoff of fp32.  An exponent log2(e) x with |x| <= 1 is off by
+2.44 u (the constant's and the product's rounding) and u more once the largest is taken away, 2.4 u of the weight; the exponential by
+2 u.  The products of 16-bit numbers are exact; where three tokens count, their sums are rounded at most three times at w's magnitude,
+each by 2 u.  In all 10.4 u w, taken as 12.  Tokens in three cuts: twice a factor that brings a part to the largest maximum (4 u with its product) and
+two additions, 24 in all."""
+import numpy as np
+import pytest
+
+import paper_2012_00596_amd as npas
+
+U = {npas.BF16: 2.0 ** -8, npas.F16: 2.0 ** -11}
+TINY = {npas.BF16: 2.0 ** -133, npas.F16: 2.0 ** -25}
+u = 2.0 ** -24
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    return t
+
+
+def _td(torch, dt):
+    return torch.bfloat16 if dt == npas.BF16 else torch.float16
+
+
+def _round(torch, x, dt):
+    return x.to(_td(torch, dt)).double()
+
+
+def _attention(torch, dt, q, k, v, page, lengths, scale, window=0, max_length=None, table=None):
+    """k, v [S][tokens][KV][D] laid into pages in random order, or (with a table) pages as they are -> y, lse on the CPU."""
+    S, H, D = q.shape
+    if table is None:
+        tokens, KV = k.shape[1:3]
+        columns = -(-tokens // page)
+        order = torch.from_numpy(np.random.default_rng(tokens).permutation(S * columns))
+        pages = []
+        for x in (k, v):
+            full = torch.zeros((S, columns * page, KV, D), dtype=x.dtype)
+            full[:, :tokens] = x
+            full = full.reshape(S * columns, page, KV, D).transpose(1, 2)
+            out = torch.empty_like(full)
+            out[order] = full
+            pages.append(out.contiguous())
+        k, v = pages
+        table = order.int().reshape(S, columns)
+    cache = npas.KvCache(k.to(_td(torch, dt)).cuda(), v.to(_td(torch, dt)).cuda(), table.cuda(), dt)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    top = max_length or max(lengths)
+    need = npas.paged_attention_workspace_bytes(cache, H, top)
+    ws = torch.full((max(need, 16) // 4 + 1,), float("nan"), device="cuda")
+    y = torch.full((S, H, D), float("nan"), dtype=_td(torch, dt), device="cuda")
+    lse = torch.full((S, H), float("nan"), device="cuda")
+    npas.paged_attention(cache, q.to(_td(torch, dt)).cuda(), y, H, n, top, scale, window=window, lse=lse, workspace=ws, workspace_bytes=need)
+    return y.double().cpu(), lse.double().cpu()
+
+
+def _cancelling(torch, dt, S, H, D, seed):
+    """Scores x [S][3][H] in [-1, 0] and values v [S][3][H][D] of the storage type whose weighted sum nearly vanishes, so that the rounding
+    of the result hides nothing; the result and w in 64 bits."""
+    g = torch.Generator().manual_seed(seed)
+    x = _round(torch, -torch.rand((S, 3, H), generator=g, dtype=torch.float64), dt)
+    v = _round(torch, 64 * torch.randn((S, 3, H, D), generator=g, dtype=torch.float64), dt)
+    p = torch.softmax(x, 1)[..., None]
+    v[:, 1] = _round(torch, -v[:, 0] * p[:, 0] / p[:, 1], dt)
+    v[:, 2] = _round(torch, -(v[:, 0] * p[:, 0] + v[:, 1] * p[:, 1]) / p[:, 2], dt)
+    return x, v, (p * v).sum(1), (p * v.abs()).sum(1)
+
+
+def _outside(got, ref, w, dt, steps):
+    return (got - ref).abs() > U[dt] * ref.abs() + TINY[dt] + steps * u * w
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("D,where,steps", [(64, (0, 1, 2), 12), (128, (0, 1, 2), 12), (256, (0, 1, 2), 12), (64, (3, 2500, 5990), 24),
+                                           (128, (100, 1000, 4999), 24)])
+def test_weights_keep_the_bits_of_fp32(torch, dt, D, where, steps):
+    S, H = 8, 8
+    x, v3, ref, w = _cancelling(torch, dt, S, H, D, 1)
+    n = where[-1] + 1
+    k, v = torch.zeros((S, n, H, D), dtype=torch.float64), torch.zeros((S, n, H, D), dtype=torch.float64)
+    k[..., 0] = -200.0                                   # the other tokens: exp(-200) is zero in fp32
+    for i, j in enumerate(where):
+        k[:, j, :, 0], v[:, j] = x[:, i], v3[:, i]
+    q = torch.zeros((S, H, D), dtype=torch.float64)
+    q[..., 0] = 1
+    y, _ = _attention(torch, dt, q, k, v, 16, [n] * S, 1.0)
+    bad = _outside(y, ref, w, dt, steps)
+    assert int(bad.sum()) == 0, f"{int(bad.sum())} of {bad.numel()} off, worst {float(((y - ref).abs() / w).max() / u)} steps"
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("above", [15.0, 17.0])
+def test_many_small_weights_beside_a_large_one(torch, dt, above):
+    """One token stands far above the rest and has the value zero: the result is what the small weights make of theirs.  (Their sums are rounded
+    no more than 64 times in turn, their exponents of up to 25 are off by 2^-20.)"""
+    S, H, D, n = 2, 4, 64, 2048
+    g = torch.Generator().manual_seed(2)
+    k, v = torch.zeros((S, n, H, D), dtype=torch.float64), _round(torch, 1 + 0.5 * torch.randn((S, n, H, D), generator=g, dtype=torch.float64), dt)
+    k[:, 700, :, 0], v[:, 700] = above, 0
+    q = torch.zeros((S, H, D), dtype=torch.float64)
+    q[..., 0] = 1
+    y, lse = _attention(torch, dt, q, k, v, 16, [n] * S, 1.0)
+    p = torch.softmax(k[..., 0], 1)[..., None]
+    bad = _outside(y, (p * v).sum(1), (p * v.abs()).sum(1), dt, 256)
+    assert int(bad.sum()) == 0, f"{int(bad.sum())} of {bad.numel()} off"
+    assert float((lse - torch.logsumexp(k[..., 0], 1)).abs().max()) <= 4 * u * (1 + above)
+
+
+COUNTS = [  # heads, kv heads, D, page, lengths, window: across the ends of tiles, of lookups of 2048 tokens and of cuts
+    (4, 1, 128, 16, [9000], 0), (8, 8, 64, 16, [6000, 70, 2047, 1], 0), (2, 2, 256, 64, [5000, 129], 0), (16, 2, 80, 7, [2600, 2049, 33], 0),
+    (8, 4, 64, 16, [4000, 1500, 999], 1000), (1, 1, 24, 3, [1400], 0), (32, 8, 128, 16, [2047, 4097], 0)]
+
+
+def _counts(torch, n, first, D):
+    """Values 1 at element j % D of token j: with equal weights a result is its element's share of the tokens."""
+    v = torch.zeros((n, D), dtype=torch.float64)
+    v[torch.arange(n), torch.arange(n) % D] = 1
+    return v, v[first:].sum(0) / (n - first)
+
+
+def _counts_hold(y, lse, ref, n, dt):
+    return bool(((y - ref).abs() <= (U[dt] + 4 * u) * ref).all()) and bool(((lse - np.log(n)).abs() <= 4 * u * (1 + np.log(n))).all())
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("case", COUNTS, ids=str)
+def test_every_token_counts_once(torch, dt, case):
+    H, KV, D, page, lengths, window = case
+    S, top = len(lengths), max(lengths)
+    v = torch.zeros((S, top, KV, D), dtype=torch.float64)
+    for s, n in enumerate(lengths):
+        v[s, :n] = _counts(torch, n, 0, D)[0][:, None]
+        v[s, n:] = 100                                    # must not come in
+    y, lse = _attention(torch, dt, torch.zeros((S, H, D), dtype=torch.float64), torch.ones_like(v), v, page, lengths, 0.125, window)
+    for s, n in enumerate(lengths):
+        first = max(0, n - window) if window else 0
+        assert _counts_hold(y[s], lse[s], _counts(torch, n, first, D)[1], n - first, dt), (s, n)
+
+
+def test_these_bounds_reject_what_they_should(torch):
+    """On the CPU: weights in fp32 pass, weights rounded to the storage type or to two parts of it do not; nor does a lost token."""
+    for dt in (npas.BF16, npas.F16):
+        x, v, ref, w = _cancelling(torch, dt, 8, 8, 64, 1)
+        p = torch.exp(x.float() - x.float().amax(1, keepdim=True))
+        for parts in ("fp32", 1, 2):
+            if parts == "fp32":
+                r = p.double()
+            else:
+                r = torch.zeros_like(p, dtype=torch.float64)
+                for _ in range(parts):
+                    r = r + _round(torch, p.double() - r, dt)
+            bad = _outside(_round(torch, (r[..., None] * v).sum(1) / r.sum(1)[..., None], dt), ref, w, dt, 12).any()
+            # two parts of fp16 hold 22 bits and a sign, as many as fp32 has
+            assert bool(bad) == (parts == 1 or (parts == 2 and dt == npas.BF16)), (dt, parts)
+        for n, D in ((9000, 128), (6000, 64), (5000, 256), (1400, 24)):
+            value, ref = _counts(torch, n, 0, D)
+            whole = lambda keep: (_round(torch, value[keep].sum(0) / len(keep), dt), torch.full((1,), float(np.log(len(keep)))).double())   # noqa: E731
+            assert _counts_hold(*whole(list(range(n))), ref, n, dt)
+            for lost in (0, 128, n - 1):
+                y, lse = whole([j for j in range(n) if j != lost])
+                assert not _counts_hold(y, lse, ref, n, dt)
