@@ -188,6 +188,14 @@ template <typename F> __device__ __forceinline__ void with_activation(int act, F
     else if (act == NPAS_ACT_RELU6) f(std::integral_constant<int, NPAS_ACT_RELU6>{});
     else f(std::integral_constant<int, NPAS_ACT_HARDSWISH>{});
 }
+// What a wave's lanes have written to or read from LDS is done before its other lanes read or write there (one wave's accesses are in order in
+// the hardware; this keeps the compiler, to which they are of unlike types, from moving them).
+__device__ __forceinline__ void wave_meets()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 // A lane's two biases of a group.
 __device__ __forceinline__ float2 group_bias(const FcMxArgs &a, int o)
 {
@@ -452,6 +460,7 @@ template <int DT, int RR, int RC> __global__ __launch_bounds__(256, 2) void fc_m
     __syncthreads();
 #pragma unroll
     for (int i0 = 0; i0 < RR; i0 += L::PASS) {
+        if (i0) wave_meets(); // the pass before has been read
         with_activation(a.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < L::PASS; ++i)
@@ -466,6 +475,7 @@ template <int DT, int RR, int RC> __global__ __launch_bounds__(256, 2) void fc_m
                         else *reinterpret_cast<uint32_t *>(p) = pack2<DT>(v0, v1);
                     }
         });
+        wave_meets();
         constexpr int LANES = RC * 32 / 8; // lanes of a row, 8 results each
 #pragma unroll 4
         for (int u = lane; u < L::PASS * 32 * LANES; u += 64) {

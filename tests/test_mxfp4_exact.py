@@ -1,0 +1,44 @@
+"""4-bit products and conversions whose results are exact: compared bit for bit, whatever the order of the sums."""
+import numpy as np
+import pytest
+
+import paper_2012_00596_amd as npas
+from tests.test_mxfp4 import DT, GRID, _dev, _f64, _td
+from workloads import dtypes
+
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    return t
+
+
+def _selection(torch, B, IN, OUT, dt):
+    """Rows with a single 1 pick a column of the weights, which are values of the format: y[b][o] = w[o][b % IN], no two rows of a tile alike.
+    -> y of the kernel, and the definition's."""
+    rng = np.random.default_rng(B + OUT)
+    x = np.zeros((B, IN))
+    x[np.arange(B), np.arange(B) % IN] = 1
+    w = GRID[rng.integers(0, 8, (OUT, IN))] * rng.choice([-1.0, 1.0], (OUT, IN))
+    w[:, ::32] = 6 * np.sign(w[:, ::32] + 0.25)                 # a block's largest magnitude, so that its exponent is 0
+    want = w[:, np.arange(B) % IN].T
+    p = npas.pack_fc_mxfp4(dtypes.quantize(w, dt)[0], dt)
+    need = p.workspace_bytes(B)
+    work = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    y = torch.full((B, OUT), 77, dtype=_td(torch, dt), device="cuda")
+    npas.fc_mxfp4(p, _dev(torch, dtypes.quantize(x, dt)[0], dt), y, B, None, npas.ACT_NONE, work, need)
+    return _f64(y, dt), want
+
+
+# By rows and outputs: sixteen waves on a piece, eight on two, tiles of 128 x 128, tiles of 256 x 128 (whose results leave in two passes
+# through the same LDS), the last two with whole and with partial tiles.
+@gpu
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("B,IN,OUT", [(3, 96, 70), (70, 200, 513), (130, 200, 2000), (640, 200, 1664), (700, 90, 1501), (4096, 200, 4096),
+                                      (3900, 333, 4033)])
+def test_every_result_in_its_place(torch, dt, B, IN, OUT):
+    print(f"fc_mxfp4 B={B} IN={IN} OUT={OUT} dtype={dt}", flush=True)
+    got, want = _selection(torch, B, IN, OUT, dt)
+    np.testing.assert_array_equal(got, want)
