@@ -302,6 +302,8 @@ int npas_kv_append(const npas_kv_cache *cache, const void *q_dev, int64_t q_stri
 /* Attention of one new token a sequence over the cache: for sequence s and head h (reading the keys of head h / (heads / kv_heads))
  *   y[s][h] = sum_j p_j v_j,  p = softmax_j(scale * q[s][h] . k_j),  max(0, n - window) <= j < n, j in the cache,
  * n = length_dev[s] cut to 0 .. min(max_length, table_stride * page_size); window 0: no window.  Where no j is left, y is zero.
+ * An infinite v_j makes its element of y infinite, or NaN beside one of the other sign or where p_j is below 2^-15 (fp16; bf16: 2^-90) of the
+ * row's largest.
  * lse_dev (nullable, fp32 [sequences][heads]): log sum_j exp(scale * q . k_j), -inf where no j is left.
  * q: row s at q + s * q_stride, heads * head_dim long; y [sequences][heads][head_dim].  Long sequences are cut over workgroups whose
  * partial results are joined through the workspace (16-byte aligned, npas_paged_attention_workspace_bytes, which may be 0). */

@@ -20,6 +20,14 @@ __device__ __forceinline__ void token_range(const AttentionArgs &a, int s, int &
     count = n - first;
 }
 
+// Two 16-bit numbers below the weights a and b, next to them or nearly so; zero for zero.
+template <int DT> __device__ __forceinline__ uint32_t below2(float a, float b)
+{
+    const uint32_t u = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u), w = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);
+    if constexpr (DT == NPAS_BF16) return __builtin_amdgcn_perm(w, u, 0x07060302u);
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(u), __uint_as_float(w)));
+}
+
 // One workgroup a (sequence, key head, 16 of its query heads, cut): its four waves take tiles of 32 tokens in turn.
 // Both products run on 16 x 16 x 32 matrix instructions with the query heads as columns, so that a key or value is read once for all
 // heads of its group.  Scores: row operand = keys as they lie in the cache (lane 16 q + r: token r, 8 elements), result register i of
@@ -27,15 +35,15 @@ __device__ __forceinline__ void token_range(const AttentionArgs &a, int s, int &
 // counted so that quarter q holds tokens 4 q .. 4 q + 3 of both 16-token tiles; its row operand, values by element, comes from rows of
 // the cache read whole (lane 16 q + r: VW consecutive elements of those eight tokens) and turned round in registers, two elements an
 // instruction: row r of tile j is element VW r + j.  Nothing passes through LDS but the cache rows of the tokens.
-// The weights go in as 16-bit numbers and what these leave over: three bf16 hold all 24 bits of a weight, two fp16 hold 22 and a sign, and the
-// matrix cores have time for them (the kernel waits for memory).  fp16 reaches down to 2^-24 only, so there the largest weight is 2^15: what
-// is below 2^-39 of it is lost.
+// A weight goes in as three 16-bit numbers whose sum it is: the matrix cores have time for them (the kernel waits for memory).  The first two
+// are taken below what there is to represent, so that all three are positive and an infinite value comes out as itself.  fp16 reaches
+// down to 2^-24 only, so there the largest weight is 2^15: what is below 2^-39 of it is lost.
 // Memory bound: 64 sequences of up to 8192 tokens, 8 key heads of 128, 1.07 GB in 227 us (4.7 TB/s); one of 131071, 4 key heads, 55 us
 // (4.9 TB/s).  Few short sequences are a chain of latencies: a launch, the length, the pages, then 1.1-1.8 us a round of tiles.
 template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * NW, NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
 {
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
-    constexpr int PITCH = DP + 4, PARTS = DT == NPAS_BF16 ? 3 : 2;
+    constexpr int PITCH = DP + 4, PARTS = 3;
     constexpr float TOP = DT == NPAS_BF16 ? 1.f : 32768.f; // the largest weight
     __shared__ __align__(16) uint32_t rows[kRows];
     __shared__ float sm[NW][16], sl[NW][16];
@@ -150,7 +158,7 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
             l += p0 + p1;
 #pragma unroll
             for (int n = 0; n < PARTS; ++n) {
-                part[n][i] = pack2<DT>(p0, p1);
+                part[n][i] = n < PARTS - 1 ? below2<DT>(p0, p1) : pack2<DT>(p0, p1);
                 p0 -= from_storage<DT>((uint16_t)part[n][i]);
                 p1 -= from_storage<DT>((uint16_t)(part[n][i] >> 16));
             }

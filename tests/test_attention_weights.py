@@ -145,6 +145,40 @@ def test_every_token_counts_once(torch, dt, case):
         assert _counts_hold(y[s], lse[s], _counts(torch, n, first, D)[1], n - first, dt), (s, n)
 
 
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("H,KV,D,length", [(4, 2, 64, 40), (8, 2, 128, 300), (2, 1, 96, 3000), (6, 3, 256, 2500), (16, 16, 64, 700)])
+def test_infinite_values_come_out_as_they_are(torch, dt, H, KV, D, length):
+    """Every element of a head has one infinite value, of a token with some weight or other; the last elements have one of each sign or a
+    NaN.  All others are what they are without them."""
+    S = 4
+    g = torch.Generator().manual_seed(H + D)
+    k, v, q = (torch.randn(shape, generator=g, dtype=torch.float64) for shape in ((S, length, KV, D), (S, length, KV, D), (S, H, D)))
+    k[..., 0] *= 0.5                                       # scores within some 8: no weight below 2^-15 of the largest
+    q[..., 1:] = 0
+    clean, lse = _attention(torch, dt, q, k, v, 16, [length] * S, 1.0)
+    bad = v.clone()
+    token = torch.randint(0, length, (S, KV, D), generator=g)
+    sign = torch.where(torch.rand((S, KV, D), generator=g) < 0.5, -1.0, 1.0).double()
+    keep = torch.arange(D) % 3 == 2                        # every third element stays finite
+    for s in range(S):
+        for h in range(KV):
+            for d in range(D):
+                if keep[d]:
+                    continue
+                bad[s, token[s, h, d], h, d] = sign[s, h, d] * float("inf")
+                if d >= D - 2:
+                    bad[s, (token[s, h, d] + 1) % length, h, d] = -sign[s, h, d] * float("inf") if s % 2 else float("nan")
+    y, again = _attention(torch, dt, q, k, bad, 16, [length] * S, 1.0)
+    want = (sign * float("inf")).repeat_interleave(H // KV, 1)
+    for d in (D - 2, D - 1):
+        want[..., d] = float("nan")
+    want = torch.where(keep, clean, want)
+    assert torch.equal(again, lse)
+    same = (y == want) | ((y != y) & (want != want))
+    assert int((~same).sum()) == 0, f"{int((~same).sum())} of {y.numel()}"
+
+
 def test_these_bounds_reject_what_they_should(torch):
     """On the CPU: weights in fp32 pass, weights rounded to the storage type or to two parts of it do not; nor does a lost token."""
     for dt in (npas.BF16, npas.F16):
