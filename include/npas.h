@@ -304,7 +304,8 @@ int npas_kv_append(const npas_kv_cache *cache, const void *q_dev, int64_t q_stri
  * n = length_dev[s] cut to 0 .. min(max_length, table_stride * page_size); window 0: no window.  Where no j is left, y is zero.
  * An infinite v_j makes its element of y infinite, or NaN beside one of the other sign or where p_j is below 2^-15 (fp16; bf16: 2^-90) of the
  * row's largest.
- * lse_dev (nullable, fp32 [sequences][heads]): log sum_j exp(scale * q . k_j), -inf where no j is left.
+ * lse_dev (nullable, fp32 [sequences][heads]): log sum_j exp(scale * q . k_j), -inf where no j is left or every score is -inf (y is zero
+ * there too), inf where a score is (y is NaN there).
  * q: row s at q + s * q_stride, heads * head_dim long; y [sequences][heads][head_dim].  Long sequences are cut over workgroups whose
  * partial results are joined through the workspace (16-byte aligned, npas_paged_attention_workspace_bytes, which may be 0). */
 size_t npas_paged_attention_workspace_bytes(const npas_kv_cache *cache, int heads, int max_length);

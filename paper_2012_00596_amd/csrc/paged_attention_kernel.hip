@@ -1,5 +1,6 @@
 // Attention of one new token a sequence over the paged cache: a split kernel that walks the tokens once with running maximum and
 // sum, and a joining kernel for sequences that were cut over several workgroups.
+#include <cfloat>
 #include <type_traits>
 
 #include "decoder_internal.h"
@@ -143,8 +144,8 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
         }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m)) {
-            const float now = fmaxf(m, top), c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+        if (__any(top > m)) { // (an infinite score has an infinite weight, and so has the sum: finite maxima keep these from being NaN)
+            const float now = fminf(fmaxf(m, top), FLT_MAX), c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
             m = now;
             l *= c;
 #pragma unroll

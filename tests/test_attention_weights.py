@@ -179,6 +179,36 @@ def test_infinite_values_come_out_as_they_are(torch, dt, H, KV, D, length):
     assert int((~same).sum()) == 0, f"{int((~same).sum())} of {y.numel()}"
 
 
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("H,KV,D,length", [(4, 2, 64, 40), (8, 2, 128, 300), (2, 1, 96, 3000), (4, 2, 256, 2500)])
+def test_infinite_and_nan_scores(torch, dt, H, KV, D, length):
+    """By sequence: a score of inf; one of inf and one of -inf; one of -inf; one of inf and one NaN; only -inf; none of these."""
+    S = 6
+    g = torch.Generator().manual_seed(H + D + 1)
+    k, v, q = (torch.randn(shape, generator=g, dtype=torch.float64) for shape in ((S, length, KV, D), (S, length, KV, D), (S, H, D)))
+    q[..., 0] = 1
+    a, b = length // 2, length - 1
+    k[0, a, :, 0] = k[1, a, :, 0] = k[3, a, :, 0] = float("inf")
+    k[1, b, :, 0] = k[2, b, :, 0] = -float("inf")
+    k[3, b, :, 0] = float("nan")
+    k[4, :, :, 0] = -float("inf")
+    v = _round(torch, v, dt)
+    y, lse = _attention(torch, dt, q, k, v, 16, [length] * S, 0.125)
+    assert bool((y[[0, 1, 3]] != y[[0, 1, 3]]).all())
+    assert bool((lse[[0, 1]] == float("inf")).all()) and bool((lse[3] != lse[3]).all())
+    assert bool((y[4] == 0).all()) and bool((lse[4] == -float("inf")).all())
+    k, q = _round(torch, k, dt), _round(torch, q, dt)
+    for s, n in ((2, length - 1), (5, length)):
+        for h in range(H):
+            x = k[s, :n, h // (H // KV)] @ q[s, h] * 0.125
+            off = D * u * (k[s, :n, h // (H // KV)].abs() @ q[s, h].abs()).max() * 0.125
+            p = torch.softmax(x, 0)
+            value = v[s, :n, h // (H // KV)]
+            assert not bool(_outside(y[s, h], p @ value, p @ value.abs(), dt, (2 * off + 64 * u) / u).any()), (s, h)
+            assert float((lse[s, h] - torch.logsumexp(x, 0)).abs()) <= off + 64 * u
+
+
 def test_these_bounds_reject_what_they_should(torch):
     """On the CPU: weights in fp32 pass, weights rounded to the storage type or to two parts of it do not; nor does a lost token."""
     for dt in (npas.BF16, npas.F16):
