@@ -394,16 +394,47 @@ class Stack:
 
 # ---- a decoder block around its linear layers ----------------------------------
 
-def _rows(t, width):
-    """(device pointer, elements from row to row) of rows of `width` elements: a tensor whose rows are contiguous (a slice of a joined
-    projection, [rows][width] or [rows][heads][head_dim]), or the address of contiguous rows."""
+# The tensors of these calls are checked for the size of their elements and for their length (the library sees addresses alone); index
+# tensors for 32-bit integers, weights and angles for fp32.  Storage types may come as any type of their size (bit patterns).
+
+def _size(dtype):
+    return {F32: 4, BF16: 2, F16: 2}.get(dtype, 0)
+
+
+def _elements(t, count, size):
+    """Device pointer of `count` elements of `size` bytes (0: of whatever size) or more."""
+    p = _dev(t)
+    if t is not None and not isinstance(t, int):
+        assert t.nbytes == count * size or not size or t.itemsize == size, "tensor of another element size than the call's"
+        assert t.nbytes >= count * size, "tensor is shorter than the call needs"
+    return p
+
+
+def _words(t, count, fp32):
+    if t is not None and not isinstance(t, int):
+        assert t.itemsize == 4, "tensor of another element size than the call's"
+        assert not t.dtype.is_complex and t.dtype.is_floating_point == fp32, "tensor is not fp32" if fp32 else "tensor is not of 32-bit integers"
+    return _buffer(t, count * 4)
+
+
+def _buffer(t, nbytes):
+    p = _dev(t)
+    assert t is None or isinstance(t, int) or t.nbytes >= nbytes, "tensor is shorter than the call needs"
+    return p
+
+
+def _rows(t, width, least, size):
+    """(device pointer, elements from row to row) of at least `least` rows of `width` elements of `size` bytes: a tensor whose rows are contiguous
+    (a slice of a joined projection, [rows][width] or [rows][heads][head_dim]), or the address of contiguous rows."""
     if t is None or isinstance(t, int):
         return t, width
     inner = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        assert size == 1 or stride == inner, "rows are not contiguous"
-        inner *= size
+    for n, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        assert n == 1 or stride == inner, "rows are not contiguous"
+        inner *= n
     assert inner == width, f"rows of {inner} elements, {width} expected"
+    assert t.shape[0] >= least, "tensor has fewer rows than the call"
+    assert not size or t.itemsize == size, "tensor of another element size than the call's"
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
 
 
@@ -413,6 +444,7 @@ class KvCache:
 
     def __init__(self, k, v, page_table, dtype):
         assert k.dim() == 4 and tuple(k.shape) == tuple(v.shape), "keys and values are [pages][kv_heads][page_size][head_dim]"
+        assert k.itemsize == v.itemsize and (dtype not in (BF16, F16) or k.itemsize == 2), "the cache's tensors are not of its type's size"
         assert page_table.dim() == 2 and page_table.element_size() == 4 and not page_table.is_floating_point(), "page_table is int32"
         self.k, self.v, self.page_table, self.dtype = k, v, page_table, dtype
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
@@ -423,18 +455,19 @@ class KvCache:
 
 
 def _gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate, post_weight, pre_weight, residual_scale, eps, stream):
-    g, gs = None, 0
+    g, gs, size = None, 0, _size(dtype)
     if gate is not None and not isinstance(gate, int):
         if gate.dim() == 1 or gate.shape[0] == 1:
-            g = _dev(gate)
+            g = _elements(gate, D, size)
             assert gate.numel() == D, "gate is [D], [1][D] or [T][D]"
         else:
             assert gate.shape[0] == T, "gate is [D], [1][D] or [T][D]"
-            g, gs = _rows(gate, D)
+            g, gs = _rows(gate, D, T, size)
     elif gate is not None:
         g, gs = gate, D
-    _check(lib().npas_gated_residual_norm(_dev(branch), _dev(h), g, gs, _dev(post_weight), _dev(pre_weight), residual_scale, eps,
-                                          _dev(h_out), _dev(n_out), T, D, dtype, stream))
+    branch, h, h_out, n_out = (_elements(t, T * D, size) for t in (branch, h, h_out, n_out))
+    _check(lib().npas_gated_residual_norm(branch, h, g, gs, _words(post_weight, D, True), _words(pre_weight, D, True), residual_scale, eps,
+                                          h_out, n_out, T, D, dtype, stream))
 
 
 def gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate=None, post_weight=None, pre_weight=None, residual_scale=1.0, eps=1e-6,
@@ -447,14 +480,15 @@ def gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate=None, post_we
 
 def _kv_append(cache, q, k, v, q_out, T, heads, positions, sequences, cos_sin, rot_dim, kind, stream):
     D = cache.head_dim
-    qp, qs = _rows(q, heads * D)
-    kp, ks = _rows(k, cache.kv_heads * D)
-    vp, vs = _rows(v, cache.kv_heads * D)
-    cp, cstride = _rows(cos_sin, rot_dim)
+    qp, qs = _rows(q, heads * D, T, 2)
+    kp, ks = _rows(k, cache.kv_heads * D, T, 2)
+    vp, vs = _rows(v, cache.kv_heads * D, T, 2)
+    cp, cstride = _rows(cos_sin, rot_dim, 0, 4)
     assert cstride == rot_dim, "cos_sin is not contiguous"
     count = -1 if cos_sin is None or isinstance(cos_sin, int) else cos_sin.shape[0]
-    _check(lib().npas_kv_append(cache.desc, qp, qs, kp, ks, vp, vs, _dev(q_out), T, heads, _dev(sequences), _dev(positions), cp, count,
-                                rot_dim, kind, stream))
+    assert count < 0 or cos_sin.dtype.is_floating_point, "tensor is not fp32"
+    _check(lib().npas_kv_append(cache.desc, qp, qs, kp, ks, vp, vs, _elements(q_out, T * heads * D, 2), T, heads, _words(sequences, T, False),
+                                _words(positions, T, False), cp, count, rot_dim, kind, stream))
 
 
 def kv_append(cache, q, k, v, q_out, T, heads, positions, sequences=None, cos_sin=None, rot_dim=0, kind=ROTATE_HALVES, stream=None):
@@ -473,9 +507,11 @@ def paged_attention(cache, q, y, heads, lengths, max_length, scale, window=0, ls
 
 
 def _paged_attention(cache, q, y, heads, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream):
-    qp, qs = _rows(q, heads * cache.head_dim)
-    _check(lib().npas_paged_attention(cache.desc, qp, qs, _dev(y), _dev(lse), heads, _dev(lengths), max_length, window, scale,
-                                      _dev(workspace), workspace_bytes, stream))
+    S = cache.sequences
+    qp, qs = _rows(q, heads * cache.head_dim, S, 2)
+    _check(lib().npas_paged_attention(cache.desc, qp, qs, _elements(y, S * heads * cache.head_dim, 2), _words(lse, S * heads, True), heads,
+                                      _words(lengths, S, False), max_length, window, scale, _buffer(workspace, workspace_bytes),
+                                      workspace_bytes, stream))
 
 
 # ---- linear layers in microscaled 4-bit floats ----------------------------------
@@ -486,8 +522,9 @@ def mxfp4_quantize(x, codes, scales, M, K, dtype, stream=None):
 
 
 def _mxfp4_quantize(x, codes, scales, M, K, dtype, stream):
-    xp, xs = _rows(x, K)
-    _check(lib().npas_mxfp4_quantize(xp, xs, _dev(codes), _dev(scales), M, K, dtype, stream))
+    xp, xs = _rows(x, K, M, _size(dtype))
+    blocks = M * ((K + 31) // 32)
+    _check(lib().npas_mxfp4_quantize(xp, xs, _elements(codes, blocks * 16, 1), _elements(scales, blocks, 1), M, K, dtype, stream))
 
 
 def mxfp4_dequantize(codes, scales, y, M, K, dtype, stream=None):
@@ -496,7 +533,9 @@ def mxfp4_dequantize(codes, scales, y, M, K, dtype, stream=None):
 
 
 def _mxfp4_dequantize(codes, scales, y, M, K, dtype, stream):
-    _check(lib().npas_mxfp4_dequantize(_dev(codes), _dev(scales), _dev(y), M, K, dtype, stream))
+    blocks = M * ((K + 31) // 32)
+    _check(lib().npas_mxfp4_dequantize(_elements(codes, blocks * 16, 1), _elements(scales, blocks, 1), _elements(y, M * K, _size(dtype)), M, K,
+                                       dtype, stream))
 
 
 class Mxfp4:
@@ -505,7 +544,7 @@ class Mxfp4:
     def __init__(self, handle):
         self.handle = handle
         v = self.info()
-        self.OUT, self.IN = v["OUT"], v["IN"]
+        self.OUT, self.IN, self.dtype = v["OUT"], v["IN"], v["dtype"]
 
     def __del__(self):
         if getattr(self, "handle", None):
@@ -539,9 +578,11 @@ def pack_fc_mxfp4(w, dtype, stream=None):
 
 def fc_mxfp4(packed, x, y, B, bias=None, act=ACT_NONE, workspace=None, workspace_bytes=0, stream=None):
     """y [B][OUT] = act(bias + x W^T) with both factors in microscaled 4-bit floats; x [B][IN] (its rows may be a slice's)."""
-    (_calls or _load_calls()).fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, packed.IN)
+    (_calls or _load_calls()).fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, packed.IN, packed.OUT, packed.dtype)
 
 
-def _fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, IN):
-    xp, xs = _rows(x, IN)
-    _check(lib().npas_fc_mxfp4(packed.handle, xp, xs, _dev(y), B, _dev(bias), act, _dev(workspace), workspace_bytes, stream))
+def _fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, IN, OUT, dtype):
+    size = _size(dtype)
+    xp, xs = _rows(x, IN, B, size)
+    _check(lib().npas_fc_mxfp4(packed.handle, xp, xs, _elements(y, B * OUT, size), B, _words(bias, OUT, True), act,
+                               _buffer(workspace, workspace_bytes), workspace_bytes, stream))

@@ -10,7 +10,7 @@ namespace {
 
 PyObject *error_class; // NpasError(code, message), set by init()
 PyObject *c_void_p;    // ctypes.c_void_p, set by init()
-PyObject *s_handle, *s_value, *s_is_contiguous, *s_data_ptr, *s_shape, *s_stride;
+PyObject *s_handle, *s_value, *s_is_contiguous, *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_itemsize, *s_dtype;
 
 // The arguments of one call, converted in their order.  Once one does not convert, the later conversions do nothing.
 struct Args {
@@ -86,12 +86,44 @@ struct Args {
         return (float)v;
     }
 
-    // Rows of `width` elements: a tensor whose rows are contiguous, or the address of contiguous rows.  count: rows of a tensor, -1 of an address.
+    // The same, where a tensor must hold `count` elements of `size` bytes (size 0: of whatever size; the library refuses the type).
+    void *elements(int i, int64_t count, int size)
+    {
+        void *p = pointer(i);
+        if (state == PLAIN && is_tensor(i)) {
+            const int64_t bytes = attribute(a[i], s_nbytes);
+            if (bytes != count * size) { // (just as long: no further look)
+                of_size(i, size);
+                if (state == PLAIN && bytes < count * size) refuse("tensor is shorter than the call needs");
+            }
+        }
+        return p;
+    }
+    // ... of `bytes` bytes, whatever its elements.
+    void *buffer(int i, size_t bytes)
+    {
+        void *p = pointer(i);
+        if (state == PLAIN && is_tensor(i) && (size_t)attribute(a[i], s_nbytes) < bytes && state == PLAIN) refuse("tensor is shorter than the call needs");
+        return p;
+    }
+    // ... of a 32-bit type: integers, or fp32.
+    void *words(int i, int64_t count, bool fp32)
+    {
+        void *p = pointer(i);
+        if (state == PLAIN && is_tensor(i)) {
+            of_kind(i, fp32);
+            if (state == PLAIN && attribute(a[i], s_nbytes) < count * 4 && state == PLAIN) refuse("tensor is shorter than the call needs");
+        }
+        return p;
+    }
+
+    // Rows of `width` elements of `size` bytes, at least `least` of them: a tensor whose rows are contiguous, or the address of contiguous rows.
+    // count: rows of a tensor, -1 of an address.
     struct Rows {
         void *p;
         int64_t stride, count;
     };
-    Rows rows(int i, int64_t width)
+    Rows rows(int i, int64_t width, int64_t least, int size)
     {
         PyObject *o = a[i];
         if (state != PLAIN || o == Py_None) return Rows{nullptr, width, -1};
@@ -111,6 +143,8 @@ struct Args {
             r.count = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0));
             if (r.count > 1) r.stride = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, 0));
             if (state == PLAIN && PyErr_Occurred()) fail();
+            if (state == PLAIN && r.count < least) refuse("tensor has fewer rows than the call");
+            of_size(i, size);
         }
         Py_XDECREF(shape);
         Py_XDECREF(stride);
@@ -123,6 +157,13 @@ struct Args {
         Py_XDECREF(p);
         return r;
     }
+    // ... that is fp32 where it is a tensor.
+    Rows rows_fp32(int i, int64_t width)
+    {
+        const Rows r = rows(i, width, 0, 0);
+        if (state == PLAIN && is_tensor(i)) of_kind(i, true);
+        return r;
+    }
     void refuse(const char *why)
     {
         PyErr_SetString(PyExc_AssertionError, why);
@@ -130,6 +171,45 @@ struct Args {
     }
 
 private:
+    bool is_tensor(int i) const { return a[i] != Py_None && !PyLong_Check(a[i]); }
+    // A number that is an attribute of o; -1 where it is not.
+    int64_t attribute(PyObject *o, PyObject *name)
+    {
+        PyObject *v = PyObject_GetAttr(o, name);
+        const int64_t n = v ? PyLong_AsLongLong(v) : -1;
+        Py_XDECREF(v);
+        if (n == -1 && PyErr_Occurred()) fail();
+        return n;
+    }
+    bool yes(PyObject *o, const char *name)
+    {
+        PyObject *v = PyObject_GetAttrString(o, name);
+        const int is = v ? PyObject_IsTrue(v) : -1;
+        Py_XDECREF(v);
+        if (is < 0) fail();
+        return is > 0;
+    }
+    void of_size(int i, int size)
+    {
+        if (state == PLAIN && size && attribute(a[i], s_itemsize) != size && state == PLAIN) refuse("tensor of another element size than the call's");
+    }
+    // 32-bit integers, or fp32.  A type's object stands for the type: the last one that was right needs no further look.
+    void of_kind(int i, bool fp32)
+    {
+        static PyObject *right[2];
+        PyObject *t = PyObject_GetAttr(a[i], s_dtype);
+        if (!t) fail();
+        else if (t != right[fp32]) {
+            of_size(i, 4);
+            const bool floating = state == PLAIN && yes(t, "is_floating_point"), complex = state == PLAIN && yes(t, "is_complex");
+            if (state == PLAIN && (complex || floating != fp32)) refuse(fp32 ? "tensor is not fp32" : "tensor is not of 32-bit integers");
+            if (state == PLAIN) {
+                Py_INCREF(t);
+                Py_XSETREF(right[fp32], t);
+            }
+        }
+        Py_XDECREF(t);
+    }
     void *fail()
     {
         state = FAILED;
@@ -169,6 +249,8 @@ template <typename F> PyObject *finish(const Args &g, Call which, Py_ssize_t n, 
     Py_END_ALLOW_THREADS
     return result(rc);
 }
+
+int size_of(int dtype) { return dtype == NPAS_F32 ? 4 : dtype == NPAS_BF16 || dtype == NPAS_F16 ? 2 : 0; }
 
 bool argc(Py_ssize_t n, Py_ssize_t want)
 {
@@ -238,28 +320,29 @@ PyObject *gated_residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (!argc(n, 13)) return nullptr;
     Args g{a};
-    void *branch = g.pointer(0), *h = g.pointer(1), *ho = g.pointer(2), *no = g.pointer(3);
-    const int T = g.integer(4), D = g.integer(5), dt = g.integer(6);
+    const int T = g.integer(4), D = g.integer(5), dt = g.integer(6), size = size_of(dt);
+    const int64_t all = (int64_t)T * D;
+    void *branch = g.elements(0, all, size), *h = g.elements(1, all, size), *ho = g.elements(2, all, size), *no = g.elements(3, all, size);
     // one row [D] or [1][D] for all tokens, or a row a token
     int64_t stride = 0;
     void *gate = nullptr;
     if (g.state == Args::PLAIN && a[7] != Py_None) {
         PyObject *shape = PyLong_Check(a[7]) ? nullptr : PyObject_GetAttr(a[7], s_shape);
-        const bool flat = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 1;
-        const int64_t row = flat ? PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) : 0;
+        const Py_ssize_t dims = shape && PyTuple_Check(shape) ? PyTuple_GET_SIZE(shape) : 0;
+        const int64_t first = dims ? PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) : 0, last = dims ? PyLong_AsLongLong(PyTuple_GET_ITEM(shape, dims - 1)) : 0;
         Py_XDECREF(shape);
         if (PyErr_Occurred()) return nullptr;
-        if (flat) {
-            gate = g.pointer(7);
-            if (g.state == Args::PLAIN && row != D) g.refuse("gate is [D], [1][D] or [T][D]");
+        if (dims == 1 || (dims == 2 && first == 1)) {
+            gate = g.elements(7, D, size);
+            if (g.state == Args::PLAIN && last != D) g.refuse("gate is [D], [1][D] or [T][D]");
         } else {
-            const Args::Rows r = g.rows(7, D);
+            const Args::Rows r = g.rows(7, D, 1, size);
             gate = r.p;
             stride = r.count == 1 ? 0 : r.stride;
             if (g.state == Args::PLAIN && r.count >= 0 && r.count != 1 && r.count != T) g.refuse("gate is [D], [1][D] or [T][D]");
         }
     }
-    void *post = g.pointer(8), *pre = g.pointer(9);
+    void *post = g.words(8, D, true), *pre = g.words(9, D, true);
     const float scale = g.real(10), eps = g.real(11);
     void *st = g.address(12);
     return finish(g, NORM, n, [&] {
@@ -275,9 +358,9 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
     const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
     const int T = g.integer(5), heads = g.integer(6), rot = g.integer(10), kind = g.integer(11);
     const int64_t D = c ? c->head_dim : 0, kv = c ? c->kv_heads : 0;
-    const Args::Rows q = g.rows(1, heads * D), k = g.rows(2, kv * D), v = g.rows(3, kv * D);
-    void *qo = g.pointer(4), *pos = g.pointer(7), *seq = g.pointer(8);
-    const Args::Rows cs = g.rows(9, rot);
+    const Args::Rows q = g.rows(1, heads * D, T, 2), k = g.rows(2, kv * D, T, 2), v = g.rows(3, kv * D, T, 2);
+    void *qo = g.elements(4, (int64_t)T * heads * D, 2), *pos = g.words(7, T, false), *seq = g.words(8, T, false);
+    const Args::Rows cs = g.rows_fp32(9, rot);
     if (g.state == Args::PLAIN && cs.stride != rot) g.refuse("cos_sin is not contiguous");
     void *st = g.address(12);
     return finish(g, APPEND, n, [&] {
@@ -293,11 +376,12 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     Args g{a};
     const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
     const int heads = g.integer(3), most = g.integer(5), window = g.integer(7);
-    const Args::Rows q = g.rows(1, (int64_t)heads * (c ? c->head_dim : 0));
-    void *y = g.pointer(2), *len = g.pointer(4);
+    const int64_t width = (int64_t)heads * (c ? c->head_dim : 0), sequences = c ? c->sequences : 0;
+    const Args::Rows q = g.rows(1, width, sequences, 2);
+    void *y = g.elements(2, sequences * width, 2), *len = g.words(4, sequences, false);
     const float scale = g.real(6);
-    void *lse = g.pointer(8), *w = g.pointer(9);
     const size_t bytes = g.size(10);
+    void *lse = g.words(8, sequences * heads, true), *w = g.buffer(9, bytes);
     void *st = g.address(11);
     return finish(g, ATTENTION, n, [&] {
         return npas_paged_attention(c, q.p, q.stride, y, (float *)lse, heads, (const int32_t *)len, most, window, scale, w, bytes, st);
@@ -310,8 +394,9 @@ PyObject *mxfp4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!argc(n, 7)) return nullptr;
     Args g{a};
     const int M = g.integer(3), K = g.integer(4), dt = g.integer(5);
-    const Args::Rows x = g.rows(0, K);
-    void *codes = g.pointer(1), *scales = g.pointer(2), *st = g.address(6);
+    const Args::Rows x = g.rows(0, K, M, size_of(dt));
+    const int64_t blocks = M * (((int64_t)K + 31) / 32);
+    void *codes = g.elements(1, blocks * 16, 1), *scales = g.elements(2, blocks, 1), *st = g.address(6);
     return finish(g, QUANTIZE, n, [&] { return npas_mxfp4_quantize(x.p, x.stride, codes, scales, M, K, (npas_dtype)dt, st); });
 }
 
@@ -320,25 +405,25 @@ PyObject *mxfp4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (!argc(n, 7)) return nullptr;
     Args g{a};
-    void *codes = g.pointer(0), *scales = g.pointer(1), *y = g.pointer(2);
     const int M = g.integer(3), K = g.integer(4), dt = g.integer(5);
+    const int64_t blocks = M * (((int64_t)K + 31) / 32);
+    void *codes = g.elements(0, blocks * 16, 1), *scales = g.elements(1, blocks, 1), *y = g.elements(2, (int64_t)M * K, size_of(dt));
     void *st = g.address(6);
     return finish(g, DEQUANTIZE, n, [&] { return npas_mxfp4_dequantize(codes, scales, y, M, K, (npas_dtype)dt, st); });
 }
 
-// fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, IN)
+// fc_mxfp4(packed, x, y, B, bias, act, workspace, workspace_bytes, stream, IN, OUT, dtype)
 PyObject *fc_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (!argc(n, 10)) return nullptr;
+    if (!argc(n, 12)) return nullptr;
     Args g{a};
     npas_mxfp4 *p = (npas_mxfp4 *)g.handle(0);
-    const Args::Rows x = g.rows(1, g.integer(9));
-    void *y = g.pointer(2);
-    const int B = g.integer(3);
-    void *b = g.pointer(4);
+    const int B = g.integer(3), IN = g.integer(9), OUT = g.integer(10), size = size_of(g.integer(11));
+    const Args::Rows x = g.rows(1, IN, B, size);
+    void *y = g.elements(2, (int64_t)B * OUT, size), *b = g.words(4, OUT, true);
     const int act = g.integer(5);
-    void *w = g.pointer(6);
     const size_t bytes = g.size(7);
+    void *w = g.buffer(6, bytes);
     void *st = g.address(8);
     return finish(g, FC_MXFP4, n, [&] { return npas_fc_mxfp4(p, x.p, x.stride, y, B, b, (npas_act)act, w, bytes, st); });
 }
@@ -383,6 +468,9 @@ PyMODINIT_FUNC PyInit__pycalls()
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_shape = PyUnicode_InternFromString("shape");
     s_stride = PyUnicode_InternFromString("stride");
-    if (!s_handle || !s_value || !s_is_contiguous || !s_data_ptr || !s_shape || !s_stride) return nullptr;
+    s_nbytes = PyUnicode_InternFromString("nbytes");
+    s_itemsize = PyUnicode_InternFromString("itemsize");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    if (!s_handle || !s_value || !s_is_contiguous || !s_data_ptr || !s_shape || !s_stride || !s_nbytes || !s_itemsize || !s_dtype) return nullptr;
     return PyModule_Create(&module);
 }
