@@ -307,7 +307,8 @@ int npas_kv_append(const npas_kv_cache *cache, const void *q_dev, int64_t q_stri
  * lse_dev (nullable, fp32 [sequences][heads]): log sum_j exp(scale * q . k_j), -inf where no j is left or every score is -inf (y is zero
  * there too), inf where a score is (y is NaN there).
  * q: row s at q + s * q_stride, heads * head_dim long; y [sequences][heads][head_dim].  Long sequences are cut over workgroups whose
- * partial results are joined through the workspace (16-byte aligned, npas_paged_attention_workspace_bytes, which may be 0). */
+ * partial results are joined through the workspace (16-byte aligned; npas_paged_attention_workspace_bytes, which may be 0, is enough for any
+ * window, and a launch in one cut needs none). */
 size_t npas_paged_attention_workspace_bytes(const npas_kv_cache *cache, int heads, int max_length);
 int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t q_stride, void *y_dev, float *lse_dev, int heads,
                          const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev,

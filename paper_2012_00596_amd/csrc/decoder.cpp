@@ -47,7 +47,7 @@ int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
 //     up to 8192 tokens 227 us, in one cut 225).
 struct Cuts {
     int chunk, splits, waves;
-    size_t stat_at, bytes; // (maximum, sum) pairs lie behind the sums; bytes: enough for any window
+    size_t stat_at, need, bytes; // (maximum, sum) pairs lie behind the sums; need: of this launch, bytes: enough for any window
 };
 Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
 {
@@ -66,13 +66,16 @@ Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
     chunk = (chunk + 127) / 128 * 128;
     k.chunk = (int)chunk;
     k.splits = (int)((n + chunk - 1) / chunk);
-    // the most cuts that any window can lead to: each has kLeast tokens, and kMost or the pair's share of the workgroups
+    // the most cuts that any window can lead to: one where the longest length is one cut; otherwise each has kLeast tokens, and kMost or the
+    // pair's share of the workgroups
     const long share = (kWorkgroups + pairs - 1) / pairs, capped = (longest + kMost - 1) / kMost;
     long most = (longest + kLeast - 1) / kLeast;
     if (most > (share > capped ? share : capped)) most = share > capped ? share : capped;
     if (most > kMaxSplits) most = kMaxSplits;
+    if (longest * c.head_dim <= kSingle) most = 1;
     const size_t rows = (size_t)c.sequences * heads;
     k.stat_at = rows * k.splits * c.head_dim * 4;
+    if (k.splits > 1) k.need = rows * k.splits * (c.head_dim * 4 + 8);
     if (most > 1) k.bytes = rows * most * (c.head_dim * 4 + 8);
     return k;
 }
@@ -177,7 +180,7 @@ int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t 
         set_error("%d sequences x %d heads x %d cuts of max_length=%d are too many workgroups", a.c.sequences, heads, cuts.splits, max_length);
         return NPAS_E_SHAPE;
     }
-    const size_t need = cuts.bytes;
+    const size_t need = cuts.need;
     if (need && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 16))) {
         set_error("paged attention needs %zu bytes of workspace at a multiple of 16, got %zu at %p", need, workspace_bytes, workspace_dev);
         return NPAS_E_WORKSPACE;

@@ -231,3 +231,30 @@ def test_these_bounds_reject_what_they_should(torch):
             for lost in (0, 128, n - 1):
                 y, lse = whole([j for j in range(n) if j != lost])
                 assert not _counts_hold(y, lse, ref, n, dt)
+
+
+@pytest.mark.parametrize("sequences,kv_heads,D,length", [(1, 16, 64, 777), (1, 1, 256, 256), (300, 2, 128, 512), (3, 5, 8, 8192)])
+def test_short_caches_need_no_workspace(sequences, kv_heads, D, length):
+    """Where the longest length is one cut, whatever the window; one token more takes several (but not of 600 pairs, which fill the card)."""
+    desc = npas.KvCacheDesc(4096, 8192, 256, npas.BF16, 10000, 16, kv_heads, D, sequences, 5000)
+    assert npas.lib().npas_paged_attention_workspace_bytes(desc, 2 * kv_heads, length) == 0
+    more = npas.lib().npas_paged_attention_workspace_bytes(desc, 2 * kv_heads, 65536 // D + 1)
+    assert more > 0 if sequences * kv_heads < 512 else more == 0
+
+
+@gpu
+def test_a_window_of_one_cut_needs_no_workspace(torch):
+    S, H, KV, D, n, window, dt = 2, 4, 2, 64, 5000, 300, npas.F16
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn((S * 313, KV, 16, D), generator=g).half() for _ in range(2))
+    q, table = torch.randn((S, H, D), generator=g).half(), torch.arange(S * 313, dtype=torch.int32).reshape(S, 313)
+    cache = npas.KvCache(k.cuda(), v.cuda(), table.cuda(), dt)
+    assert npas.paged_attention_workspace_bytes(cache, H, n) > 0
+    y, lengths = torch.empty((S, H, D), dtype=torch.float16, device="cuda"), torch.tensor([n, 100], dtype=torch.int32, device="cuda")
+    npas.paged_attention(cache, q.cuda(), y, H, lengths, n, 0.125, window=window)
+    for s, (lo, hi) in enumerate(((n - window, n), (0, 100))):
+        for h in range(H):
+            keys, values = (x[s * 313:(s + 1) * 313, h // 2].reshape(-1, D)[lo:hi].double() for x in (k, v))
+            p = torch.softmax(keys @ q[s, h].double() * 0.125, 0)
+            off = 2 * D * float((keys.abs() @ q[s, h].double().abs()).max()) * 0.125 + 64
+            assert not bool(_outside(y[s, h].double().cpu(), p @ values, p @ values.abs(), dt, off).any())
