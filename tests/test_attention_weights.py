@@ -258,3 +258,28 @@ def test_a_window_of_one_cut_needs_no_workspace(torch):
             p = torch.softmax(keys @ q[s, h].double() * 0.125, 0)
             off = 2 * D * float((keys.abs() @ q[s, h].double().abs()).max()) * 0.125 + 64
             assert not bool(_outside(y[s, h].double().cpu(), p @ values, p @ values.abs(), dt, off).any())
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+def test_no_cut_of_the_longest_length_is_lost(torch, dt):
+    """2^31 - 1 tokens of equal weight in 512 cuts of 128 pages.  All places of the table are one page of zeros but for one in each eighth of
+    it, the first or last place of a cut, whose values are 2^14 at an element of its own."""
+    D, page, places = 8, 2 ** 15, 2 ** 16
+    v = torch.zeros((D + 1, 1, page, D))
+    table = torch.zeros((1, places), dtype=torch.int32)
+    at = [0, 8192 + 127, 16384, 24576 + 127, 32768 + 512, 40960 + 1023, 57344 - 1, places - 1]
+    for d, j in enumerate(at):
+        v[d + 1, ..., d], table[0, j] = 2.0 ** 14, d + 1
+    n = 2 ** 31 - 1
+    cache = npas.KvCache(torch.ones((D + 1, 1, page, D), dtype=_td(torch, dt), device="cuda"), v.to(_td(torch, dt)).cuda(), table.cuda(), dt)
+    ws = torch.full((npas.paged_attention_workspace_bytes(cache, 1, n) // 4 + 1,), float("nan"), device="cuda")
+    y, lse = torch.empty((1, 1, D), dtype=_td(torch, dt), device="cuda"), torch.empty((1, 1), device="cuda")
+    npas.paged_attention(cache, torch.zeros((1, 1, D), dtype=_td(torch, dt), device="cuda"), y, 1, torch.tensor([n], dtype=torch.int32).cuda(), n,
+                         1.0, lse=lse, workspace=ws, workspace_bytes=ws.nbytes)
+    rows = torch.full((D,), float(page), dtype=torch.float64)
+    rows[-1] -= 1                                               # the last token of the table is past the length
+    ref = rows * 2.0 ** 14 / n
+    # sums of powers of two are exact up to 2^24 of them; joins and the division take a few roundings
+    assert bool(((y.double().cpu()[0, 0] - ref).abs() <= (U[dt] + 8 * u) * ref).all()), y
+    assert abs(float(lse) - np.log(n)) <= 8 * u * (1 + np.log(n))
