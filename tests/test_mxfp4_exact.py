@@ -42,3 +42,23 @@ def test_every_result_in_its_place(torch, dt, B, IN, OUT):
     print(f"fc_mxfp4 B={B} IN={IN} OUT={OUT} dtype={dt}", flush=True)
     got, want = _selection(torch, B, IN, OUT, dt)
     np.testing.assert_array_equal(got, want)
+
+
+@gpu
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("B,IN,OUT", [(1, 4096, 512), (5, 1000, 333), (70, 2050, 513), (200, 384, 1700), (700, 1000, 1501), (4000, 520, 4090)])
+def test_two_calls_give_the_same_bits(torch, dt, B, IN, OUT):
+    """Sums are added in one order, whatever the type; rows that stand for NaN among the others."""
+    g = torch.Generator().manual_seed(B)
+    x, w = torch.randn((B, IN), generator=g).numpy(), torch.randn((OUT, IN), generator=g).numpy()
+    x[B // 2, IN // 3] = np.inf if B > 1 else 1
+    p = npas.pack_fc_mxfp4(dtypes.quantize(w, dt)[0], dt)
+    need = p.workspace_bytes(B)
+    work = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    store, bits = _dev(torch, dtypes.quantize(x, dt)[0], dt), torch.int32 if dt == npas.F32 else torch.int16
+    first = None
+    for i in range(6):
+        y = torch.full((B, OUT), 77 + i, dtype=_td(torch, dt), device="cuda")
+        npas.fc_mxfp4(p, store, y, B, None, npas.ACT_NONE, work, need)
+        first = y if first is None else first
+        assert torch.equal(y.view(bits), first.view(bits)), f"call {i}"
