@@ -62,3 +62,30 @@ def test_two_calls_give_the_same_bits(torch, dt, B, IN, OUT):
         npas.fc_mxfp4(p, store, y, B, None, npas.ACT_NONE, work, need)
         first = y if first is None else first
         assert torch.equal(y.view(bits), first.view(bits)), f"call {i}"
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+def test_every_16_bit_value_under_every_exponent(torch, dt):
+    """Every finite bit pattern in blocks of every power of two that can stand over it, 2^-133 .. 2^127 (bf16) and 2^-24 .. 2^15 (fp16): codes
+    and scales bit for bit."""
+    lowest, top = (-133, 127) if dt == npas.BF16 else (-24, 15)
+    td = torch.bfloat16 if dt == npas.BF16 else torch.float16
+    pattern = torch.arange(2 ** 16, dtype=torch.int32, device="cuda").to(torch.int16)
+    value = pattern.view(td).double()
+    for k in range(lowest, top + 1):
+        x = pattern[value.abs() < 2.0 ** (k + 1)]               # (a NaN is not)
+        x = torch.cat([x, torch.zeros(-len(x) % 31, dtype=torch.int16, device="cuda")]).reshape(-1, 31)
+        pin = torch.full((len(x), 1), 2.0 ** k, dtype=torch.float64, device="cuda").to(td).view(torch.int16)
+        rows = torch.cat([x[:, :k % 31], pin, x[:, k % 31:]], 1).contiguous()
+        codes = torch.empty((len(rows), 16), dtype=torch.uint8, device="cuda")
+        scales = torch.empty((len(rows), 1), dtype=torch.uint8, device="cuda")
+        npas.mxfp4_quantize(rows, codes, scales, len(rows), 32, dt)
+        e = max(k - 2, -127)
+        assert bool((scales == e + 127).all()), k
+        r, code = value[rows.long() & 0xFFFF].abs() * 2.0 ** -e, torch.zeros(rows.shape, dtype=torch.int32, device="cuda")
+        for i in range(7):                                      # of two equally near ones the even code
+            middle = float(GRID[i] + GRID[i + 1]) / 2
+            code += (r >= middle) if i % 2 else (r > middle)
+        code += (rows < 0) * 8
+        assert torch.equal(codes, (code[:, ::2] + 16 * code[:, 1::2]).to(torch.uint8)), k
