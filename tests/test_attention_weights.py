@@ -10,6 +10,7 @@ import numpy as np
 import pytest
 
 import paper_2012_00596_amd as npas
+from tests import test_decoder_ops as ops
 
 U = {npas.BF16: 2.0 ** -8, npas.F16: 2.0 ** -11}
 TINY = {npas.BF16: 2.0 ** -133, npas.F16: 2.0 ** -25}
@@ -283,3 +284,21 @@ def test_no_cut_of_the_longest_length_is_lost(torch, dt):
     # sums of powers of two are exact up to 2^24 of them; joins and the division take a few roundings
     assert bool(((y.double().cpu()[0, 0] - ref).abs() <= (U[dt] + 8 * u) * ref).all()), y
     assert abs(float(lse) - np.log(n)) <= 8 * u * (1 + np.log(n))
+
+
+@gpu
+@pytest.mark.parametrize("case", ops.ATTENTION + ops.CUTS, ids=str)
+def test_ragged_cases_without_an_allowance_for_rounded_weights(torch, monkeypatch, case):
+    """The ragged cases with windows, holes and NaN around them: weights are off by twice their scores' error, and by the sums' roundings (no
+    lane adds more than 128 numbers in turn, no result more than 96 products of up to 2 u each; taken together as 320), lse by its
+    score's error and as many; fp16 weights below 2^-39 of the largest are lost."""
+    def strict(torch, q, k, v, table, lengths, scale, window, max_length, dt, y, lse):
+        ref, lref, w, ds = ops._attention64(torch, q, k, v, table, lengths, scale, window, max_length)
+        lost = int(lengths.max()) * 2.0 ** -39 * float(v.double().nan_to_num().abs().max()) if dt == npas.F16 else 0.0
+        got, le, none = y.double().cpu(), lse.double().cpu(), lref == -float("inf")
+        bad = ~((got - ref).abs() <= U[dt] * ref.abs() + TINY[dt] + (2 * ds[..., None] + 320 * u) * w + lost)
+        assert int(bad.sum()) == 0, f"{int(bad.sum())} of {bad.numel()} off, worst {float((got - ref).abs().max())}"
+        assert bool((le[none] == -float("inf")).all())
+        assert bool(((le - lref).abs()[~none] <= ds[~none] + 320 * u + 4 * u * lref[~none].abs()).all())
+    monkeypatch.setattr(ops, "_check_attention", strict)
+    ops._run_attention(torch, case)
