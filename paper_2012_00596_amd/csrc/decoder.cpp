@@ -45,6 +45,8 @@ int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
 //   - Longer ones in 512 workgroups (131071 tokens of 4 pairs 54 us, in 1024 workgroups 56), at least 128 tokens each (4096 tokens of 8 pairs
 //     8.6 us, 256 each 10.3); and at most 2048, so that a long sequence in a ragged batch does not run alone at the end (512 pairs of
 //     up to 8192 tokens 227 us, in one cut 225).
+// Cuts follow max_length, not the lengths, which are on the device: a launch for much longer sequences than it meets leaves compute units idle
+// (8 pairs of 4096 tokens, head_dim 128, 8.7 us at max_length 4096, 11.7 at 32768, 25.5 at 131072; 128 pairs of 2048 26 us, 65 at 32768).
 struct Cuts {
     int chunk, splits, waves;
     size_t stat_at, need, bytes; // (maximum, sum) pairs lie behind the sums; need: of this launch, bytes: enough for any window

@@ -96,6 +96,7 @@ template <int DT, int NV, int WPR> __global__ __launch_bounds__(WPR == 1 ? 256 :
 }
 
 // Rows too long for registers: three walks over the row, the last of which forms h_out again and writes it (h_out may be h).
+// Element by element: 1024 rows of 16392 in 105 us (1.6 TB/s as five tensors; of 16384, in registers, 26), 256 of 65536 in 178.
 template <int DT> __global__ __launch_bounds__(1024) void gated_residual_norm_long_kernel(NormArgs a)
 {
     __shared__ float part[2][16];

@@ -306,10 +306,11 @@ template <int DT, int W, int J, bool FUSED> __global__ __launch_bounds__(64 * W)
 // that no read is young when the wave reaches the barrier) have two places.  One barrier a stage: before it a wave waits until its own
 // loads of stage t + 1 have landed (all but those of the stage behind it may be outstanding) and its reads of stage t are done; behind
 // it stage t is free for stage t + 3.
-// 4096 x 4096 -> 8192 in 67-72 us (4.1-3.8 PFLOP/s), about 18 of them launch, first stages and 67 MB of results; the loop runs at 5-5.7
-// PFLOP/s of the 6.7 that nothing but such instructions reach.  What bounds it is power: with zeros for codes the whole call takes 64-66 us
-// instead of 82-89.  LDS: a stage's operand reads and direct loads take as many cycles as its multiplications (128 x 128 tiles 1.33 times as
-// many); 256 x 256 tiles of four waves, 0.67, had no second workgroup to cover their stores (71.9 us).
+// 4096 x 4096 -> 8192 in 67-75 us (4.1-3.7 PFLOP/s), about 18 of them launch, first stages and 67 MB of results; the loop runs at 5-5.7
+// PFLOP/s of the 6.7 that nothing but such instructions reach.  With zeros for codes the whole call takes 63-66 us instead of 82-92: so much
+// is power.  The rest above the 41 of the instructions is those 18, which two rounds of workgroups do not cover, and 9 for the codes.
+// LDS: a stage's operand reads and direct loads take as many cycles as its multiplications (128 x 128 tiles 1.33 times as many); 256 x 256
+// tiles of four waves, 0.67, had no second workgroup to cover their stores (71.9 us).
 template <int DT, int RR, int RC> struct MxTile {
     static constexpr int XI = 4 * RR, WI = 4 * RC, STAGE = (XI + WI) * 1024, RING = 3;  // images of a stage: activations, then weights
     static constexpr int SCALES = (2 * RR + 2 * RC) * 256, LOADS = RR + RC;              // scale words of two stages; loads of a wave, a stage
