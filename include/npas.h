@@ -53,7 +53,8 @@ typedef struct npas_packed npas_packed; /* one packed layer */
 typedef struct npas_stack npas_stack;   /* a wired list of layers */
 typedef struct npas_mxfp4 npas_mxfp4;   /* one linear layer in microscaled 4-bit floats */
 
-typedef enum { NPAS_F32 = 0, NPAS_BF16 = 1, NPAS_F16 = 2 } npas_dtype;
+/* NPAS_E4M3 (sign, four exponent bits with bias 7, three mantissa bits, no infinities) is a type of caches alone. */
+typedef enum { NPAS_F32 = 0, NPAS_BF16 = 1, NPAS_F16 = 2, NPAS_E4M3 = 3 } npas_dtype;
 /* ReLU6 = min(max(v, 0), 6); hard-swish (what Phase 1 of the framework puts in place of swish,
  * section 5.1) = v * min(max(v + 3, 0), 6) / 6.  Applied after bias and residual, before rounding. */
 typedef enum { NPAS_ACT_NONE = 0, NPAS_ACT_RELU = 1, NPAS_ACT_RELU6 = 2, NPAS_ACT_HARDSWISH = 3 } npas_act;
@@ -256,7 +257,7 @@ void npas_stack_free(npas_stack *s);
 
 /* ---- a decoder block around its linear layers ------------------------------
  * What a transformer's decoder block needs between projections that run as npas_fc_sparse (block-based pruning) or npas_fc_mxfp4:
- * norms with gate and residual, a paged cache of keys and values, attention of one new token a sequence.  Rows are tokens; a
+ * norms with gate and residual, a paged cache of keys and values in 16 or 8 bits, attention of one new token or a run of them a sequence.  Rows are tokens; a
  * row is contiguous, rows lie `.._stride` elements apart (slices of a joined projection need no copy).  Pointers need the
  * alignment of their element type, the two caches 16 bytes.  Outputs overlap no input but where a call says so.  Sums, norms and
  * softmax statistics are held in fp32; a result is rounded to the storage type once.  Nothing allocates or synchronises; lengths,
@@ -313,6 +314,55 @@ size_t npas_paged_attention_workspace_bytes(const npas_kv_cache *cache, int head
 int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t q_stride, void *y_dev, float *lse_dev, int heads,
                          const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev,
                          size_t workspace_bytes, void *hip_stream);
+
+/* A cache in 8-bit floats is described by a npas_kv_cache whose dtype is NPAS_E4M3 (keys and values are bytes, [pages][kv_heads][page_size]
+ * [head_dim] as ever) and by its scales.  A row is cut into blocks of 32 elements (the last may be partial); a block has one power of two 2^e, kept
+ * as the byte e + 127 in k_scale and v_scale [pages][kv_heads][page_size][ceil(head_dim / 32)], 16-byte aligned, and per element the NPAS_E4M3
+ * number nearest to x / 2^e, ties to the even code.  e is the least of -15 .. 8 (dtype NPAS_F16; NPAS_BF16: -110 .. 120) with magnitudes up to
+ * 448 * 2^e; at the largest e they stop at 240 * 2^e (61440, or 3.19e38).  So every number that a cache written here stands for is one of dtype's.  A block
+ * that holds an infinity or a NaN has byte 255 and stands for NaN throughout.  head_dim: a multiple of 16.  dtype is the storage type of the rows outside: queries, keys,
+ * values, results.  The calls above refuse such a cache; those below take scales == NULL for a cache of 16 bits. */
+typedef struct {
+    void *k_scale_dev, *v_scale_dev;
+    int dtype;
+} npas_kv_scales;
+
+/* Norm of every head's queries and keys, rotation, keys and values into the paged cache: npas_kv_append with
+ *   x = x * weight / sqrt(mean(x^2) + eps) over the head's elements, weight fp32 [head_dim]
+ * before the rotation, for queries where q_weight is not NULL and for keys where k_weight is not; and into a cache of 8-bit floats too (scales
+ * not NULL).  Norm, rotation and what is written are formed from unrounded fp32.  Everything else is as npas_kv_append says. */
+int npas_kv_write(const npas_kv_cache *cache, const npas_kv_scales *scales, const void *q_dev, int64_t q_stride, const void *k_dev,
+                  int64_t k_stride, const void *v_dev, int64_t v_stride, void *q_out_dev, int T, int heads, const int32_t *sequence_dev,
+                  const int32_t *position_dev, const float *q_weight_dev, const float *k_weight_dev, float eps, const float *cos_sin_dev,
+                  int positions, int rot_dim, npas_rotation kind, void *hip_stream);
+
+/* Keys and values out of a cache of 8-bit floats: those of sequence_dev[t] (NULL: t itself) at position_dev[t] to k_out, v_out
+ * [T][kv_heads][head_dim] in the scales' dtype (one of them may be NULL).  Zeros where the position is negative, the sequence none of the
+ * cache's or the page not in the cache. */
+int npas_kv_read(const npas_kv_cache *cache, const npas_kv_scales *scales, void *k_out_dev, void *v_out_dev, int T,
+                 const int32_t *sequence_dev, const int32_t *position_dev, void *hip_stream);
+
+/* npas_paged_attention over a cache of 8-bit floats: q and y in the scales' dtype. */
+size_t npas_paged_attention8_workspace_bytes(const npas_kv_cache *cache, const npas_kv_scales *scales, int heads, int max_length);
+int npas_paged_attention8(const npas_kv_cache *cache, const npas_kv_scales *scales, const void *q_dev, int64_t q_stride, void *y_dev,
+                          float *lse_dev, int heads, const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev,
+                          size_t workspace_bytes, void *hip_stream);
+
+/* Causal attention of runs of new tokens over the cache (whole prompts, pieces of one, drafted tokens), of 16 bits (scales NULL) or 8.  Sequence
+ * s has the rows start_dev[s] .. start_dev[s + 1] - 1 of q (int32 [sequences + 1], rising, 0 .. T; none: an empty run); their keys and values are in
+ * the cache already.  With n = length_dev[s] (the new tokens among them) cut to 0 .. min(max_length, table_stride * page_size) and m rows, row
+ * i of the run stands at position p = n - m + i and
+ *   y = sum_j p_j v_j,  p = softmax_j(scale * q . k_j),  max(0, p + 1 - window) <= j <= p, j in the cache;  window 0: no window.
+ * Where no j is left (p < 0 among them), y is zero.  Rows of q before start_dev[0] or from start_dev[sequences] on: their y and lse stay as they were.
+ * q: row t at q + t * q_stride, heads * head_dim long; y [T][heads][head_dim]; lse_dev (nullable) fp32 [T][heads], as npas_paged_attention's.
+ * A weight is rounded to 16 bits before it is multiplied (bf16 to 2^-8 of itself; fp16 2^-11, at least 2^-40 of the largest that the row has met): y is off by at most that part
+ * of sum_j p_j |v_j| beside its own rounding.  A weight that is lost so, times an infinite v_j, gives NaN.
+ * Where there are few rows, long sequences are cut over workgroups whose partial results are joined through the workspace (16-byte aligned;
+ * npas_chunk_attention_workspace_bytes, which may be 0, is enough for any window, any lengths up to max_length and any parting of T). */
+size_t npas_chunk_attention_workspace_bytes(const npas_kv_cache *cache, const npas_kv_scales *scales, int T, int heads, int max_length);
+int npas_chunk_attention(const npas_kv_cache *cache, const npas_kv_scales *scales, const void *q_dev, int64_t q_stride, void *y_dev,
+                         float *lse_dev, int T, int heads, const int32_t *start_dev, const int32_t *length_dev, int max_length, int window,
+                         float scale, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 /* ---- linear layers in microscaled 4-bit floats -------------------------------
  * Rows are cut into blocks of 32 consecutive elements (the last may be partial: as if zeros followed).  A block has one power of two 2^e,

@@ -12,11 +12,13 @@ _LIB = os.path.join(_HERE, "libnpas.so")
 _CALLS = os.path.join(_HERE, "_pycalls.so")  # CPython entry points of the run calls, linked to libnpas.so
 SOURCES = ["pack.cpp", "api.cpp", "kernels.hip", "spatial_direct_kernel.hip", "small_channel_rows_kernel.hip", "small_kernels.hip", "block_kernels.hip",
            "inverted_residual_kernel.hip", "pointwise_stream_kernel.hip", "bottleneck_tail_kernel.hip", "noalloc.hip",
-           "decoder.cpp", "decoder_kernels.hip", "paged_attention_kernel.hip", "mxfp4.cpp", "mxfp4_kernels.hip"]
-HEADERS = ["npas_internal.h", "device_util.h", "decoder_internal.h", "mxfp4_internal.h", "row_vectors.h"]
+           "decoder.cpp", "decoder_kernels.hip", "paged_attention_kernel.hip", "kv_cache.cpp", "kv_write_kernel.hip", "chunk_attention_kernel.hip",
+           "mxfp4.cpp", "mxfp4_kernels.hip"]
+HEADERS = ["npas_internal.h", "device_util.h", "decoder_internal.h", "mxfp4_internal.h", "row_vectors.h", "cache8.h"]
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "npas.h")
 
 F32, BF16, F16 = 0, 1, 2
+E4M3 = 3               # of caches alone
 ACT_NONE, ACT_RELU, ACT_RELU6, ACT_HARDSWISH = 0, 1, 2, 3
 SCHEME_BLOCK_PUNCHED, SCHEME_FC_BLOCK, SCHEME_PATTERN, SCHEME_DEPTHWISE = 0, 1, 2, 3
 LAYER_CONV, LAYER_FC, LAYER_MAXPOOL3X3S2, LAYER_GLOBAL_AVGPOOL, LAYER_DEPTHWISE3X3 = 0, 1, 2, 3, 4
@@ -36,6 +38,8 @@ EXPORTS = [
     "npas_run_stack", "npas_stack_num_launches", "npas_stack_free", "npas_stack_describe", "npas_debug_set_switches",
     "npas_run_stack_static", "npas_debug_launch_empty", "npas_debug_device_kernel", "npas_debug_direct_plan",
     "npas_gated_residual_norm", "npas_kv_append", "npas_paged_attention_workspace_bytes", "npas_paged_attention",
+    "npas_kv_write", "npas_kv_read", "npas_paged_attention8_workspace_bytes", "npas_paged_attention8",
+    "npas_chunk_attention_workspace_bytes", "npas_chunk_attention",
     "npas_mxfp4_quantize", "npas_mxfp4_dequantize", "npas_pack_fc_mxfp4", "npas_mxfp4_info", "npas_mxfp4_export", "npas_mxfp4_free",
     "npas_fc_mxfp4_workspace_bytes", "npas_fc_mxfp4",
 ]
@@ -88,6 +92,9 @@ class KvCacheDesc(C.Structure):
                 ("page_size", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("sequences", C.c_int),
                 ("table_stride", C.c_int)]
 
+class KvScalesDesc(C.Structure):
+    _fields_ = [("k_scale_dev", C.c_void_p), ("v_scale_dev", C.c_void_p), ("dtype", C.c_int)]
+
 
 _lib = None
 
@@ -138,6 +145,15 @@ def lib():
         L.npas_paged_attention_workspace_bytes.argtypes = [cache, ip, ip]
         L.npas_paged_attention_workspace_bytes.restype = C.c_size_t
         L.npas_paged_attention.argtypes = [cache, vp, i64, vp, vp, ip, vp, ip, ip, C.c_float, vp, C.c_size_t, vp]
+        scales = C.POINTER(KvScalesDesc)
+        L.npas_kv_write.argtypes = [cache, scales, vp, i64, vp, i64, vp, i64, vp, ip, ip, vp, vp, vp, vp, C.c_float, vp, ip, ip, ip, vp]
+        L.npas_kv_read.argtypes = [cache, scales, vp, vp, ip, vp, vp, vp]
+        L.npas_paged_attention8_workspace_bytes.argtypes = [cache, scales, ip, ip]
+        L.npas_paged_attention8_workspace_bytes.restype = C.c_size_t
+        L.npas_paged_attention8.argtypes = [cache, scales, vp, i64, vp, vp, ip, vp, ip, ip, C.c_float, vp, C.c_size_t, vp]
+        L.npas_chunk_attention_workspace_bytes.argtypes = [cache, scales, ip, ip, ip]
+        L.npas_chunk_attention_workspace_bytes.restype = C.c_size_t
+        L.npas_chunk_attention.argtypes = [cache, scales, vp, i64, vp, vp, ip, ip, vp, vp, ip, ip, C.c_float, vp, C.c_size_t, vp]
         L.npas_mxfp4_quantize.argtypes = [vp, i64, vp, vp, ip, ip, ip, vp]
         L.npas_mxfp4_dequantize.argtypes = [vp, vp, vp, ip, ip, ip, vp]
         L.npas_pack_fc_mxfp4.argtypes = [vp, ip, ip, ip, vp, C.POINTER(vp)]
@@ -167,7 +183,7 @@ def _load_calls():
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
         mod.init(NpasError, C.c_void_p, _conv2d_sparse, _fc_sparse, _depthwise3x3, _run_stack, _gated_residual_norm, _kv_append,
-                 _paged_attention, _mxfp4_quantize, _mxfp4_dequantize, _fc_mxfp4)
+                 _paged_attention, _mxfp4_quantize, _mxfp4_dequantize, _fc_mxfp4, _kv_write, _kv_read, _paged_attention8, _chunk_attention)
         _calls = mod
     return _calls
 
@@ -442,6 +458,8 @@ class KvCache:
     """A paged cache of keys and values: k, v [pages][kv_heads][page_size][head_dim] (16-bit), page_table int32 [sequences][pages of the
     longest]; keeps the tensors alive.  dtype: BF16 or F16."""
 
+    scales = scales_desc = None   # of a cache in 8-bit floats
+
     def __init__(self, k, v, page_table, dtype):
         assert k.dim() == 4 and tuple(k.shape) == tuple(v.shape), "keys and values are [pages][kv_heads][page_size][head_dim]"
         assert k.itemsize == v.itemsize and (dtype not in (BF16, F16) or k.itemsize == 2), "the cache's tensors are not of its type's size"
@@ -452,6 +470,21 @@ class KvCache:
         self.desc = KvCacheDesc(_dev(k), _dev(v), _dev(page_table), dtype, self.pages, self.page_size, self.kv_heads, self.head_dim,
                                 self.sequences, page_table.shape[1])
         self.handle = C.c_void_p(C.addressof(self.desc))
+
+
+class KvCache8(KvCache):
+    """A paged cache in 8-bit floats: k, v of one-byte elements, shaped as KvCache's; k_scale, v_scale uint8 [pages][kv_heads][page_size]
+    [ceil(head_dim / 32)], the exponents of their blocks (npas_kv_scales).  dtype: of the rows outside, BF16 or F16."""
+
+    def __init__(self, k, v, k_scale, v_scale, page_table, dtype):
+        assert k.dim() == 4 and k.itemsize == 1, "keys and values of an 8-bit cache are bytes"
+        super().__init__(k, v, page_table, E4M3)
+        want = tuple(k.shape[:3]) + ((k.shape[3] + 31) // 32,)
+        assert tuple(k_scale.shape) == tuple(v_scale.shape) == want, "scales are [pages][kv_heads][page_size][ceil(head_dim / 32)]"
+        assert k_scale.itemsize == v_scale.itemsize == 1, "scales are bytes"
+        self.k_scale, self.v_scale, self.dtype = k_scale, v_scale, dtype
+        self.scales_desc = KvScalesDesc(_dev(k_scale), _dev(v_scale), dtype)
+        self.scales = C.c_void_p(C.addressof(self.scales_desc))
 
 
 def _gated_residual_norm(branch, h, h_out, n_out, T, D, dtype, gate, post_weight, pre_weight, residual_scale, eps, stream):
@@ -512,6 +545,76 @@ def _paged_attention(cache, q, y, heads, lengths, max_length, scale, window, lse
     _check(lib().npas_paged_attention(cache.desc, qp, qs, _elements(y, S * heads * cache.head_dim, 2), _words(lse, S * heads, True), heads,
                                       _words(lengths, S, False), max_length, window, scale, _buffer(workspace, workspace_bytes),
                                       workspace_bytes, stream))
+
+
+def _kv_write(cache, q, k, v, q_out, T, heads, positions, sequences, q_weight, k_weight, eps, cos_sin, rot_dim, kind, stream):
+    D = cache.head_dim
+    qp, qs = _rows(q, heads * D, T, 2)
+    kp, ks = _rows(k, cache.kv_heads * D, T, 2)
+    vp, vs = _rows(v, cache.kv_heads * D, T, 2)
+    cp, cstride = _rows(cos_sin, rot_dim, 0, 4)
+    assert cstride == rot_dim, "cos_sin is not contiguous"
+    count = -1 if cos_sin is None or isinstance(cos_sin, int) else cos_sin.shape[0]
+    assert count < 0 or cos_sin.dtype.is_floating_point, "tensor is not fp32"
+    _check(lib().npas_kv_write(cache.desc, cache.scales_desc, qp, qs, kp, ks, vp, vs, _elements(q_out, T * heads * D, 2), T, heads,
+                               _words(sequences, T, False), _words(positions, T, False), _words(q_weight, D, True), _words(k_weight, D, True),
+                               eps, cp, count, rot_dim, kind, stream))
+
+
+def kv_write(cache, q, k, v, q_out, T, heads, positions, sequences=None, q_weight=None, k_weight=None, eps=1e-6, cos_sin=None, rot_dim=0,
+             kind=ROTATE_HALVES, stream=None):
+    """kv_append with a norm of every head's queries and keys before the rotation (q_weight, k_weight fp32 [head_dim]; None: no norm), into a
+    KvCache or a KvCache8 (npas_kv_write)."""
+    (_calls or _load_calls()).kv_write(cache, q, k, v, q_out, T, heads, positions, sequences, q_weight, k_weight, eps, cos_sin, rot_dim, kind,
+                                       stream)
+
+
+def _kv_read(cache, k, v, T, positions, sequences, stream):
+    count = T * cache.kv_heads * cache.head_dim
+    _check(lib().npas_kv_read(cache.desc, cache.scales_desc, _elements(k, count, 2), _elements(v, count, 2), T, _words(sequences, T, False),
+                              _words(positions, T, False), stream))
+
+
+def kv_read(cache, k, v, T, positions, sequences=None, stream=None):
+    """Keys and values of T tokens out of a KvCache8, to k, v [T][kv_heads][head_dim] (npas_kv_read); one of them may be None."""
+    (_calls or _load_calls()).kv_read(cache, k, v, T, positions, sequences, stream)
+
+
+def paged_attention8_workspace_bytes(cache, heads, max_length):
+    return int(lib().npas_paged_attention8_workspace_bytes(cache.desc, cache.scales_desc, heads, max_length))
+
+
+def paged_attention8(cache, q, y, heads, lengths, max_length, scale, window=0, lse=None, workspace=None, workspace_bytes=0, stream=None):
+    """Attention of one new token a sequence over a KvCache8 (npas_paged_attention8); lengths int32 [sequences]."""
+    (_calls or _load_calls()).paged_attention8(cache, q, y, heads, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream)
+
+
+def _paged_attention8(cache, q, y, heads, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream):
+    S = cache.sequences
+    qp, qs = _rows(q, heads * cache.head_dim, S, 2)
+    _check(lib().npas_paged_attention8(cache.desc, cache.scales_desc, qp, qs, _elements(y, S * heads * cache.head_dim, 2),
+                                       _words(lse, S * heads, True), heads, _words(lengths, S, False), max_length, window, scale,
+                                       _buffer(workspace, workspace_bytes), workspace_bytes, stream))
+
+
+def chunk_attention_workspace_bytes(cache, T, heads, max_length):
+    return int(lib().npas_chunk_attention_workspace_bytes(cache.desc, cache.scales_desc, T, heads, max_length))
+
+
+def chunk_attention(cache, q, y, T, heads, starts, lengths, max_length, scale, window=0, lse=None, workspace=None, workspace_bytes=0,
+                    stream=None):
+    """Causal attention of runs of new tokens over a KvCache or KvCache8 (npas_chunk_attention): sequence s has the rows starts[s] ..
+    starts[s + 1] - 1 of q, which are the last of its lengths[s] cached tokens.  starts int32 [sequences + 1], lengths int32 [sequences]."""
+    (_calls or _load_calls()).chunk_attention(cache, q, y, T, heads, starts, lengths, max_length, scale, window, lse, workspace,
+                                              workspace_bytes, stream)
+
+
+def _chunk_attention(cache, q, y, T, heads, starts, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream):
+    S = cache.sequences
+    qp, qs = _rows(q, heads * cache.head_dim, T, 2)
+    _check(lib().npas_chunk_attention(cache.desc, cache.scales_desc, qp, qs, _elements(y, T * heads * cache.head_dim, 2),
+                                      _words(lse, T * heads, True), T, heads, _words(starts, S + 1, False), _words(lengths, S, False),
+                                      max_length, window, scale, _buffer(workspace, workspace_bytes), workspace_bytes, stream))
 
 
 # ---- linear layers in microscaled 4-bit floats ----------------------------------

@@ -1,21 +1,21 @@
 // C-ABI calls of the decoder-block operators: argument checks and launches.
 #include "decoder_internal.h"
 
-using namespace npas;
-
-namespace {
+namespace npas {
 
 bool misaligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
-bool storage(int dt) { return dt == NPAS_F32 || dt == NPAS_BF16 || dt == NPAS_F16; }
+bool bad_stride(int64_t stride, int64_t row) { return stride < row || stride > (int64_t)1 << 40; }
 
-int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
+int check_cache(const npas_kv_cache *c, const npas_kv_scales *scales, int heads, CacheArgs *out, int *dt)
 {
-    if (!c || !c->k_dev || !c->v_dev || !c->page_table_dev) {
-        set_error("NULL argument (cache, its keys, values or page table)");
+    if (!c || !c->k_dev || !c->v_dev || !c->page_table_dev || (scales && (!scales->k_scale_dev || !scales->v_scale_dev))) {
+        set_error("NULL argument (cache, its keys, values or page table, or a scale)");
         return NPAS_E_NULL;
     }
-    if (c->dtype != NPAS_BF16 && c->dtype != NPAS_F16) {
-        set_error("a cache holds bf16 or fp16, not storage type %d", c->dtype);
+    const int rows = scales ? scales->dtype : c->dtype;
+    if ((scales && c->dtype != NPAS_E4M3) || (rows != NPAS_BF16 && rows != NPAS_F16)) {
+        if (scales) set_error("a cache with scales holds e4m3 for rows of bf16 or fp16, not storage type %d for rows of type %d", c->dtype, rows);
+        else set_error("a cache holds bf16 or fp16, not storage type %d", c->dtype);
         return NPAS_E_DTYPE;
     }
     if (c->pages <= 0 || c->page_size <= 0 || c->kv_heads <= 0 || c->sequences <= 0 || c->table_stride <= 0 || c->head_dim <= 0 ||
@@ -28,13 +28,28 @@ int check_cache(const npas_kv_cache *c, int heads, CacheArgs *out)
         set_error("%d heads over %d key heads of %d elements and %d sequences", heads, c->kv_heads, c->head_dim, c->sequences);
         return NPAS_E_SHAPE;
     }
-    if (misaligned(c->k_dev, 16) || misaligned(c->v_dev, 16) || misaligned(c->page_table_dev, 4)) {
-        set_error("the caches need 16-byte alignment, the page table 4");
+    if (misaligned(c->k_dev, 16) || misaligned(c->v_dev, 16) || misaligned(c->page_table_dev, 4) ||
+        (scales && (misaligned(scales->k_scale_dev, 16) || misaligned(scales->v_scale_dev, 16)))) {
+        set_error("the caches and their scales need 16-byte alignment, the page table 4");
         return NPAS_E_SHAPE;
     }
-    *out = CacheArgs{c->k_dev, c->v_dev, c->page_table_dev, c->pages, c->page_size, c->kv_heads, c->head_dim, c->sequences, c->table_stride};
+    if (scales && c->head_dim % 16) {
+        set_error("a cache of 8-bit floats takes head_dim in multiples of 16, not %d", c->head_dim);
+        return NPAS_E_SHAPE;
+    }
+    *out = CacheArgs{c->k_dev, c->v_dev, c->page_table_dev, c->pages, c->page_size, c->kv_heads, c->head_dim, c->sequences, c->table_stride,
+                     scales ? (uint8_t *)scales->k_scale_dev : nullptr, scales ? (uint8_t *)scales->v_scale_dev : nullptr};
+    *dt = rows;
     return NPAS_OK;
 }
+
+} // namespace npas
+
+using namespace npas;
+
+namespace {
+
+bool storage(int dt) { return dt == NPAS_F32 || dt == NPAS_BF16 || dt == NPAS_F16; }
 
 // How a launch cuts the tokens.  A pair is a sequence's key head (with up to 16 of its query heads): one workgroup a pair and cut.
 //   - Up to kSingle elements of keys a pair one cut: the joining launch takes longer to issue (1.6 to 2.4 us) than it saves (from call to call: 16
@@ -82,7 +97,43 @@ Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
     return k;
 }
 
-bool bad_stride(int64_t stride, int64_t row) { return stride < row || stride > (int64_t)1 << 40; }
+int paged_attention(const npas_kv_cache *cache, const npas_kv_scales *scales, const void *q_dev, int64_t q_stride, void *y_dev, float *lse_dev,
+                    int heads, const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev, size_t workspace_bytes,
+                    void *hip_stream)
+{
+    AttentionArgs a{};
+    int dt;
+    if (int rc = check_cache(cache, scales, heads, &a.c, &dt)) return rc;
+    if (!q_dev || !y_dev || !length_dev) {
+        set_error("NULL argument (q=%p y=%p length=%p)", q_dev, y_dev, (const void *)length_dev);
+        return NPAS_E_NULL;
+    }
+    if (max_length <= 0 || window < 0 || bad_stride(q_stride, (int64_t)heads * a.c.head_dim) || !(scale == scale)) {
+        set_error("bad shape heads=%d max_length=%d window=%d q_stride=%lld scale=%g", heads, max_length, window, (long long)q_stride,
+                  (double)scale);
+        return NPAS_E_SHAPE;
+    }
+    if (misaligned(q_dev, 2) || misaligned(y_dev, 2) || misaligned(lse_dev, 4) || misaligned(length_dev, 4)) {
+        set_error("a pointer is not aligned to its element type");
+        return NPAS_E_SHAPE;
+    }
+    const Cuts cuts = plan_cuts(a.c, heads, max_length, window);
+    if ((double)a.c.sequences * cuts.splits * heads > 2147483647.0) {
+        set_error("%d sequences x %d heads x %d cuts of max_length=%d are too many workgroups", a.c.sequences, heads, cuts.splits, max_length);
+        return NPAS_E_SHAPE;
+    }
+    const size_t need = cuts.need;
+    if (need && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 16))) {
+        set_error("paged attention needs %zu bytes of workspace at a multiple of 16, got %zu at %p", need, workspace_bytes, workspace_dev);
+        return NPAS_E_WORKSPACE;
+    }
+    a.q = q_dev; a.y = y_dev; a.lse = lse_dev; a.q_stride = q_stride; a.length = length_dev;
+    a.heads = heads; a.max_length = max_length; a.window = window; a.scale = scale;
+    a.chunk = cuts.chunk; a.splits = cuts.splits; a.waves = cuts.waves;
+    a.part = (float *)workspace_dev;
+    a.part_stat = (float2 *)((uint8_t *)workspace_dev + cuts.stat_at);
+    return launch_paged_attention(dt, a, hip_stream);
+}
 
 } // namespace
 
@@ -125,7 +176,8 @@ int npas_kv_append(const npas_kv_cache *cache, const void *q_dev, int64_t q_stri
                    void *hip_stream)
 {
     AppendArgs a{};
-    if (int rc = check_cache(cache, heads, &a.c)) return rc;
+    int dt;
+    if (int rc = check_cache(cache, nullptr, heads, &a.c, &dt)) return rc;
     if (!k_dev || !v_dev || !position_dev || !q_dev != !q_out_dev || (rot_dim > 0 && !cos_sin_dev)) {
         set_error("NULL argument (q=%p q_out=%p k=%p v=%p position=%p cos_sin=%p)", q_dev, q_out_dev, k_dev, v_dev,
                   (const void *)position_dev, (const void *)cos_sin_dev);
@@ -148,13 +200,14 @@ int npas_kv_append(const npas_kv_cache *cache, const void *q_dev, int64_t q_stri
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
     a.sequence = sequence_dev; a.position = position_dev; a.cos_sin = cos_sin_dev;
     a.T = T; a.heads = heads; a.positions = positions; a.rot_dim = rot_dim; a.pairs = kind == NPAS_ROTATE_PAIRS;
-    return launch_kv_append(cache->dtype, a, hip_stream);
+    return launch_kv_append(dt, a, hip_stream);
 }
 
 size_t npas_paged_attention_workspace_bytes(const npas_kv_cache *cache, int heads, int max_length)
 {
     CacheArgs c;
-    if (max_length <= 0 || check_cache(cache, heads, &c)) return 0;
+    int dt;
+    if (max_length <= 0 || check_cache(cache, nullptr, heads, &c, &dt)) return 0;
     return plan_cuts(c, heads, max_length, 0).bytes;
 }
 
@@ -162,37 +215,28 @@ int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t 
                          const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev,
                          size_t workspace_bytes, void *hip_stream)
 {
-    AttentionArgs a{};
-    if (int rc = check_cache(cache, heads, &a.c)) return rc;
-    if (!q_dev || !y_dev || !length_dev) {
-        set_error("NULL argument (q=%p y=%p length=%p)", q_dev, y_dev, (const void *)length_dev);
+    return paged_attention(cache, nullptr, q_dev, q_stride, y_dev, lse_dev, heads, length_dev, max_length, window, scale, workspace_dev,
+                           workspace_bytes, hip_stream);
+}
+
+size_t npas_paged_attention8_workspace_bytes(const npas_kv_cache *cache, const npas_kv_scales *scales, int heads, int max_length)
+{
+    CacheArgs c;
+    int dt;
+    if (max_length <= 0 || !scales || check_cache(cache, scales, heads, &c, &dt)) return 0;
+    return plan_cuts(c, heads, max_length, 0).bytes;
+}
+
+int npas_paged_attention8(const npas_kv_cache *cache, const npas_kv_scales *scales, const void *q_dev, int64_t q_stride, void *y_dev,
+                          float *lse_dev, int heads, const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev,
+                          size_t workspace_bytes, void *hip_stream)
+{
+    if (!scales) {
+        set_error("NULL argument (scales)");
         return NPAS_E_NULL;
     }
-    if (max_length <= 0 || window < 0 || bad_stride(q_stride, (int64_t)heads * a.c.head_dim) || !(scale == scale)) {
-        set_error("bad shape heads=%d max_length=%d window=%d q_stride=%lld scale=%g", heads, max_length, window, (long long)q_stride,
-                  (double)scale);
-        return NPAS_E_SHAPE;
-    }
-    if (misaligned(q_dev, 2) || misaligned(y_dev, 2) || misaligned(lse_dev, 4) || misaligned(length_dev, 4)) {
-        set_error("a pointer is not aligned to its element type");
-        return NPAS_E_SHAPE;
-    }
-    const Cuts cuts = plan_cuts(a.c, heads, max_length, window);
-    if ((double)a.c.sequences * cuts.splits * heads > 2147483647.0) {
-        set_error("%d sequences x %d heads x %d cuts of max_length=%d are too many workgroups", a.c.sequences, heads, cuts.splits, max_length);
-        return NPAS_E_SHAPE;
-    }
-    const size_t need = cuts.need;
-    if (need && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 16))) {
-        set_error("paged attention needs %zu bytes of workspace at a multiple of 16, got %zu at %p", need, workspace_bytes, workspace_dev);
-        return NPAS_E_WORKSPACE;
-    }
-    a.q = q_dev; a.y = y_dev; a.lse = lse_dev; a.q_stride = q_stride; a.length = length_dev;
-    a.heads = heads; a.max_length = max_length; a.window = window; a.scale = scale;
-    a.chunk = cuts.chunk; a.splits = cuts.splits; a.waves = cuts.waves;
-    a.part = (float *)workspace_dev;
-    a.part_stat = (float2 *)((uint8_t *)workspace_dev + cuts.stat_at);
-    return launch_paged_attention(cache->dtype, a, hip_stream);
+    return paged_attention(cache, scales, q_dev, q_stride, y_dev, lse_dev, heads, length_dev, max_length, window, scale, workspace_dev,
+                           workspace_bytes, hip_stream);
 }
 
 } // extern "C"

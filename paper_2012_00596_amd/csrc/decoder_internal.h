@@ -1,5 +1,5 @@
 // Kernel argument blocks and launchers of the decoder-block operators (norm with gate and residual, paged cache,
-// attention of one token).
+// attention of one token and of runs of tokens).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -19,12 +19,14 @@ struct NormArgs {
     int T, D;
 };
 
-// The cache as the kernels see it; a row is head_dim elements.
+// The cache as the kernels see it; a row is head_dim elements.  Scales: of a cache of 8-bit floats, a byte for 32 elements.
 struct CacheArgs {
     void *k, *v;
     const int32_t *table;
     int pages, page_size, kv_heads, head_dim, sequences, table_stride;
+    uint8_t *k_scale, *v_scale;
 };
+constexpr uint32_t kAbsent = 0xffffffffu; // the row of a token that is not in the cache
 
 struct AppendArgs {
     CacheArgs c;
@@ -52,9 +54,52 @@ struct AttentionArgs {
 };
 constexpr int kMaxSplits = 512;
 
+struct WriteArgs {
+    CacheArgs c;
+    const void *q, *k, *v;
+    void *q_out;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *sequence, *position;
+    const float *q_weight, *k_weight, *cos_sin;
+    float eps;
+    int T, heads, positions, rot_dim, pairs;
+};
+
+struct ReadArgs {
+    CacheArgs c;
+    void *k_out, *v_out;
+    const int32_t *sequence, *position;
+    int T;
+};
+
+struct ChunkArgs {
+    CacheArgs c;
+    const void *q;
+    void *y;
+    float *lse;
+    int64_t q_stride;
+    const int32_t *start, *length;
+    int T, heads, max_length, window;
+    float scale;
+    // cuts of `chunk` tokens; more than one: unnormalised sums [row][cut][head_dim] and (maximum, sum) of each, rows [T][heads]
+    int chunk, splits, few; // few: the form for runs of few rows
+    float *part;
+    float2 *part_stat;
+};
+// Rows (tokens x query heads of a key head) of a workgroup's tile.
+int chunk_tile_rows(int head_dim, int few);
+
 int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream);
 int launch_kv_append(int dt, const AppendArgs &a, void *stream);
 int launch_paged_attention(int dt, const AttentionArgs &a, void *stream);
+int launch_kv_write(int dt, const WriteArgs &a, void *stream);
+int launch_kv_read(int dt, const ReadArgs &a, void *stream);
+int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream);
+
+// Arguments that the calls on a cache share.  scales NULL: a cache of 16 bits; dt: storage type of the rows outside.
+int check_cache(const npas_kv_cache *c, const npas_kv_scales *scales, int heads, CacheArgs *out, int *dt);
+bool misaligned(const void *p, size_t to);
+bool bad_stride(int64_t stride, int64_t row);
 
 // Refuses what is more than a launch can have, 2^32 - 1 threads.
 int check_grid(const char *what, uint64_t workgroups, unsigned threads);

@@ -3,12 +3,12 @@
 #include <cfloat>
 #include <type_traits>
 
+#include "cache8.h"
 #include "decoder_internal.h"
 #include "device_util.h"
 
 namespace npas {
 
-constexpr uint32_t kAbsent = 0xffffffffu;
 constexpr int kRows = 2048; // tokens whose cache rows are looked up at once
 
 // The tokens of sequence s that take part: [first, first + count).
@@ -41,7 +41,10 @@ template <int DT> __device__ __forceinline__ uint32_t below2(float a, float b)
 // down to 2^-24 only, so there the largest weight is 2^15: what is below 2^-39 of it is lost.
 // Memory bound: 64 sequences of up to 8192 tokens, 8 key heads of 128, 1.07 GB in 227 us (4.7 TB/s); one of 131071, 4 key heads, 55 us
 // (4.9 TB/s).  Few short sequences are a chain of latencies: a launch, the length, the pages, then 1.1-1.8 us a round of tiles.
-template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * NW, NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
+// E8: the cache holds 8-bit floats with a power of two for 32 elements.  A lane keeps the bytes and the scales of its next tile and makes 16-bit numbers of
+// them, exactly, when they are multiplied: keys as the first product's operand (where head_dim is DP a lane takes 16 consecutive elements of 64, so that a load
+// has 16 bytes; the query's elements are taken in the same order), values before they are turned round.
+template <int DT, int NC, bool FULL, int NW, bool E8> __global__ __launch_bounds__(64 * NW, NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
 {
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
     constexpr int PITCH = DP + 4, PARTS = 3;
@@ -63,10 +66,12 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
     if (from >= count && (split > 0 || a.splits > 1)) return;
     const int t0 = first + (int)from, cnt = min(a.chunk, count - (int)from);
     const bool real = h0 + r < group;
+    // first of the eight elements that a lane has in the first product's step c
+    auto key_element = [&](int c) __attribute__((always_inline)) { return E8 && FULL ? (c >> 1) * 64 + 16 * q + 8 * (c & 1) : 32 * c + 8 * q; };
     uint4 qf[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int d = 32 * c + 8 * q;
+        const int d = key_element(c);
         qf[c] = make_uint4(0, 0, 0, 0);
         if (real && d < D) {
             struct __attribute__((packed, aligned(2))) Words { uint32_t w[4]; };
@@ -76,27 +81,54 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
         }
     }
     const uint8_t *kb = reinterpret_cast<const uint8_t *>(a.c.k), *vb = reinterpret_cast<const uint8_t *>(a.c.v);
-    const uint32_t row_bytes = (uint32_t)D * 2;
+    const uint32_t row_bytes = (uint32_t)D * (E8 ? 1 : 2), blocks = (uint32_t)(D + 31) >> 5;
     const float to2 = a.scale * 1.4426950408889634f; // scores in powers of two
     f32x4 o[VW] = {};
     float m = -INFINITY, l = 0.f;
 
     // A tile's keys and values have one place each: the next tile's keys are asked for as soon as the scores are formed, its values as soon as
     // they have been multiplied, so that one tile is on its way all the time and the registers leave room for more waves.
-    uint4 kt[2][NC];
-    uint32_t vt[8][VP * VD], absent;
+    constexpr int VR = E8 ? VP * VD / 2 : VP * VD; // words of a lane's value row
+    std::conditional_t<E8, uint2, uint4> kt[2][NC];
+    uint32_t vt[8][VR], absent;
+    uint32_t ks[2][E8 ? NC : 1], vs[E8 ? 8 : 1]; // scales: of each step's elements, of each token's
     auto load_keys = [&](int tile) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t row = rows[tile * 32 + 16 * h + r];
-            const uint8_t *p = kb + (uint64_t)(row == kAbsent ? 0u : row) * row_bytes;
+            const uint32_t row = rows[tile * 32 + 16 * h + r], at = row == kAbsent ? 0u : row;
+            const uint8_t *p = kb + (uint64_t)at * row_bytes;
+            if constexpr (E8) {
+                const uint8_t *sp = a.c.k_scale + (uint64_t)at * blocks;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const int d = 32 * c + 8 * q;
-                if (FULL || d < D) kt[h][c] = *reinterpret_cast<const uint4 *>(p + 2 * d);
-                else kt[h][c] = make_uint4(0, 0, 0, 0);
+                for (int c = 0; c < NC; ++c) {
+                    const int d = key_element(c);
+                    if constexpr (FULL) {
+                        if (c % 2 == 0) {
+                            const uint4 w = *reinterpret_cast<const uint4 *>(p + d);
+                            kt[h][c] = make_uint2(w.x, w.y), kt[h][c + 1] = make_uint2(w.z, w.w);
+                            ks[h][c] = ks[h][c + 1] = sp[d >> 5];
+                        }
+                    } else if (d < D) {
+                        kt[h][c] = *reinterpret_cast<const uint2 *>(p + d);
+                        ks[h][c] = sp[d >> 5];
+                    } else {
+                        kt[h][c] = make_uint2(0, 0);
+                        ks[h][c] = 127;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const int d = 32 * c + 8 * q;
+                    if (FULL || d < D) kt[h][c] = *reinterpret_cast<const uint4 *>(p + 2 * d);
+                    else kt[h][c] = make_uint4(0, 0, 0, 0);
+                }
             }
         }
+    };
+    auto keys = [&](int h, int c) __attribute__((always_inline)) {
+        if constexpr (E8) return from_e4m3x8<DT>(kt[h][c], ks[h][c]);
+        else return kt[h][c];
     };
     auto load_values = [&](int tile) __attribute__((always_inline)) {
         absent = 0;
@@ -109,12 +141,14 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
                 const bool none = row[i] == kAbsent;
                 if (none) absent |= 1u << (4 * h + i);
                 const uint8_t *p = vb + (uint64_t)(none ? 0u : row[i]) * row_bytes;
+                if constexpr (E8) vs[4 * h + i] = a.c.v_scale[(uint64_t)(none ? 0u : row[i]) * blocks + (FULL || VW * r < D ? VW * r >> 5 : 0)];
 #pragma unroll
                 for (int e = 0; e < VP; ++e) {
                     const int d = VW * r + 8 * e;
-                    const uint8_t *x = p + 2 * (FULL || d < D ? d : 0); // elements past the head: their results are not kept
-                    uint32_t *v = &vt[4 * h + i][e * VD];
-                    if constexpr (VD == 4) {
+                    const uint8_t *x = p + (E8 ? 1 : 2) * (FULL || d < D ? d : 0); // elements past the head: their results are not kept
+                    uint32_t *v = &vt[4 * h + i][e * VR / VP];
+                    if constexpr (VR / VP == 1) v[0] = *reinterpret_cast<const uint32_t *>(x);
+                    else if constexpr (VR / VP == 4) {
                         const uint4 w = *reinterpret_cast<const uint4 *>(x);
                         v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
                     } else {
@@ -131,8 +165,8 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
         f32x4 c0 = {}, c1 = {};
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            c0 = mfma16<DT>(kt[0][c], qf[c], c0);
-            c1 = mfma16<DT>(kt[1][c], qf[c], c1);
+            c0 = mfma16<DT>(keys(0, c), qf[c], c0);
+            c1 = mfma16<DT>(keys(1, c), qf[c], c1);
         }
         if (MORE) load_keys(next);
         __builtin_amdgcn_sched_barrier(0);
@@ -166,16 +200,23 @@ template <int DT, int NC, bool FULL, int NW> __global__ __launch_bounds__(64 * N
         }
         if (__any(absent != 0)) // an absent token's row is another's: it must not bring in an infinity or a NaN
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 8; ++i) {
 #pragma unroll
-                for (int w = 0; w < VW / 2; ++w) vt[i][w] = absent >> i & 1 ? 0u : vt[i][w];
+                for (int w = 0; w < VR; ++w) vt[i][w] = absent >> i & 1 ? 0u : vt[i][w];
+                if constexpr (E8) vs[i] = absent >> i & 1 ? 127u : vs[i];
+            }
 #pragma unroll
         for (int w = 0; w < VW / 2; ++w) {
             uint32_t even[4], odd[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                even[i] = __builtin_amdgcn_perm(vt[2 * i + 1][w], vt[2 * i][w], 0x05040100u);
-                odd[i] = __builtin_amdgcn_perm(vt[2 * i + 1][w], vt[2 * i][w], 0x07060302u);
+                uint32_t lo, hi; // two elements of two tokens
+                if constexpr (E8) {
+                    lo = w & 1 ? from_e4m3x2<DT, true>(vt[2 * i][w >> 1], vs[2 * i]) : from_e4m3x2<DT, false>(vt[2 * i][w >> 1], vs[2 * i]);
+                    hi = w & 1 ? from_e4m3x2<DT, true>(vt[2 * i + 1][w >> 1], vs[2 * i + 1]) : from_e4m3x2<DT, false>(vt[2 * i + 1][w >> 1], vs[2 * i + 1]);
+                } else lo = vt[2 * i][w], hi = vt[2 * i + 1][w];
+                even[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+                odd[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
             }
             const uint4 ve = make_uint4(even[0], even[1], even[2], even[3]), vo = make_uint4(odd[0], odd[1], odd[2], odd[3]);
 #pragma unroll
@@ -321,8 +362,13 @@ int launch_paged_attention(int dt, const AttentionArgs &a, void *stream)
             constexpr int NC = decltype(ncc)::value;
             auto form = [&](auto nwc) {
                 constexpr int NW = decltype(nwc)::value;
-                if (a.c.head_dim == 32 * NC) hipLaunchKernelGGL((paged_attention_kernel<DT, NC, true, NW>), grid, dim3(64 * NW), 0, st, a);
-                else hipLaunchKernelGGL((paged_attention_kernel<DT, NC, false, NW>), grid, dim3(64 * NW), 0, st, a);
+                auto width = [&](auto e8c) {
+                    constexpr bool E8 = decltype(e8c)::value;
+                    if (a.c.head_dim == 32 * NC) hipLaunchKernelGGL((paged_attention_kernel<DT, NC, true, NW, E8>), grid, dim3(64 * NW), 0, st, a);
+                    else hipLaunchKernelGGL((paged_attention_kernel<DT, NC, false, NW, E8>), grid, dim3(64 * NW), 0, st, a);
+                };
+                if (a.c.k_scale) width(std::true_type{});
+                else width(std::false_type{});
             };
             if constexpr (NC <= 4) {
                 if (a.waves == 8) return form(std::integral_constant<int, 8>{});

@@ -10,7 +10,7 @@ namespace {
 
 PyObject *error_class; // NpasError(code, message), set by init()
 PyObject *c_void_p;    // ctypes.c_void_p, set by init()
-PyObject *s_handle, *s_value, *s_is_contiguous, *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_itemsize, *s_dtype;
+PyObject *s_handle, *s_scales, *s_value, *s_is_contiguous, *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_itemsize, *s_dtype;
 
 // The arguments of one call, converted in their order.  Once one does not convert, the later conversions do nothing.
 struct Args {
@@ -43,10 +43,11 @@ struct Args {
     }
 
     // Library handle of a Packed / Stack object: its `handle` is a ctypes c_void_p, or None once released.
-    void *handle(int i)
+    void *handle(int i) { return handle(i, s_handle); }
+    void *handle(int i, PyObject *name)
     {
         if (state != PLAIN) return nullptr;
-        PyObject *h = PyObject_GetAttr(a[i], s_handle);
+        PyObject *h = PyObject_GetAttr(a[i], name);
         if (!h) return fail();
         void *v = nullptr;
         if (PyLong_Check(h)) v = number(PyLong_AsUnsignedLongLongMask(h));
@@ -236,7 +237,7 @@ PyObject *result(int rc)
 
 // What follows the conversions: the library call without the interpreter lock, or, where an argument is of another kind, the
 // same call through ctypes (which accepts or refuses it).
-enum Call { CONV2D, FC, DEPTHWISE, STACK, NORM, APPEND, ATTENTION, QUANTIZE, DEQUANTIZE, FC_MXFP4, CALLS };
+enum Call { CONV2D, FC, DEPTHWISE, STACK, NORM, APPEND, ATTENTION, QUANTIZE, DEQUANTIZE, FC_MXFP4, WRITE, READ, ATTENTION8, CHUNK, CALLS };
 PyObject *by_ctypes[CALLS]; // set by init()
 
 template <typename F> PyObject *finish(const Args &g, Call which, Py_ssize_t n, F call)
@@ -370,11 +371,12 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 // paged_attention(cache, q, y, heads, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream)
-PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+template <Call CALL> PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (!argc(n, 12)) return nullptr;
     Args g{a};
     const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
+    const npas_kv_scales *scales = CALL == ATTENTION8 ? (const npas_kv_scales *)g.handle(0, s_scales) : nullptr;
     const int heads = g.integer(3), most = g.integer(5), window = g.integer(7);
     const int64_t width = (int64_t)heads * (c ? c->head_dim : 0), sequences = c ? c->sequences : 0;
     const Args::Rows q = g.rows(1, width, sequences, 2);
@@ -383,8 +385,67 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     const size_t bytes = g.size(10);
     void *lse = g.words(8, sequences * heads, true), *w = g.buffer(9, bytes);
     void *st = g.address(11);
-    return finish(g, ATTENTION, n, [&] {
+    return finish(g, CALL, n, [&] {
+        if (CALL == ATTENTION8)
+            return npas_paged_attention8(c, scales, q.p, q.stride, y, (float *)lse, heads, (const int32_t *)len, most, window, scale, w, bytes, st);
         return npas_paged_attention(c, q.p, q.stride, y, (float *)lse, heads, (const int32_t *)len, most, window, scale, w, bytes, st);
+    });
+}
+
+// kv_write(cache, q, k, v, q_out, T, heads, positions, sequences, q_weight, k_weight, eps, cos_sin, rot_dim, kind, stream)
+PyObject *kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 16)) return nullptr;
+    Args g{a};
+    const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
+    const npas_kv_scales *scales = (const npas_kv_scales *)g.handle(0, s_scales);
+    const int T = g.integer(5), heads = g.integer(6), rot = g.integer(13), kind = g.integer(14);
+    const int64_t D = c ? c->head_dim : 0, kv = c ? c->kv_heads : 0;
+    const Args::Rows q = g.rows(1, heads * D, T, 2), k = g.rows(2, kv * D, T, 2), v = g.rows(3, kv * D, T, 2);
+    void *qo = g.elements(4, (int64_t)T * heads * D, 2), *pos = g.words(7, T, false), *seq = g.words(8, T, false);
+    void *qw = g.words(9, D, true), *kw = g.words(10, D, true);
+    const float eps = g.real(11);
+    const Args::Rows cs = g.rows_fp32(12, rot);
+    if (g.state == Args::PLAIN && cs.stride != rot) g.refuse("cos_sin is not contiguous");
+    void *st = g.address(15);
+    return finish(g, WRITE, n, [&] {
+        return npas_kv_write(c, scales, q.p, q.stride, k.p, k.stride, v.p, v.stride, qo, T, heads, (const int32_t *)seq, (const int32_t *)pos,
+                             (const float *)qw, (const float *)kw, eps, (const float *)cs.p, (int)(cs.count > 0x7fffffff ? 0x7fffffff : cs.count), rot,
+                             (npas_rotation)kind, st);
+    });
+}
+
+// kv_read(cache, k, v, T, positions, sequences, stream)
+PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 7)) return nullptr;
+    Args g{a};
+    const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
+    const npas_kv_scales *scales = (const npas_kv_scales *)g.handle(0, s_scales);
+    const int T = g.integer(3);
+    const int64_t count = (int64_t)T * (c ? (int64_t)c->kv_heads * c->head_dim : 0);
+    void *k = g.elements(1, count, 2), *v = g.elements(2, count, 2), *pos = g.words(4, T, false), *seq = g.words(5, T, false), *st = g.address(6);
+    return finish(g, READ, n, [&] { return npas_kv_read(c, scales, k, v, T, (const int32_t *)seq, (const int32_t *)pos, st); });
+}
+
+// chunk_attention(cache, q, y, T, heads, starts, lengths, max_length, scale, window, lse, workspace, workspace_bytes, stream)
+PyObject *chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!argc(n, 14)) return nullptr;
+    Args g{a};
+    const npas_kv_cache *c = (const npas_kv_cache *)g.handle(0);
+    const npas_kv_scales *scales = (const npas_kv_scales *)g.handle(0, s_scales);
+    const int T = g.integer(3), heads = g.integer(4), most = g.integer(7), window = g.integer(9);
+    const int64_t width = (int64_t)heads * (c ? c->head_dim : 0), sequences = c ? c->sequences : 0;
+    const Args::Rows q = g.rows(1, width, T, 2);
+    void *y = g.elements(2, T * width, 2), *start = g.words(5, sequences + 1, false), *len = g.words(6, sequences, false);
+    const float scale = g.real(8);
+    const size_t bytes = g.size(12);
+    void *lse = g.words(10, (int64_t)T * heads, true), *w = g.buffer(11, bytes);
+    void *st = g.address(13);
+    return finish(g, CHUNK, n, [&] {
+        return npas_chunk_attention(c, scales, q.p, q.stride, y, (float *)lse, T, heads, (const int32_t *)start, (const int32_t *)len, most, window,
+                                    scale, w, bytes, st);
     });
 }
 
@@ -450,7 +511,11 @@ PyMethodDef methods[] = {
     {"run_stack", (PyCFunction)(void (*)(void))run_stack, METH_FASTCALL, nullptr},
     {"gated_residual_norm", (PyCFunction)(void (*)(void))gated_residual_norm, METH_FASTCALL, nullptr},
     {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, nullptr},
-    {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, nullptr},
+    {"paged_attention", (PyCFunction)(void (*)(void))attention<ATTENTION>, METH_FASTCALL, nullptr},
+    {"paged_attention8", (PyCFunction)(void (*)(void))attention<ATTENTION8>, METH_FASTCALL, nullptr},
+    {"kv_write", (PyCFunction)(void (*)(void))kv_write, METH_FASTCALL, nullptr},
+    {"kv_read", (PyCFunction)(void (*)(void))kv_read, METH_FASTCALL, nullptr},
+    {"chunk_attention", (PyCFunction)(void (*)(void))chunk_attention, METH_FASTCALL, nullptr},
     {"mxfp4_quantize", (PyCFunction)(void (*)(void))mxfp4_quantize, METH_FASTCALL, nullptr},
     {"mxfp4_dequantize", (PyCFunction)(void (*)(void))mxfp4_dequantize, METH_FASTCALL, nullptr},
     {"fc_mxfp4", (PyCFunction)(void (*)(void))fc_mxfp4, METH_FASTCALL, nullptr},
@@ -463,6 +528,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycalls", nullptr, -1, methods, n
 PyMODINIT_FUNC PyInit__pycalls()
 {
     s_handle = PyUnicode_InternFromString("handle");
+    s_scales = PyUnicode_InternFromString("scales");
     s_value = PyUnicode_InternFromString("value");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
@@ -471,6 +537,6 @@ PyMODINIT_FUNC PyInit__pycalls()
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_itemsize = PyUnicode_InternFromString("itemsize");
     s_dtype = PyUnicode_InternFromString("dtype");
-    if (!s_handle || !s_value || !s_is_contiguous || !s_data_ptr || !s_shape || !s_stride || !s_nbytes || !s_itemsize || !s_dtype) return nullptr;
+    if (!s_handle || !s_scales || !s_value || !s_is_contiguous || !s_data_ptr || !s_shape || !s_stride || !s_nbytes || !s_itemsize || !s_dtype) return nullptr;
     return PyModule_Create(&module);
 }
