@@ -31,6 +31,14 @@ template <int DT> __device__ __forceinline__ bool not_finite2(uint32_t w)
     return (w & e) == e || (w >> 16 & e) == e;
 }
 
+// The largest of three, one instruction; a NaN is left out, as fmaxf leaves it.
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+
 // Tile of a workgroup: BM rows (token, query head of the key head) of one sequence.
 struct Tile {
     int s, token0, row0, rows; // sequence, its first row of q, first row of the tile and rows from there on within the run
@@ -64,46 +72,45 @@ template <int BM> __device__ __forceinline__ bool find_tile(const ChunkArgs &a, 
     return t.rows > 0;
 }
 
-// One workgroup a (tile of BM = 32 WM rows, key head, cut).  A wave has 32 rows as columns of 32 x 32 x 16 matrix instructions and walks the tokens in steps of
-// 32 NSUB: scores S = K Q^T (row operand: keys from LDS as they lie), running maximum and sum a column, O^T = V^T P^T, where the weights
+// One workgroup a (tile of BM = 32 WAVES rows, key head, cut).  A wave has 32 rows as columns of 32 x 32 x 16 matrix instructions and walks the tokens in steps of
+// BN = 32 NSUB: scores S = K Q^T (row operand: keys from LDS as they lie), running maximum and sum a column, O^T = V^T P^T, where the weights
 // are the column operand as the first product leaves them, if a step's tokens are counted so that a lane's half h has tokens 4 h .. 4 h + 3 of
-// each eight; the values come out of LDS turned round.  WK waves side by side take different tokens of a step and are joined at the end.
+// each eight; the values come out of LDS turned round.
 // Keys and values of a step come through registers into one of two places in LDS (16-byte pieces in an order that spreads rows over the banks; 8-bit
 // floats become 16-bit numbers on the way) while the other is multiplied; the cache rows of the tokens are looked up two steps ahead.
-template <int DT, bool E8, int ND, int NSUB, int WM, int WK>
-__global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chunk_attention_kernel(ChunkArgs a, int places)
+// The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled.
+template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a, int places)
 {
-    constexpr int DP = 32 * ND, BM = 32 * WM, BN = 32 * NSUB * WK, THREADS = 64 * WM * WK, PIECES = DP / 8, STRIDE = DP * 2;
+    constexpr int DP = 32 * ND, BM = 32 * WAVES, BN = 32 * NSUB, THREADS = 64 * WAVES, PIECES = DP / 8, STRIDE = DP * 2;
     constexpr int UNITS = E8 ? BN * PIECES / 2 : BN * PIECES, PER = (UNITS + THREADS - 1) / THREADS, IN_ROW = E8 ? PIECES / 2 : PIECES;
-    constexpr float TOP = DT == NPAS_BF16 ? 0.f : 15.f; // the largest weight is 2^TOP: fp16 reaches down to 2^-24 only
-    __shared__ __align__(16) uint8_t kv[2][2][BN * STRIDE]; // [place][keys, values]
-    __shared__ uint32_t ring[3][BN];
-    __shared__ uint32_t gone[3][(BN + 63) / 64 * 2]; // a bit a token: not there
-    __shared__ float stat[2][WK][32];
+    constexpr float GROW = DT == NPAS_BF16 ? 8.f : 4.f, TOP = DT == NPAS_BF16 ? 0.f : 11.f; // a weight is at most 2^(TOP + GROW)
+    __shared__ __align__(16) uint8_t kbuf[2][BN * STRIDE], vbuf[2][BN * STRIDE];
+    __shared__ uint32_t ring[3][BN], gone[3][NSUB]; // cache rows of a step's tokens; a bit a token that is not there
+    __shared__ uint32_t odd[2]; // values of a step hold an infinity or a NaN, and not every row sees every token
     auto swizzle = [](int row) { return ND == 2 ? (row >> 1 & 3) * 2 : ND == 3 ? (row >> 2 & 1) * 2 : (row & 7) * 2; };
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % WM, wk = wave / WM, r = lane & 31, h = lane >> 5, D = a.c.head_dim;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, D = a.c.head_dim;
     const int group = a.heads / a.c.kv_heads;
     uint32_t id = blockIdx.x;
-    const int head0 = id % a.c.kv_heads * group, kvh = id % a.c.kv_heads;
+    const int kvh = id % a.c.kv_heads, head0 = kvh * group;
     id /= a.c.kv_heads;
     const int cut = id % a.splits, place = places - 1 - (int)(id / a.splits); // (the last tiles of a run have most to do)
     Tile t;
     if (!find_tile<BM>(a, place, group, t)) return;
 
     // the lane's row
-    const int row = 32 * wm + r;
+    const int row = 32 * wave + r;
     const bool real = row < t.rows;
     const int in_run = t.row0 + (real ? row : 0), token = in_run / group, head = head0 + in_run - token * group;
     const int at = t.at0 + token; // its position
     const size_t out_row = (size_t)(t.token0 + token) * a.heads + head;
     // tokens that some row of the tile sees, and this cut's share
-    const int last_row = min(t.rows, BM) - 1;
-    const int end = max(0, t.at0 + (t.row0 + last_row) / group + 1), from0 = a.window > 0 ? max(0, t.at0 + t.row0 / group - a.window + 1) : 0;
-    const long skip = (long)cut * a.chunk;
-    const int from = (int)min((long)end, from0 + skip), to = (int)min((long)end, (long)from + a.chunk);
+    const int last_row = min(t.rows, BM) - 1, at_first = t.at0 + t.row0 / group, at_last = t.at0 + (t.row0 + last_row) / group;
+    const int end = max(0, at_last + 1), from0 = a.window > 0 ? max(0, at_first - a.window + 1) : 0;
+    const int from = (int)min((long)end, from0 + (long)cut * a.chunk), to = (int)min((long)end, (long)from + a.chunk);
     const int steps = (to - from + BN - 1) / BN;
 
     uint4 qf[2 * ND];
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
     for (int c = 0; c < 2 * ND; ++c) {
         const int d = 16 * c + 8 * h;
@@ -111,10 +118,11 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
         if (real && d < D) {
             struct __attribute__((packed, aligned(2))) Words { uint32_t w[4]; };
             const Words x = *reinterpret_cast<const Words *>(reinterpret_cast<const uint16_t *>(a.q) + (size_t)(t.token0 + token) * a.q_stride + (size_t)head * D + d);
-            qf[c] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+            qf[c] = make_uint4(x.w[0] ^ sign, x.w[1] ^ sign, x.w[2] ^ sign, x.w[3] ^ sign);
         }
     }
-    const float to2 = a.scale * 1.4426950408889634f; // scores in powers of two
+    // scores in powers of two; positive, so that a score that is left out can be minus infinity throughout
+    const float to2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, FLT_MIN);
     f32x16 o[ND] = {};
     float m = -INFINITY, l = 0.f;
 
@@ -129,7 +137,15 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
         const bool there = (uint32_t)page < (uint32_t)a.c.pages;
         if (threadIdx.x < BN) ring[i % 3][threadIdx.x] = there ? ((uint32_t)page * a.c.kv_heads + kvh) * a.c.page_size + j % (uint32_t)a.c.page_size : kAbsent;
         const uint64_t none = ~__ballot(there);
-        if (lane == 0) gone[i % 3][2 * wave] = (uint32_t)none, gone[i % 3][2 * wave + 1] = (uint32_t)(none >> 32);
+        if (lane == 0) {
+            gone[i % 3][2 * wave] = (uint32_t)none;
+            if (NSUB > 1) gone[i % 3][2 * wave + 1] = (uint32_t)(none >> 32);
+        }
+    };
+    // whether a row of the workgroup does not see a token of step i that another sees
+    auto parted = [&](int i) __attribute__((always_inline)) {
+        const long base = (long)from + (long)i * BN;
+        return base + BN - 1 > at_first || (a.window > 0 && base <= (long)at_last - a.window);
     };
     uint4 in[2][PER];
     uint32_t scale8[2][E8 ? PER : 1], absent; // absent: a bit a unit
@@ -138,8 +154,7 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, d = (n - key * IN_ROW) * (E8 ? 16 : 8);
-            const bool used = UNITS % THREADS == 0 || n < UNITS;
-            const uint32_t row = used ? ring[i % 3][key] : kAbsent;
+            const uint32_t row = UNITS % THREADS == 0 || n < UNITS ? ring[i % 3][key] : kAbsent;
             const bool there = row != kAbsent && d < D;
             if (!there) absent |= 1u << u;
             const uint64_t at = (uint64_t)(there ? row : 0u) * D + (there ? d : 0);
@@ -151,140 +166,150 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
         }
     };
     auto store = [&](int i) __attribute__((always_inline)) {
+        if (__any(absent)) { // another's row, or the padding of a head
+            asm volatile("" : : : "memory");
+#pragma unroll
+            for (int u = 0; u < PER; ++u)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (absent >> u & 1) {
+                        in[x][u] = make_uint4(0, 0, 0, 0);
+                        if constexpr (E8) scale8[x][u] = 127;
+                    }
+        }
+        if (parted(i)) {
+            bool bad = false;
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const uint4 w = in[1][u];
+                if constexpr (E8) bad = bad || scale8[1][u] == 255;
+                else bad = bad || not_finite2<DT>(w.x) || not_finite2<DT>(w.y) || not_finite2<DT>(w.z) || not_finite2<DT>(w.w);
+            }
+            if (bad) odd[i & 1] = 1;
+        }
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, p = (n - key * IN_ROW) * (E8 ? 2 : 1);
             if (UNITS % THREADS && n >= UNITS) continue;
-            const bool none = absent >> u & 1;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                uint8_t *row = kv[i & 1][x] + key * STRIDE;
-                uint4 w = in[x][u];
-                if (none) w = make_uint4(0, 0, 0, 0);
+                uint8_t *to = (x ? vbuf : kbuf)[i & 1] + key * STRIDE;
+                const uint4 w = in[x][u];
                 if constexpr (E8) {
-                    const uint32_t byte = none ? 127u : scale8[x][u];
-                    *reinterpret_cast<uint4 *>(row + ((p ^ swizzle(key)) << 4)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), byte);
-                    *reinterpret_cast<uint4 *>(row + (((p + 1) ^ swizzle(key)) << 4)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), byte);
-                } else *reinterpret_cast<uint4 *>(row + ((p ^ swizzle(key)) << 4)) = w;
+                    *reinterpret_cast<uint4 *>(to + ((p ^ swizzle(key)) << 4)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), scale8[x][u]);
+                    *reinterpret_cast<uint4 *>(to + (((p + 1) ^ swizzle(key)) << 4)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), scale8[x][u]);
+                } else *reinterpret_cast<uint4 *>(to + ((p ^ swizzle(key)) << 4)) = w;
             }
         }
     };
-    auto value_columns = [&](const uint8_t *vb, int key0, int dt, int part) __attribute__((always_inline)) {
-        const int key = key0 + 8 * part + 4 * h + (lane >> 2 & 3), p = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-        return read_columns(vb + key * STRIDE + ((p ^ swizzle(key)) << 4) + (lane & 1) * 8);
+    // the tokens of 32 from step i's sub-step u that the lane's row sees, a bit each
+    auto seen = [&](int i, int u) __attribute__((always_inline)) {
+        const long base = (long)from + (long)i * BN + 32 * u, past = at - base, before = a.window > 0 ? at - a.window + 1 - base : 0;
+        uint32_t bits = ~gone[i % 3][u];
+        if (past < 31) bits &= past < 0 ? 0u : (2u << past) - 1u;
+        if (before > 0) bits &= before > 31 ? 0u : ~0u << before;
+        return bits;
+    };
+    // Values that are infinite or NaN in a step that not every row sees, where a weight of zero would make them NaN: added to the rows that see them, and zero for the products.
+    auto part_values = [&](int i) __attribute__((always_inline)) {
+        uint8_t *buf = vbuf[i & 1];
+#pragma unroll 1
+        for (int n = 0; n < BN; ++n) {
+            const bool see = seen(i, n >> 5) >> (n & 31) & 1;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint2 v = *reinterpret_cast<const uint2 *>(buf + n * STRIDE + (((4 * dt + x) ^ swizzle(n)) << 4) + 8 * h);
+                    const uint32_t w[2] = {v.x, v.y};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float y = from_storage<DT>((uint16_t)(w[k >> 1] >> 16 * (k & 1)));
+                        o[dt][4 * x + k] += see && !(fabsf(y) < INFINITY) ? y : 0.f;
+                    }
+                }
+        }
+        __syncthreads();
+        for (int n = threadIdx.x; n < BN * STRIDE / 4; n += THREADS) {
+            uint32_t &w = reinterpret_cast<uint32_t *>(buf)[n];
+            constexpr uint32_t e = DT == NPAS_BF16 ? 0x7f80u : 0x7c00u;
+            if ((w & e) == e) w &= 0xffff0000u;
+            if ((w >> 16 & e) == e) w &= 0xffffu;
+        }
+        if (threadIdx.x == 0) odd[i & 1] = 0;
+        __syncthreads();
     };
     auto compute = [&](int i) __attribute__((always_inline)) {
-        const uint8_t *kb = kv[i & 1][0], *vb = kv[i & 1][1];
+        const uint8_t *kb = kbuf[i & 1], *vb = vbuf[i & 1];
         f32x16 sc[NSUB];
 #pragma unroll
-        for (int u = 0; u < NSUB; ++u) {
-            sc[u] = f32x16{};
-            const int key = 32 * (wk * NSUB + u) + r;
+        for (int u = 0; u < NSUB; ++u) sc[u] = f32x16{};
 #pragma unroll
-            for (int c = 0; c < 2 * ND; ++c) {
-                const uint4 kf = *reinterpret_cast<const uint4 *>(kb + key * STRIDE + (((2 * c + h) ^ swizzle(key)) << 4));
-                sc[u] = mfma32<DT>(kf, qf[c], sc[u]);
-            }
-        }
-        float top = -INFINITY;
-        uint32_t seen[NSUB]; // a bit a token of the 32
-        bool all = true;
-#pragma unroll
-        for (int u = 0; u < NSUB; ++u) {
-            const int sub = wk * NSUB + u;
-            const long base = (long)from + (long)i * BN + 32 * sub, past = at - base, before = a.window > 0 ? at - a.window + 1 - base : 0;
-            uint32_t bits = ~gone[i % 3][sub];
-            if (past < 31) bits &= past < 0 ? 0u : (2u << past) - 1u;
-            if (before > 0) bits &= before > 31 ? 0u : ~0u << before;
-            seen[u] = bits;
-            all = all && bits == ~0u;
-        }
-        const bool whole = __all(all);
-#pragma unroll
-        for (int u = 0; u < NSUB; ++u)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) sc[u][k] *= to2;
-        if (!whole)
+        for (int c = 0; c < 2 * ND; ++c)
 #pragma unroll
             for (int u = 0; u < NSUB; ++u) {
-                const uint32_t bits = seen[u] >> 4 * h;
+                const int key = 32 * u + r;
+                sc[u] = mfma32<DT>(*reinterpret_cast<const uint4 *>(kb + key * STRIDE + (((2 * c + h) ^ swizzle(key)) << 4)), qf[c], sc[u]);
+            }
+        uint32_t none = 0;
+#pragma unroll
+        for (int u = 0; u < NSUB; ++u) none |= gone[i % 3][u];
+        if (parted(i) || __builtin_amdgcn_readfirstlane(none)) {
+            asm volatile("" : : : "memory");
+#pragma unroll
+            for (int u = 0; u < NSUB; ++u) {
+                const uint32_t bits = seen(i, u) >> 4 * h;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) sc[u][k] = bits >> (8 * (k >> 2) + (k & 3)) & 1 ? sc[u][k] : -INFINITY;
             }
+        }
+        float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < NSUB; ++u)
 #pragma unroll
-            for (int k = 0; k < 16; ++k) top = fmaxf(top, sc[u][k]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m)) { // (an infinite score has an infinite weight, and so has the sum: finite maxima keep these from being NaN)
-            const float now = fminf(fmaxf(m, top), FLT_MAX), c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+            for (int k = 0; k < 16; k += 2) top = max3(top, sc[u][k], sc[u][k + 1]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * to2;
+        float mul = to2;
+        if (__any(fabsf(top) > 0x1p20f && top != -INFINITY)) { // (where a product's rounding would count in the exponent)
+            asm volatile("" : : : "memory");
+#pragma unroll
+            for (int u = 0; u < NSUB; ++u) sc[u] *= to2;
+            mul = 1.f;
+        }
+        if (__any(top > m + GROW)) { // (an infinite score has an infinite weight, and so has the sum: finite maxima keep these from being NaN)
+            const float now = fminf(fmaxf(m, top), FLT_MAX), c = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
             m = now;
             l *= c;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] *= c;
         }
         const float base = m == -INFINITY ? 0.f : m - TOP;
-        uint4 pf[2 * NSUB];
 #pragma unroll
-        for (int u = 0; u < NSUB; ++u) {
+        for (int u = 0; u < NSUB; ++u)
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                sc[u][k] = __builtin_amdgcn_exp2f(sc[u][k] - base);
-                l += sc[u][k];
-            }
+            for (int x = 0; x < 2; ++x) {
+                float p[8];
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                pf[2 * u + x] = make_uint4(pack2<DT>(sc[u][8 * x], sc[u][8 * x + 1]), pack2<DT>(sc[u][8 * x + 2], sc[u][8 * x + 3]),
-                                           pack2<DT>(sc[u][8 * x + 4], sc[u][8 * x + 5]), pack2<DT>(sc[u][8 * x + 6], sc[u][8 * x + 7]));
-        }
-        // A weight of zero times an infinity would be NaN in rows that do not see the token: such values are added one by one.
-        bool odd = false;
-        if (!whole)
-#pragma unroll
-            for (int u = 0; u < 2 * NSUB; ++u)
-#pragma unroll
-                for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const uint2 v = value_columns(vb, 32 * wk * NSUB + 16 * u, dt, x);
-                        odd = odd || not_finite2<DT>(v.x) || not_finite2<DT>(v.y);
-                    }
-        if (!__any(odd)) {
-#pragma unroll
-            for (int u = 0; u < 2 * NSUB; ++u)
+                for (int k = 0; k < 8; ++k) {
+                    p[k] = __builtin_amdgcn_exp2f(fmaf(sc[u][8 * x + k], mul, -base));
+                    l += p[k];
+                }
+                const uint4 pf = make_uint4(pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7]));
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) {
-                    const uint2 v0 = value_columns(vb, 32 * wk * NSUB + 16 * u, dt, 0), v1 = value_columns(vb, 32 * wk * NSUB + 16 * u, dt, 1);
-                    o[dt] = mfma32<DT>(make_uint4(v0.x, v0.y, v1.x, v1.y), pf[u], o[dt]);
+                    uint2 v[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int key = 32 * u + 16 * x + 8 * y + 4 * h + (lane >> 2 & 3), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+                        v[y] = read_columns(vb + key * STRIDE + ((piece ^ swizzle(key)) << 4) + (lane & 1) * 8);
+                    }
+                    o[dt] = mfma32<DT>(make_uint4(v[0].x, v[0].y, v[1].x, v[1].y), pf, o[dt]);
                 }
-        } else {
-#pragma unroll
-            for (int u = 0; u < NSUB; ++u)
-#pragma unroll 1
-                for (int n = 0; n < 32; ++n) {
-                    float p = 0.f; // the weight of token n: in half n >> 2 & 1, register 4 (n >> 3) + (n & 3)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) p = k == 4 * (n >> 3) + (n & 3) ? sc[u][k] : p;
-                    p = __shfl(p, r + 32 * (n >> 2 & 1));
-                    const bool see = seen[u] >> n & 1;
-                    const int key = 32 * (wk * NSUB + u) + n;
-#pragma unroll
-                    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const uint2 v = *reinterpret_cast<const uint2 *>(vb + key * STRIDE + (((4 * dt + g) ^ swizzle(key)) << 4) + 8 * h);
-                            const uint32_t w[2] = {v.x, v.y};
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const float x = from_storage<DT>((uint16_t)(w[k >> 1] >> 16 * (k & 1)));
-                                o[dt][4 * g + k] += see ? p * x : 0.f;
-                            }
-                        }
-                }
-        }
+            }
     };
 
     if (steps > 0) {
+        if (threadIdx.x < 2) odd[threadIdx.x] = 0;
         look_up(0, page_of(0));
         look_up(1, page_of(1));
         __syncthreads();
@@ -292,6 +317,7 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
         store(0);
         for (int i = 0; i < steps; ++i) {
             __syncthreads();
+            if (__builtin_amdgcn_readfirstlane(odd[i & 1])) part_values(i);
             const int page = page_of(i + 2);
             if (i + 1 < steps) load(i + 1);
             compute(i);
@@ -300,45 +326,6 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
         }
     }
     l += __shfl_xor(l, 32);
-    if constexpr (WK > 1) {
-        // the side-by-side waves' sums, rescaled to the largest maximum and added in the waves' order; columns lie in LDS
-        static_assert(WM * WK * 32 * DP * 4 <= sizeof(kv), "the sums fit where keys and values were");
-        auto sums = [&](int w, int dt, int g) { // four of the lane's, in an order that spreads columns over the banks
-            return reinterpret_cast<float4 *>(kv) + (w * 32 + r) * (DP / 4) + ((8 * dt + 2 * g + h) ^ (r & 7));
-        };
-        __syncthreads(); // (the last step's readers are done)
-        if (h == 0) stat[0][wave][r] = m;
-        __syncthreads();
-        float top = stat[0][wm][r];
-#pragma unroll
-        for (int w = 1; w < WK; ++w) top = fmaxf(top, stat[0][w * WM + wm][r]);
-        const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *sums(wave, dt, g) = make_float4(c * o[dt][4 * g], c * o[dt][4 * g + 1], c * o[dt][4 * g + 2], c * o[dt][4 * g + 3]);
-        if (h == 0) stat[1][wave][r] = c * l;
-        __syncthreads();
-        if (wk) return;
-        m = top;
-        l = 0.f;
-#pragma unroll
-        for (int w = 0; w < WK; ++w) l += stat[1][w * WM + wm][r];
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < WK; ++w) {
-                    const float4 v = *sums(w * WM + wm, dt, g);
-                    sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-                }
-                o[dt][4 * g] = sum.x, o[dt][4 * g + 1] = sum.y, o[dt][4 * g + 2] = sum.z, o[dt][4 * g + 3] = sum.w;
-            }
-        }
-    }
     if (!real) return;
     if (a.splits > 1) {
         float *part = a.part + (out_row * a.splits + cut) * D;
@@ -350,7 +337,7 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
                     const int d = 32 * dt + 8 * g + 4 * h;
                     if (d < D) *reinterpret_cast<float4 *>(part + d) = make_float4(o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]);
                 }
-        if (h == 0) a.part_stat[out_row * a.splits + cut] = make_float2(m, l);
+        if (h == 0) a.part_stat[out_row * a.splits + cut] = make_float2(m - TOP, l);
         return;
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -370,7 +357,6 @@ __global__ __launch_bounds__(64 * WM * WK, ND <= 4 && WK == 1 ? 2 : 1) void chun
 // One wave a row: the cuts' sums, rescaled to the largest maximum and added in their order.
 template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_kernel(ChunkArgs a)
 {
-    constexpr float TOP = DT == NPAS_BF16 ? 0.f : 15.f;
     const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, D = a.c.head_dim;
     if (row >= (size_t)a.T * a.heads) return;
@@ -397,10 +383,10 @@ template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_ke
     struct __attribute__((packed, aligned(2))) Words { uint32_t w[2]; };
     if (lane * 4 < D)
         *reinterpret_cast<Words *>(reinterpret_cast<uint16_t *>(a.y) + row * D + lane * 4) = Words{{pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv)}};
-    if (lane == 0 && a.lse) a.lse[row] = l != 0.f ? (m - TOP + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (lane == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-int chunk_tile_rows(int head_dim, int few) { return few ? (head_dim <= 128 ? 32 : 64) : 128; }
+int chunk_tile_rows(int head_dim, int few) { return 128; }
 
 int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream)
 {
@@ -414,9 +400,8 @@ int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream)
         constexpr bool E8 = decltype(e8c)::value;
         auto width = [&](auto ndc) {
             constexpr int ND = decltype(ndc)::value;
-            if (!a.few) hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, ND <= 4 ? 2 : 1, 4, 1>), grid, block, 0, st, a, (int)places);
-            else if constexpr (ND <= 4) hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, 1, 1, 4>), grid, block, 0, st, a, (int)places);
-            else hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, 1, 2, 2>), grid, block, 0, st, a, (int)places);
+            if constexpr (ND <= 4) hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, 2, 4, 2>), grid, block, 0, st, a, (int)places);
+            else hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, 1, 4, 1>), grid, block, 0, st, a, (int)places);
         };
         if (D <= 64) width(std::integral_constant<int, 2>{});
         else if (D <= 96) width(std::integral_constant<int, 3>{});
