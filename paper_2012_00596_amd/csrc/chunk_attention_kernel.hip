@@ -87,7 +87,9 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
     __shared__ __align__(16) uint8_t kbuf[2][BN * STRIDE], vbuf[2][BN * STRIDE];
     __shared__ uint32_t ring[3][BN], gone[3][NSUB]; // cache rows of a step's tokens; a bit a token that is not there
     __shared__ uint32_t odd[2]; // values of a step hold an infinity or a NaN, and not every row sees every token
-    auto swizzle = [](int row) { return ND == 2 ? (row >> 1 & 3) * 2 : ND == 3 ? (row >> 2 & 1) * 2 : (row & 7) * 2; };
+    // Where a row's pieces lie, so that what a read takes at once is spread over all banks: keys are read one piece of 16 rows, values two or four of 4 or 8.
+    auto key_piece = [](int row, int p) { return (p ^ (ND == 2 ? row >> 1 & 7 : ND == 3 ? row >> 2 & 3 : row & 15)) << 4; };
+    auto value_piece = [](int row, int p) { return (p ^ ((ND == 2 ? (row >> 1 & 1) * 4 : ND == 3 ? 0 : (row & 3) * 4) + (row >> 2 & 1) * 2)) << 4; };
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, D = a.c.head_dim;
     const int group = a.heads / a.c.kv_heads;
     uint32_t id = blockIdx.x;
@@ -194,11 +196,12 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint8_t *to = (x ? vbuf : kbuf)[i & 1] + key * STRIDE;
+                auto piece = [&](int p) { return x ? value_piece(key, p) : key_piece(key, p); };
                 const uint4 w = in[x][u];
                 if constexpr (E8) {
-                    *reinterpret_cast<uint4 *>(to + ((p ^ swizzle(key)) << 4)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), scale8[x][u]);
-                    *reinterpret_cast<uint4 *>(to + (((p + 1) ^ swizzle(key)) << 4)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), scale8[x][u]);
-                } else *reinterpret_cast<uint4 *>(to + ((p ^ swizzle(key)) << 4)) = w;
+                    *reinterpret_cast<uint4 *>(to + piece(p)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), scale8[x][u]);
+                    *reinterpret_cast<uint4 *>(to + piece(p + 1)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), scale8[x][u]);
+                } else *reinterpret_cast<uint4 *>(to + piece(p)) = w;
             }
         }
     };
@@ -220,7 +223,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const uint2 v = *reinterpret_cast<const uint2 *>(buf + n * STRIDE + (((4 * dt + x) ^ swizzle(n)) << 4) + 8 * h);
+                    const uint2 v = *reinterpret_cast<const uint2 *>(buf + n * STRIDE + value_piece(n, 4 * dt + x) + 8 * h);
                     const uint32_t w[2] = {v.x, v.y};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -249,7 +252,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
 #pragma unroll
             for (int u = 0; u < NSUB; ++u) {
                 const int key = 32 * u + r;
-                sc[u] = mfma32<DT>(*reinterpret_cast<const uint4 *>(kb + key * STRIDE + (((2 * c + h) ^ swizzle(key)) << 4)), qf[c], sc[u]);
+                sc[u] = mfma32<DT>(*reinterpret_cast<const uint4 *>(kb + key * STRIDE + key_piece(key, 2 * c + h)), qf[c], sc[u]);
             }
         uint32_t none = 0;
 #pragma unroll
@@ -301,7 +304,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const int key = 32 * u + 16 * x + 8 * y + 4 * h + (lane >> 2 & 3), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-                        v[y] = read_columns(vb + key * STRIDE + ((piece ^ swizzle(key)) << 4) + (lane & 1) * 8);
+                        v[y] = read_columns(vb + key * STRIDE + value_piece(key, piece) + (lane & 1) * 8);
                     }
                     o[dt] = mfma32<DT>(make_uint4(v[0].x, v[0].y, v[1].x, v[1].y), pf, o[dt]);
                 }
