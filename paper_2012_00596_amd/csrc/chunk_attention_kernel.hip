@@ -39,6 +39,13 @@ __device__ __forceinline__ float max3(float x, float y, float z)
     return r;
 }
 
+// The larger of a lane's and its partner's in the other half of the wave.
+__device__ __forceinline__ float over_halves(float x)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
 // Tile of a workgroup: BM rows (token, query head of the key head) of one sequence.
 struct Tile {
     int s, token0, row0, rows; // sequence, its first row of q, first row of the tile and rows from there on within the run
@@ -85,7 +92,8 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
     constexpr int UNITS = E8 ? BN * PIECES / 2 : BN * PIECES, PER = (UNITS + THREADS - 1) / THREADS, IN_ROW = E8 ? PIECES / 2 : PIECES;
     constexpr float GROW = DT == NPAS_BF16 ? 8.f : 4.f, TOP = DT == NPAS_BF16 ? 0.f : 11.f; // a weight is at most 2^(TOP + GROW)
     __shared__ __align__(16) uint8_t kbuf[2][BN * STRIDE], vbuf[2][BN * STRIDE];
-    __shared__ uint32_t ring[3][BN], gone[3][NSUB]; // cache rows of a step's tokens; a bit a token that is not there
+    constexpr int AHEAD = THREADS / BN; // steps whose tokens are looked up at once, one a thread
+    __shared__ uint32_t ring[2][THREADS], gone[2][THREADS / 32], holes[2][AHEAD]; // cache rows of tokens; a bit a token that is not there; whether a step has such
     __shared__ uint32_t odd[2]; // values of a step hold an infinity or a NaN, and not every row sees every token
     // Where a row's pieces lie, so that what a read takes at once is spread over all banks: keys are read one piece of 16 rows, values two or four of 4 or 8.
     auto key_piece = [](int row, int p) { return (p ^ (ND == 2 ? row >> 1 & 7 : ND == 3 ? row >> 2 & 3 : row & 15)) << 4; };
@@ -128,46 +136,70 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
     f32x16 o[ND] = {};
     float m = -INFINITY, l = 0.f;
 
-    // Tokens of step i: the cache rows of those that are there.
-    auto page_of = [&](int i) __attribute__((always_inline)) {
-        const long j = (long)from + (long)i * BN + threadIdx.x;
-        return threadIdx.x < BN && j < to ? a.c.table[(size_t)t.s * a.c.table_stride + (uint32_t)j / (uint32_t)a.c.page_size] : -1;
+    // Tokens of the steps AHEAD n .. : the cache rows of those that are there.
+    auto page_of = [&](int n) __attribute__((always_inline)) {
+        const long j = (long)from + (long)n * THREADS + threadIdx.x;
+        return j < to ? a.c.table[(size_t)t.s * a.c.table_stride + (uint32_t)j / (uint32_t)a.c.page_size] : -1;
     };
-    auto look_up = [&](int i, int page) __attribute__((always_inline)) {
-        if (threadIdx.x >= (BN + 63) / 64 * 64) return;
-        const uint32_t j = (uint32_t)from + (uint32_t)i * BN + threadIdx.x;
+    auto look_up = [&](int n, int page) __attribute__((always_inline)) {
+        const uint32_t j = (uint32_t)from + (uint32_t)n * THREADS + threadIdx.x;
         const bool there = (uint32_t)page < (uint32_t)a.c.pages;
-        if (threadIdx.x < BN) ring[i % 3][threadIdx.x] = there ? ((uint32_t)page * a.c.kv_heads + kvh) * a.c.page_size + j % (uint32_t)a.c.page_size : kAbsent;
+        ring[n & 1][threadIdx.x] = there ? ((uint32_t)page * a.c.kv_heads + kvh) * a.c.page_size + j % (uint32_t)a.c.page_size : kAbsent;
         const uint64_t none = ~__ballot(there);
         if (lane == 0) {
-            gone[i % 3][2 * wave] = (uint32_t)none;
-            if (NSUB > 1) gone[i % 3][2 * wave + 1] = (uint32_t)(none >> 32);
+            gone[n & 1][2 * wave] = (uint32_t)none;
+            gone[n & 1][2 * wave + 1] = (uint32_t)(none >> 32);
+            if (BN == 64) holes[n & 1][wave] = none != 0;
+            else holes[n & 1][2 * wave] = (uint32_t)none, holes[n & 1][2 * wave + 1] = (uint32_t)(none >> 32);
         }
     };
+    auto rows_of = [&](int i) { return ring[i / AHEAD & 1] + i % AHEAD * BN; };
     // whether a row of the workgroup does not see a token of step i that another sees
     auto parted = [&](int i) __attribute__((always_inline)) {
         const long base = (long)from + (long)i * BN;
         return base + BN - 1 > at_first || (a.window > 0 && base <= (long)at_last - a.window);
     };
-    uint4 in[2][PER];
+    uint4 in[2][E8 ? PER : 1];
     uint32_t scale8[2][E8 ? PER : 1], absent; // absent: a bit a unit
+    // 16 bits: straight into LDS, a wave 64 pieces at a time as they lie there; what is not there is another token's, and left out of scores and sums.
+    typedef __attribute__((address_space(3))) uint8_t lds_u8;
+    auto load16 = [&](int i) __attribute__((always_inline)) {
+        static_assert(E8 || UNITS % THREADS == 0, "every thread has as many pieces");
+        uint32_t rows[PER];
+#pragma unroll
+        for (int u = 0; u < PER; ++u) rows[u] = rows_of(i)[(threadIdx.x + u * THREADS) / PIECES];
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int n = threadIdx.x + u * THREADS, key = n / PIECES, slot = n - key * PIECES;
+            const uint32_t row = rows[u], first = (uint32_t)(n - lane) * 16;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int p = (x ? value_piece(key, slot) : key_piece(key, slot)) >> 4; // (an exclusive or: its own inverse)
+                if (D == DP || p * 8 < D)
+                    lds_dma16(reinterpret_cast<const uint16_t *>(x ? a.c.v : a.c.k) + ((uint64_t)(row == kAbsent ? 0u : row) * D + p * 8),
+                              (uint32_t)(uintptr_t)(lds_u8 *)(x ? vbuf : kbuf)[i & 1] + first);
+            }
+        }
+    };
     auto load = [&](int i) __attribute__((always_inline)) {
+        if constexpr (!E8) return load16(i);
         absent = 0;
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
-            const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, d = (n - key * IN_ROW) * (E8 ? 16 : 8);
-            const uint32_t row = UNITS % THREADS == 0 || n < UNITS ? ring[i % 3][key] : kAbsent;
+            const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, d = (n - key * IN_ROW) * 16;
+            const uint32_t row = UNITS % THREADS == 0 || n < UNITS ? rows_of(i)[key] : kAbsent;
             const bool there = row != kAbsent && d < D;
             if (!there) absent |= 1u << u;
             const uint64_t at = (uint64_t)(there ? row : 0u) * D + (there ? d : 0);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                in[x][u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint8_t *>(x ? a.c.v : a.c.k) + at * (E8 ? 1 : 2));
-                if constexpr (E8) scale8[x][u] = (x ? a.c.v_scale : a.c.k_scale)[(uint64_t)(there ? row : 0u) * ((uint32_t)(D + 31) >> 5) + (there ? d >> 5 : 0)];
+                in[x][u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint8_t *>(x ? a.c.v : a.c.k) + at);
+                scale8[x][u] = (x ? a.c.v_scale : a.c.k_scale)[(uint64_t)(there ? row : 0u) * ((uint32_t)(D + 31) >> 5) + (there ? d >> 5 : 0)];
             }
         }
     };
     auto store = [&](int i) __attribute__((always_inline)) {
+        if constexpr (!E8) return;
         if (__any(absent)) { // another's row, or the padding of a head
             asm volatile("" : : : "memory");
 #pragma unroll
@@ -176,39 +208,35 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
                 for (int x = 0; x < 2; ++x)
                     if (absent >> u & 1) {
                         in[x][u] = make_uint4(0, 0, 0, 0);
-                        if constexpr (E8) scale8[x][u] = 127;
+                        scale8[x][u] = 127;
                     }
         }
         if (parted(i)) {
             bool bad = false;
 #pragma unroll
             for (int u = 0; u < PER; ++u) {
-                const uint4 w = in[1][u];
-                if constexpr (E8) bad = bad || scale8[1][u] == 255;
-                else bad = bad || not_finite2<DT>(w.x) || not_finite2<DT>(w.y) || not_finite2<DT>(w.z) || not_finite2<DT>(w.w);
+                bad = bad || scale8[1][u] == 255;
             }
             if (bad) odd[i & 1] = 1;
         }
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
-            const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, p = (n - key * IN_ROW) * (E8 ? 2 : 1);
+            const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, p = (n - key * IN_ROW) * 2;
             if (UNITS % THREADS && n >= UNITS) continue;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint8_t *to = (x ? vbuf : kbuf)[i & 1] + key * STRIDE;
                 auto piece = [&](int p) { return x ? value_piece(key, p) : key_piece(key, p); };
                 const uint4 w = in[x][u];
-                if constexpr (E8) {
-                    *reinterpret_cast<uint4 *>(to + piece(p)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), scale8[x][u]);
-                    *reinterpret_cast<uint4 *>(to + piece(p + 1)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), scale8[x][u]);
-                } else *reinterpret_cast<uint4 *>(to + piece(p)) = w;
+                *reinterpret_cast<uint4 *>(to + piece(p)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), scale8[x][u]);
+                *reinterpret_cast<uint4 *>(to + piece(p + 1)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), scale8[x][u]);
             }
         }
     };
     // the tokens of 32 from step i's sub-step u that the lane's row sees, a bit each
     auto seen = [&](int i, int u) __attribute__((always_inline)) {
         const long base = (long)from + (long)i * BN + 32 * u, past = at - base, before = a.window > 0 ? at - a.window + 1 - base : 0;
-        uint32_t bits = ~gone[i % 3][u];
+        uint32_t bits = ~gone[i / AHEAD & 1][i % AHEAD * NSUB + u];
         if (past < 31) bits &= past < 0 ? 0u : (2u << past) - 1u;
         if (before > 0) bits &= before > 31 ? 0u : ~0u << before;
         return bits;
@@ -242,7 +270,17 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
         if (threadIdx.x == 0) odd[i & 1] = 0;
         __syncthreads();
     };
-    auto compute = [&](int i) __attribute__((always_inline)) {
+    // 16 bits: whether there are such values is looked up where they lie, in the steps where it matters.
+    auto look_for_odd = [&](int i) __attribute__((always_inline)) {
+        bool bad = false;
+        for (int n = threadIdx.x; n < BN * PIECES; n += THREADS) {
+            const uint4 w = reinterpret_cast<const uint4 *>(vbuf[i & 1])[n];
+            bad = bad || not_finite2<DT>(w.x) || not_finite2<DT>(w.y) || not_finite2<DT>(w.z) || not_finite2<DT>(w.w);
+        }
+        if (bad) odd[i & 1] = 1;
+        __syncthreads();
+    };
+    auto compute = [&](int i, bool some_hidden) __attribute__((always_inline)) {
         const uint8_t *kb = kbuf[i & 1], *vb = vbuf[i & 1];
         f32x16 sc[NSUB];
 #pragma unroll
@@ -254,10 +292,15 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
                 const int key = 32 * u + r;
                 sc[u] = mfma32<DT>(*reinterpret_cast<const uint4 *>(kb + key * STRIDE + key_piece(key, 2 * c + h)), qf[c], sc[u]);
             }
-        uint32_t none = 0;
+        // two keys' reads are on their way while one is multiplied
+        __builtin_amdgcn_sched_group_barrier(0x100, 3 * NSUB, 0);
 #pragma unroll
-        for (int u = 0; u < NSUB; ++u) none |= gone[i % 3][u];
-        if (parted(i) || __builtin_amdgcn_readfirstlane(none)) {
+        for (int n = 0; n < 2 * ND - 3; ++n) {
+            __builtin_amdgcn_sched_group_barrier(0x008, NSUB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, NSUB, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 3 * NSUB, 0);
+        if (some_hidden) {
             asm volatile("" : : : "memory");
 #pragma unroll
             for (int u = 0; u < NSUB; ++u) {
@@ -271,7 +314,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
         for (int u = 0; u < NSUB; ++u)
 #pragma unroll
             for (int k = 0; k < 16; k += 2) top = max3(top, sc[u][k], sc[u][k + 1]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * to2;
+        top = over_halves(top) * to2;
         float mul = to2;
         if (__any(fabsf(top) > 0x1p20f && top != -INFINITY)) { // (where a product's rounding would count in the exponent)
             asm volatile("" : : : "memory");
@@ -287,45 +330,75 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
             for (int dt = 0; dt < ND; ++dt) o[dt] *= c;
         }
         const float base = m == -INFINITY ? 0.f : m - TOP;
+        // 16 tokens at a time; between the products of one such part the next one's values are read and its weights formed
+        constexpr int PARTS = 2 * NSUB;
+        uint4 pf[2], vf[2][ND];
+        float p[8];
+        auto weigh = [&](int part, int k) __attribute__((always_inline)) {
+            p[k] = __builtin_amdgcn_exp2f(fmaf(sc[part >> 1][8 * (part & 1) + k], mul, -base));
+            l += p[k];
+        };
+        auto pack = [&](int part) __attribute__((always_inline)) {
+            pf[part & 1] = make_uint4(pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7]));
+        };
+        auto read = [&](int part, int dt) __attribute__((always_inline)) {
+            uint2 v[2];
 #pragma unroll
-        for (int u = 0; u < NSUB; ++u)
+            for (int y = 0; y < 2; ++y) {
+                const int key = 16 * part + 8 * y + 4 * h + (lane >> 2 & 3), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+                v[y] = read_columns(vb + key * STRIDE + value_piece(key, piece) + (lane & 1) * 8);
+            }
+            vf[part & 1][dt] = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+        };
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                float p[8];
+        for (int dt = 0; dt < ND; ++dt) read(0, dt);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    p[k] = __builtin_amdgcn_exp2f(fmaf(sc[u][8 * x + k], mul, -base));
-                    l += p[k];
-                }
-                const uint4 pf = make_uint4(pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7]));
+        for (int k = 0; k < 8; ++k) weigh(0, k);
+        pack(0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) {
-                    uint2 v[2];
+        for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int key = 32 * u + 16 * x + 8 * y + 4 * h + (lane >> 2 & 3), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-                        v[y] = read_columns(vb + key * STRIDE + value_piece(key, piece) + (lane & 1) * 8);
-                    }
-                    o[dt] = mfma32<DT>(make_uint4(v[0].x, v[0].y, v[1].x, v[1].y), pf, o[dt]);
+            for (int dt = 0; dt < ND; ++dt) {
+                o[dt] = mfma32<DT>(vf[part & 1][dt], pf[part & 1], o[dt]);
+                if (part + 1 < PARTS) {
+                    read(part + 1, dt);
+#pragma unroll
+                    for (int k = 8 * dt / ND; k < 8 * (dt + 1) / ND; ++k) weigh(part + 1, k);
+                    if (dt + 1 == ND) pack(part + 1);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
+        }
+        asm volatile("" : "+v"(l)); // (its additions belong here)
     };
 
     if (steps > 0) {
         if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+        if (!E8 && D < DP) // the padding of the heads
+            for (int n = threadIdx.x; n < 2 * BN * PIECES; n += THREADS)
+                reinterpret_cast<uint4 *>(kbuf)[n] = reinterpret_cast<uint4 *>(vbuf)[n] = make_uint4(0, 0, 0, 0);
         look_up(0, page_of(0));
-        look_up(1, page_of(1));
         __syncthreads();
         load(0);
         store(0);
+        if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         for (int i = 0; i < steps; ++i) {
             __syncthreads();
-            if (__builtin_amdgcn_readfirstlane(odd[i & 1])) part_values(i);
-            const int page = page_of(i + 2);
-            if (i + 1 < steps) load(i + 1);
-            compute(i);
-            if (i + 1 < steps) store(i + 1);
-            look_up(i + 2, page);
+            const int hole = holes[i / AHEAD & 1][i % AHEAD], strange = odd[i & 1];
+            const bool more = i + 1 < steps;
+            if (more) load(i + 1);
+            const bool hidden = parted(i) || __builtin_amdgcn_readfirstlane(hole);
+            if (!E8 && hidden) look_for_odd(i);
+            if (__builtin_amdgcn_readfirstlane(E8 || !hidden ? strange : (int)odd[i & 1])) part_values(i);
+            // the next tokens are looked up in the first step of the last that were
+            const int next = i / AHEAD + 1;
+            const bool ask = i % AHEAD == 0 && (long)next * AHEAD < steps;
+            const int page = ask ? page_of(next) : -1;
+            compute(i, hidden);
+            if (more) store(i + 1);
+            if (ask) look_up(next, page);
+            if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); // what is on its way into LDS
         }
     }
     l += __shfl_xor(l, 32);
