@@ -144,7 +144,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
     auto look_up = [&](int n, int page) __attribute__((always_inline)) {
         const uint32_t j = (uint32_t)from + (uint32_t)n * THREADS + threadIdx.x;
         const bool there = (uint32_t)page < (uint32_t)a.c.pages;
-        ring[n & 1][threadIdx.x] = there ? ((uint32_t)page * a.c.kv_heads + kvh) * a.c.page_size + j % (uint32_t)a.c.page_size : kAbsent;
+        ring[n & 1][threadIdx.x] = there ? ((uint32_t)page * a.c.kv_heads + kvh) * a.c.page_size + j % (uint32_t)a.c.page_size : 0;
         const uint64_t none = ~__ballot(there);
         if (lane == 0) {
             gone[n & 1][2 * wave] = (uint32_t)none;
@@ -159,77 +159,60 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
         const long base = (long)from + (long)i * BN;
         return base + BN - 1 > at_first || (a.window > 0 && base <= (long)at_last - a.window);
     };
-    uint4 in[2][E8 ? PER : 1];
-    uint32_t scale8[2][E8 ? PER : 1], absent; // absent: a bit a unit
-    // 16 bits: straight into LDS, a wave 64 pieces at a time as they lie there; what is not there is another token's, and left out of scores and sums.
-    typedef __attribute__((address_space(3))) uint8_t lds_u8;
-    auto load16 = [&](int i) __attribute__((always_inline)) {
-        static_assert(E8 || UNITS % THREADS == 0, "every thread has as many pieces");
-        uint32_t rows[PER];
+    // The next step's keys and values are asked for a part at a time, between the products: a wave that asks for all at once stands still while the compute unit
+    // takes them in, 64 bytes a cycle.  A part is 64 pieces of the wave, or 64 sixteens of 8-bit floats; its address is one multiplication and addition.
+    // 16 bits: straight into LDS as the pieces lie there, a lane taking the one that belongs in its place.  A token that is not there is row 0 of the cache: it
+    // has no score, and no value but where holes are looked after.
+    const int wave0 = __builtin_amdgcn_readfirstlane(wave);
+    auto key_of = [&](int u) { return THREADS % IN_ROW == 0 ? (int)threadIdx.x / IN_ROW + u * (THREADS / IN_ROW) : ((int)threadIdx.x + u * THREADS) / IN_ROW; };
+    auto slot_of = [&](int u) { return THREADS % IN_ROW == 0 ? (int)threadIdx.x % IN_ROW : ((int)threadIdx.x + u * THREADS) % IN_ROW; };
+    const uint32_t row_bytes = (uint32_t)D * (E8 ? 1 : 2), blocks = (uint32_t)(D + 31) >> 5;
+    uint32_t rows[PER];
+    auto rows_of_step = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < PER; ++u) rows[u] = rows_of(i)[(threadIdx.x + u * THREADS) / PIECES];
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int n = threadIdx.x + u * THREADS, key = n / PIECES, slot = n - key * PIECES;
-            const uint32_t row = rows[u], first = (uint32_t)(n - lane) * 16;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int p = (x ? value_piece(key, slot) : key_piece(key, slot)) >> 4; // (an exclusive or: its own inverse)
-                if (D == DP || p * 8 < D)
-                    lds_dma16(reinterpret_cast<const uint16_t *>(x ? a.c.v : a.c.k) + ((uint64_t)(row == kAbsent ? 0u : row) * D + p * 8),
-                              (uint32_t)(uintptr_t)(lds_u8 *)(x ? vbuf : kbuf)[i & 1] + first);
-            }
-        }
+        for (int u = 0; u < PER; ++u) rows[u] = rows_of(i)[UNITS % THREADS == 0 || key_of(u) < BN ? key_of(u) : 0];
     };
-    auto load = [&](int i) __attribute__((always_inline)) {
-        if constexpr (!E8) return load16(i);
-        absent = 0;
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, d = (n - key * IN_ROW) * 16;
-            const uint32_t row = UNITS % THREADS == 0 || n < UNITS ? rows_of(i)[key] : kAbsent;
-            const bool there = row != kAbsent && d < D;
-            if (!there) absent |= 1u << u;
-            const uint64_t at = (uint64_t)(there ? row : 0u) * D + (there ? d : 0);
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                in[x][u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint8_t *>(x ? a.c.v : a.c.k) + at);
-                scale8[x][u] = (x ? a.c.v_scale : a.c.k_scale)[(uint64_t)(there ? row : 0u) * ((uint32_t)(D + 31) >> 5) + (there ? d >> 5 : 0)];
-            }
+    typedef __attribute__((address_space(3))) uint8_t lds_u8;
+    uint4 in[2][E8 ? PER : 1];
+    uint32_t scale8[2][E8 ? PER : 1];
+    auto load = [&](int i, int u, int x) __attribute__((always_inline)) {
+        const int slot = slot_of(u), p = E8 ? 2 * slot : (x ? value_piece(key_of(u), slot) : key_piece(key_of(u), slot)) >> 4; // (an exclusive or: its own inverse)
+        const uint8_t *from = reinterpret_cast<const uint8_t *>(x ? a.c.v : a.c.k) + p * (E8 ? 8 : 16) + (uint64_t)rows[u] * row_bytes;
+        if (D == DP || p * 8 < D) {
+            if constexpr (E8) {
+                in[x][u] = *reinterpret_cast<const uint4 *>(from);
+                scale8[x][u] = ((x ? a.c.v_scale : a.c.k_scale) + (p >> 2))[(uint64_t)rows[u] * blocks];
+            } else lds_dma16(from, (uint32_t)(uintptr_t)(lds_u8 *)(x ? vbuf : kbuf)[i & 1] + (uint32_t)(wave0 * 64 + u * THREADS) * 16);
         }
     };
     auto store = [&](int i) __attribute__((always_inline)) {
         if constexpr (!E8) return;
-        if (__any(absent)) { // another's row, or the padding of a head
-            asm volatile("" : : : "memory");
+        if (__builtin_amdgcn_readfirstlane(holes[i / AHEAD & 1][i % AHEAD]))
 #pragma unroll
             for (int u = 0; u < PER; ++u)
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (absent >> u & 1) {
-                        in[x][u] = make_uint4(0, 0, 0, 0);
-                        scale8[x][u] = 127;
-                    }
-        }
+                if ((UNITS % THREADS == 0 || key_of(u) < BN) && gone[i / AHEAD & 1][i % AHEAD * NSUB + (key_of(u) >> 5)] >> (key_of(u) & 31) & 1) {
+                    in[0][u] = in[1][u] = make_uint4(0, 0, 0, 0);
+                    scale8[0][u] = scale8[1][u] = 127;
+                }
         if (parted(i)) {
             bool bad = false;
 #pragma unroll
-            for (int u = 0; u < PER; ++u) {
-                bad = bad || scale8[1][u] == 255;
-            }
+            for (int u = 0; u < PER; ++u) bad = bad || scale8[1][u] == 255;
             if (bad) odd[i & 1] = 1;
         }
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
-            const int n = threadIdx.x + u * THREADS, key = n / IN_ROW, p = (n - key * IN_ROW) * 2;
-            if (UNITS % THREADS && n >= UNITS) continue;
+            const int key = key_of(u), p = slot_of(u) * 2;
+            if (UNITS % THREADS && key >= BN) continue;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint8_t *to = (x ? vbuf : kbuf)[i & 1] + key * STRIDE;
                 auto piece = [&](int p) { return x ? value_piece(key, p) : key_piece(key, p); };
                 const uint4 w = in[x][u];
-                *reinterpret_cast<uint4 *>(to + piece(p)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), scale8[x][u]);
-                *reinterpret_cast<uint4 *>(to + piece(p + 1)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), scale8[x][u]);
+                const bool flip = x && (key & 1); // (values: neighbouring rows' pieces on other banks)
+                const uint2 one = make_uint2(flip ? w.z : w.x, flip ? w.w : w.y), two = make_uint2(flip ? w.x : w.z, flip ? w.y : w.w);
+                *reinterpret_cast<uint4 *>(to + piece(p + flip)) = from_e4m3x8<DT>(one, scale8[x][u]);
+                *reinterpret_cast<uint4 *>(to + piece(p + !flip)) = from_e4m3x8<DT>(two, scale8[x][u]);
             }
         }
     };
@@ -280,26 +263,29 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
         if (bad) odd[i & 1] = 1;
         __syncthreads();
     };
-    auto compute = [&](int i, bool some_hidden) __attribute__((always_inline)) {
+    auto compute = [&](int i, bool some_hidden, bool more) __attribute__((always_inline)) {
         const uint8_t *kb = kbuf[i & 1], *vb = vbuf[i & 1];
         f32x16 sc[NSUB];
 #pragma unroll
         for (int u = 0; u < NSUB; ++u) sc[u] = f32x16{};
+        uint4 kf[3][NSUB];
+        auto read_keys = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int c = 0; c < 2 * ND; ++c)
+            for (int u = 0; u < NSUB; ++u) kf[c % 3][u] = *reinterpret_cast<const uint4 *>(kb + (32 * u + r) * STRIDE + key_piece(32 * u + r, 2 * c + h));
+        };
+        read_keys(0);
+        read_keys(1);
 #pragma unroll
-            for (int u = 0; u < NSUB; ++u) {
-                const int key = 32 * u + r;
-                sc[u] = mfma32<DT>(*reinterpret_cast<const uint4 *>(kb + key * STRIDE + key_piece(key, 2 * c + h)), qf[c], sc[u]);
-            }
-        // two keys' reads are on their way while one is multiplied
-        __builtin_amdgcn_sched_group_barrier(0x100, 3 * NSUB, 0);
+        for (int c = 0; c < 2 * ND; ++c) {
+            if (c + 2 < 2 * ND) read_keys(c + 2);
 #pragma unroll
-        for (int n = 0; n < 2 * ND - 3; ++n) {
-            __builtin_amdgcn_sched_group_barrier(0x008, NSUB, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, NSUB, 0);
+            for (int u = 0; u < NSUB; ++u) sc[u] = mfma32<DT>(kf[c % 3][u], qf[c], sc[u]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < PER; ++u)
+                if (more && u * 2 * ND / PER == c) load(i + 1, u, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 3 * NSUB, 0);
         if (some_hidden) {
             asm volatile("" : : : "memory");
 #pragma unroll
@@ -368,6 +354,12 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
                     if (dt + 1 == ND) pack(part + 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+#pragma unroll
+                for (int u = 0; u < PER; ++u)
+                    if (more && u * PARTS * ND / PER == part * ND + dt) {
+                        load(i + 1, u, 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
             }
         }
         asm volatile("" : "+v"(l)); // (its additions belong here)
@@ -375,19 +367,32 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
 
     if (steps > 0) {
         if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-        if (!E8 && D < DP) // the padding of the heads
-            for (int n = threadIdx.x; n < 2 * BN * PIECES; n += THREADS)
-                reinterpret_cast<uint4 *>(kbuf)[n] = reinterpret_cast<uint4 *>(vbuf)[n] = make_uint4(0, 0, 0, 0);
+        if (D < DP) { // the padding of the heads
+            if constexpr (E8)
+#pragma unroll
+                for (int u = 0; u < PER; ++u) {
+                    in[0][u] = in[1][u] = make_uint4(0, 0, 0, 0);
+                    scale8[0][u] = scale8[1][u] = 127;
+                }
+            else
+                for (int n = threadIdx.x; n < 2 * BN * PIECES; n += THREADS)
+                    reinterpret_cast<uint4 *>(kbuf)[n] = reinterpret_cast<uint4 *>(vbuf)[n] = make_uint4(0, 0, 0, 0);
+        }
         look_up(0, page_of(0));
         __syncthreads();
-        load(0);
+        rows_of_step(0);
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            load(0, u, 0);
+            load(0, u, 1);
+        }
         store(0);
         if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         for (int i = 0; i < steps; ++i) {
             __syncthreads();
             const int hole = holes[i / AHEAD & 1][i % AHEAD], strange = odd[i & 1];
             const bool more = i + 1 < steps;
-            if (more) load(i + 1);
+            if (more) rows_of_step(i + 1);
             const bool hidden = parted(i) || __builtin_amdgcn_readfirstlane(hole);
             if (!E8 && hidden) look_for_odd(i);
             if (__builtin_amdgcn_readfirstlane(E8 || !hidden ? strange : (int)odd[i & 1])) part_values(i);
@@ -395,7 +400,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
             const int next = i / AHEAD + 1;
             const bool ask = i % AHEAD == 0 && (long)next * AHEAD < steps;
             const int page = ask ? page_of(next) : -1;
-            compute(i, hidden);
+            compute(i, hidden, more);
             if (more) store(i + 1);
             if (ask) look_up(next, page);
             if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); // what is on its way into LDS
