@@ -11,6 +11,9 @@ namespace npas {
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
+// Zeros, as 8-bit numbers and as 16-bit ones; the first byte as a scale too.
+__device__ const uint4 kNothing = {};
+
 template <int DT> __device__ __forceinline__ f32x16 mfma32(uint4 a, uint4 b, f32x16 c)
 {
     if constexpr (DT == NPAS_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -55,24 +58,29 @@ struct Tile {
 // Sequence s owns the places [start G / BM] + s .. of the grid: as many as its rows need, whatever the parting.
 template <int BM> __device__ __forceinline__ bool find_tile(const ChunkArgs &a, int place, int group, Tile &t)
 {
-    auto start = [&](int s) { return max(0, min(a.start[s], a.T)); };
-    auto first = [&](int s) { return (int)((long)start(s) * group / BM) + s; };
+    auto bounded = [&](int start) { return max(0, min(start, a.T)); };
+    auto first = [&](int start, int s) { return (int)((long)start * group / BM) + s; };
     const int lane = threadIdx.x & 63;
-    int count = 0; // sequences that begin at or before this place
+    int begin = 0, after = 0, n = 0; // of the last sequence that begins at or before this place
+    t.s = -1;
     for (int s0 = 0; s0 < a.c.sequences; s0 += 64) {
-        const int s = s0 + lane;
-        const int here = __popcll(__ballot(s < a.c.sequences && first(s) <= place));
-        count += here;
+        const int s = min(s0 + lane, a.c.sequences - 1), b = bounded(a.start[s]), e = bounded(a.start[s + 1]), len = a.length[s];
+        const int here = __popcll(__ballot(s0 + lane < a.c.sequences && first(b, s) <= place));
+        if (here) {
+            t.s = s0 + here - 1;
+            begin = __builtin_amdgcn_readlane(b, here - 1);
+            after = __builtin_amdgcn_readlane(e, here - 1);
+            n = __builtin_amdgcn_readlane(len, here - 1);
+        }
         if (here < 64) break;
     }
-    if (!count) return false;
-    t.s = count - 1;
-    t.token0 = start(t.s);
-    const int run = max(0, start(t.s + 1) - t.token0);
-    t.row0 = (place - first(t.s)) * BM;
+    if (t.s < 0) return false;
+    t.token0 = begin;
+    const int run = max(0, after - begin);
+    t.row0 = (place - first(begin, t.s)) * BM;
     t.rows = run * group - t.row0;
     const long room = (long)a.c.table_stride * a.c.page_size;
-    int n = max(0, min(a.length[t.s], a.max_length));
+    n = max(0, min(n, a.max_length));
     if (n > room) n = (int)room;
     t.length = n;
     t.at0 = n - run;
@@ -86,19 +94,19 @@ template <int BM> __device__ __forceinline__ bool find_tile(const ChunkArgs &a, 
 // Keys and values of a step come through registers into one of two places in LDS (16-byte pieces in an order that spreads rows over the banks; 8-bit
 // floats become 16-bit numbers on the way) while the other is multiplied; the cache rows of the tokens are looked up two steps ahead.
 // The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled.
-template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a, int places)
+template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a, int places)
 {
     constexpr int DP = 32 * ND, BM = 32 * WAVES, BN = 32 * NSUB, THREADS = 64 * WAVES, PIECES = DP / 8, STRIDE = DP * 2;
     constexpr int UNITS = E8 ? BN * PIECES / 2 : BN * PIECES, PER = (UNITS + THREADS - 1) / THREADS, IN_ROW = E8 ? PIECES / 2 : PIECES;
     constexpr float GROW = DT == NPAS_BF16 ? 8.f : 4.f, TOP = DT == NPAS_BF16 ? 0.f : 11.f; // a weight is at most 2^(TOP + GROW)
     __shared__ __align__(16) uint8_t kbuf[2][BN * STRIDE], vbuf[2][BN * STRIDE];
     constexpr int AHEAD = THREADS / BN; // steps whose tokens are looked up at once, one a thread
-    __shared__ uint32_t ring[2][THREADS], gone[2][THREADS / 32], holes[2][AHEAD]; // cache rows of tokens; a bit a token that is not there; whether a step has such
+    __shared__ uint32_t ring[2 * THREADS], gone[2 * THREADS / 32], holes[2 * AHEAD]; // cache rows of tokens; a bit a token that is not there; whether a step has such
     __shared__ uint32_t odd[2]; // values of a step hold an infinity or a NaN, and not every row sees every token
     // Where a row's pieces lie, so that what a read takes at once is spread over all banks: keys are read one piece of 16 rows, values two or four of 4 or 8.
     auto key_piece = [](int row, int p) { return (p ^ (ND == 2 ? row >> 1 & 7 : ND == 3 ? row >> 2 & 3 : row & 15)) << 4; };
     auto value_piece = [](int row, int p) { return (p ^ ((ND == 2 ? (row >> 1 & 1) * 4 : ND == 3 ? 0 : (row & 3) * 4) + (row >> 2 & 1) * 2)) << 4; };
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, D = a.c.head_dim;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, D = FULL ? DP : a.c.head_dim;
     const int group = a.heads / a.c.kv_heads;
     uint32_t id = blockIdx.x;
     const int kvh = id % a.c.kv_heads, head0 = kvh * group;
@@ -144,21 +152,21 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
     auto look_up = [&](int n, int page) __attribute__((always_inline)) {
         const uint32_t j = (uint32_t)from + (uint32_t)n * THREADS + threadIdx.x;
         const bool there = (uint32_t)page < (uint32_t)a.c.pages;
-        ring[n & 1][threadIdx.x] = there ? ((uint32_t)page * a.c.kv_heads + kvh) * a.c.page_size + j % (uint32_t)a.c.page_size : 0;
+        ring[(n & 1) * THREADS + threadIdx.x] = there ? ((uint32_t)page * a.c.kv_heads + kvh) * a.c.page_size + j % (uint32_t)a.c.page_size : 0;
         const uint64_t none = ~__ballot(there);
         if (lane == 0) {
-            gone[n & 1][2 * wave] = (uint32_t)none;
-            gone[n & 1][2 * wave + 1] = (uint32_t)(none >> 32);
-            if (BN == 64) holes[n & 1][wave] = none != 0;
-            else holes[n & 1][2 * wave] = (uint32_t)none, holes[n & 1][2 * wave + 1] = (uint32_t)(none >> 32);
+            gone[(n & 1) * (THREADS / 32) + 2 * wave] = (uint32_t)none;
+            gone[(n & 1) * (THREADS / 32) + 2 * wave + 1] = (uint32_t)(none >> 32);
+            if (BN == 64) holes[(n & 1) * AHEAD + wave] = none != 0;
+            else holes[(n & 1) * AHEAD + 2 * wave] = (uint32_t)none, holes[(n & 1) * AHEAD + 2 * wave + 1] = (uint32_t)(none >> 32);
         }
     };
-    auto rows_of = [&](int i) { return ring[i / AHEAD & 1] + i % AHEAD * BN; };
-    // whether a row of the workgroup does not see a token of step i that another sees
-    auto parted = [&](int i) __attribute__((always_inline)) {
-        const long base = (long)from + (long)i * BN;
-        return base + BN - 1 > at_first || (a.window > 0 && base <= (long)at_last - a.window);
-    };
+    auto rows_of = [&](int i) { return ring + i % (2 * AHEAD) * BN; };
+    // Every row sees every token of the steps lo .. hi - 1.
+    const int hi = (int)max(0l, min((long)steps, ((long)at_first + 1 - from) >> (BN == 64 ? 6 : 5)));
+    const int lo = a.window > 0 ? (int)max(0l, min((long)steps, ((long)at_last - a.window - from) / BN + 1)) : 0;
+    auto parted = [&](int i) { return i >= hi || (i < lo && at_last - a.window >= from); };
+    auto hole = [&](int i) { return __builtin_amdgcn_readfirstlane(holes[i % (2 * AHEAD)]) != 0; };
     // The next step's keys and values are asked for a part at a time, between the products: a wave that asks for all at once stands still while the compute unit
     // takes them in, 64 bytes a cycle.  A part is 64 pieces of the wave, or 64 sixteens of 8-bit floats; its address is one multiplication and addition.
     // 16 bits: straight into LDS as the pieces lie there, a lane taking the one that belongs in its place.  A token that is not there is row 0 of the cache: it
@@ -175,22 +183,23 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
     typedef __attribute__((address_space(3))) uint8_t lds_u8;
     uint4 in[2][E8 ? PER : 1];
     uint32_t scale8[2][E8 ? PER : 1];
-    auto load = [&](int i, int u, int x) __attribute__((always_inline)) {
+    auto load = [&](auto place, int u, int x) __attribute__((always_inline)) {
         const int slot = slot_of(u), p = E8 ? 2 * slot : (x ? value_piece(key_of(u), slot) : key_piece(key_of(u), slot)) >> 4; // (an exclusive or: its own inverse)
         const uint8_t *from = reinterpret_cast<const uint8_t *>(x ? a.c.v : a.c.k) + p * (E8 ? 8 : 16) + (uint64_t)rows[u] * row_bytes;
-        if (D == DP || p * 8 < D) {
-            if constexpr (E8) {
-                in[x][u] = *reinterpret_cast<const uint4 *>(from);
-                scale8[x][u] = ((x ? a.c.v_scale : a.c.k_scale) + (p >> 2))[(uint64_t)rows[u] * blocks];
-            } else lds_dma16(from, (uint32_t)(uintptr_t)(lds_u8 *)(x ? vbuf : kbuf)[i & 1] + (uint32_t)(wave0 * 64 + u * THREADS) * 16);
-        }
+        const bool behind = !FULL && p * 8 >= D; // the end of the head
+        if (behind) from = reinterpret_cast<const uint8_t *>(&kNothing);
+        if constexpr (E8) {
+            const uint8_t *scale = ((x ? a.c.v_scale : a.c.k_scale) + (p >> 2)) + (uint64_t)rows[u] * blocks;
+            in[x][u] = *reinterpret_cast<const uint4 *>(from);
+            scale8[x][u] = *(behind ? from : scale);
+        } else lds_dma16(from, (uint32_t)(uintptr_t)(lds_u8 *)(x ? vbuf : kbuf)[place] + (uint32_t)(wave0 * 64 + u * THREADS) * 16);
     };
     auto store = [&](int i) __attribute__((always_inline)) {
         if constexpr (!E8) return;
-        if (__builtin_amdgcn_readfirstlane(holes[i / AHEAD & 1][i % AHEAD]))
+        if (hole(i))
 #pragma unroll
             for (int u = 0; u < PER; ++u)
-                if ((UNITS % THREADS == 0 || key_of(u) < BN) && gone[i / AHEAD & 1][i % AHEAD * NSUB + (key_of(u) >> 5)] >> (key_of(u) & 31) & 1) {
+                if ((UNITS % THREADS == 0 || key_of(u) < BN) && gone[i % (2 * AHEAD) * NSUB + (key_of(u) >> 5)] >> (key_of(u) & 31) & 1) {
                     in[0][u] = in[1][u] = make_uint4(0, 0, 0, 0);
                     scale8[0][u] = scale8[1][u] = 127;
                 }
@@ -209,17 +218,15 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
                 uint8_t *to = (x ? vbuf : kbuf)[i & 1] + key * STRIDE;
                 auto piece = [&](int p) { return x ? value_piece(key, p) : key_piece(key, p); };
                 const uint4 w = in[x][u];
-                const bool flip = x && (key & 1); // (values: neighbouring rows' pieces on other banks)
-                const uint2 one = make_uint2(flip ? w.z : w.x, flip ? w.w : w.y), two = make_uint2(flip ? w.x : w.z, flip ? w.y : w.w);
-                *reinterpret_cast<uint4 *>(to + piece(p + flip)) = from_e4m3x8<DT>(one, scale8[x][u]);
-                *reinterpret_cast<uint4 *>(to + piece(p + !flip)) = from_e4m3x8<DT>(two, scale8[x][u]);
+                *reinterpret_cast<uint4 *>(to + piece(p)) = from_e4m3x8<DT>(make_uint2(w.x, w.y), scale8[x][u]);
+                *reinterpret_cast<uint4 *>(to + piece(p + 1)) = from_e4m3x8<DT>(make_uint2(w.z, w.w), scale8[x][u]);
             }
         }
     };
     // the tokens of 32 from step i's sub-step u that the lane's row sees, a bit each
     auto seen = [&](int i, int u) __attribute__((always_inline)) {
         const long base = (long)from + (long)i * BN + 32 * u, past = at - base, before = a.window > 0 ? at - a.window + 1 - base : 0;
-        uint32_t bits = ~gone[i / AHEAD & 1][i % AHEAD * NSUB + u];
+        uint32_t bits = ~gone[i % (2 * AHEAD) * NSUB + u];
         if (past < 31) bits &= past < 0 ? 0u : (2u << past) - 1u;
         if (before > 0) bits &= before > 31 ? 0u : ~0u << before;
         return bits;
@@ -263,8 +270,9 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
         if (bad) odd[i & 1] = 1;
         __syncthreads();
     };
-    auto compute = [&](int i, bool some_hidden, bool more) __attribute__((always_inline)) {
-        const uint8_t *kb = kbuf[i & 1], *vb = vbuf[i & 1];
+    auto compute = [&](int i, auto parity, bool some_hidden, auto morec) __attribute__((always_inline)) {
+        constexpr bool more = decltype(morec)::value;
+        const uint8_t *kb = kbuf[parity], *vb = vbuf[parity];
         f32x16 sc[NSUB];
 #pragma unroll
         for (int u = 0; u < NSUB; ++u) sc[u] = f32x16{};
@@ -283,7 +291,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < PER; ++u)
-                if (more && u * 2 * ND / PER == c) load(i + 1, u, 0);
+                if (more && u * 2 * ND / PER == c) load(1 - parity, u, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
         if (some_hidden) {
@@ -357,7 +365,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
 #pragma unroll
                 for (int u = 0; u < PER; ++u)
                     if (more && u * PARTS * ND / PER == part * ND + dt) {
-                        load(i + 1, u, 1);
+                        load(1 - parity, u, 1);
                         __builtin_amdgcn_sched_barrier(0);
                     }
             }
@@ -367,17 +375,6 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
 
     if (steps > 0) {
         if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-        if (D < DP) { // the padding of the heads
-            if constexpr (E8)
-#pragma unroll
-                for (int u = 0; u < PER; ++u) {
-                    in[0][u] = in[1][u] = make_uint4(0, 0, 0, 0);
-                    scale8[0][u] = scale8[1][u] = 127;
-                }
-            else
-                for (int n = threadIdx.x; n < 2 * BN * PIECES; n += THREADS)
-                    reinterpret_cast<uint4 *>(kbuf)[n] = reinterpret_cast<uint4 *>(vbuf)[n] = make_uint4(0, 0, 0, 0);
-        }
         look_up(0, page_of(0));
         __syncthreads();
         rows_of_step(0);
@@ -388,23 +385,27 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC> __global__ __la
         }
         store(0);
         if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        for (int i = 0; i < steps; ++i) {
+        auto step = [&](int i, auto parity, auto morec) __attribute__((always_inline)) {
+            constexpr bool more = decltype(morec)::value; // another follows
             __syncthreads();
-            const int hole = holes[i / AHEAD & 1][i % AHEAD], strange = odd[i & 1];
-            const bool more = i + 1 < steps;
             if (more) rows_of_step(i + 1);
-            const bool hidden = parted(i) || __builtin_amdgcn_readfirstlane(hole);
-            if (!E8 && hidden) look_for_odd(i);
-            if (__builtin_amdgcn_readfirstlane(E8 || !hidden ? strange : (int)odd[i & 1])) part_values(i);
+            const bool hidden = parted(i) || hole(i);
+            if (hidden) {
+                if (!E8) look_for_odd(i);
+                if (__builtin_amdgcn_readfirstlane(odd[i & 1])) part_values(i);
+            }
             // the next tokens are looked up in the first step of the last that were
             const int next = i / AHEAD + 1;
-            const bool ask = i % AHEAD == 0 && (long)next * AHEAD < steps;
+            const bool ask = more && i % AHEAD == 0 && (long)next * AHEAD < steps;
             const int page = ask ? page_of(next) : -1;
-            compute(i, hidden, more);
+            compute(i, parity, hidden, morec);
             if (more) store(i + 1);
             if (ask) look_up(next, page);
             if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); // what is on its way into LDS
-        }
+        };
+        int i = 0;
+        for (; i + 1 < steps; ++i) step(i, i & 1, std::true_type{});
+        step(i, i & 1, std::false_type{});
     }
     l += __shfl_xor(l, 32);
     if (!real) return;
@@ -481,8 +482,9 @@ int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream)
         constexpr bool E8 = decltype(e8c)::value;
         auto width = [&](auto ndc) {
             constexpr int ND = decltype(ndc)::value;
-            if constexpr (ND <= 4) hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, 2, 4, 2>), grid, block, 0, st, a, (int)places);
-            else hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, 1, 4, 1>), grid, block, 0, st, a, (int)places);
+            constexpr int OCC = ND <= 4 ? 2 : 1, NSUB = ND <= 4 ? 2 : 1;
+            if (D == 32 * ND) hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, NSUB, 4, OCC, true>), grid, block, 0, st, a, (int)places);
+            else hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, NSUB, 4, OCC, false>), grid, block, 0, st, a, (int)places);
         };
         if (D <= 64) width(std::integral_constant<int, 2>{});
         else if (D <= 96) width(std::integral_constant<int, 3>{});
