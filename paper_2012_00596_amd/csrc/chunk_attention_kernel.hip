@@ -5,6 +5,7 @@
 #include "cache8.h"
 #include "decoder_internal.h"
 #include "device_util.h"
+#include "run_tiles.h"
 
 namespace npas {
 
@@ -49,44 +50,6 @@ __device__ __forceinline__ float over_halves(float x)
     return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
 }
 
-// Tile of a workgroup: BM rows (token, query head of the key head) of one sequence.
-struct Tile {
-    int s, token0, row0, rows; // sequence, its first row of q, first row of the tile and rows from there on within the run
-    int at0;                   // position of the run's first token
-    int length;
-};
-// Sequence s owns the places [start G / BM] + s .. of the grid: as many as its rows need, whatever the parting.
-template <int BM> __device__ __forceinline__ bool find_tile(const ChunkArgs &a, int place, int group, Tile &t)
-{
-    auto bounded = [&](int start) { return max(0, min(start, a.T)); };
-    auto first = [&](int start, int s) { return (int)((long)start * group / BM) + s; };
-    const int lane = threadIdx.x & 63;
-    int begin = 0, after = 0, n = 0; // of the last sequence that begins at or before this place
-    t.s = -1;
-    for (int s0 = 0; s0 < a.c.sequences; s0 += 64) {
-        const int s = min(s0 + lane, a.c.sequences - 1), b = bounded(a.start[s]), e = bounded(a.start[s + 1]), len = a.length[s];
-        const int here = __popcll(__ballot(s0 + lane < a.c.sequences && first(b, s) <= place));
-        if (here) {
-            t.s = s0 + here - 1;
-            begin = __builtin_amdgcn_readlane(b, here - 1);
-            after = __builtin_amdgcn_readlane(e, here - 1);
-            n = __builtin_amdgcn_readlane(len, here - 1);
-        }
-        if (here < 64) break;
-    }
-    if (t.s < 0) return false;
-    t.token0 = begin;
-    const int run = max(0, after - begin);
-    t.row0 = (place - first(begin, t.s)) * BM;
-    t.rows = run * group - t.row0;
-    const long room = (long)a.c.table_stride * a.c.page_size;
-    n = max(0, min(n, a.max_length));
-    if (n > room) n = (int)room;
-    t.length = n;
-    t.at0 = n - run;
-    return t.rows > 0;
-}
-
 // One workgroup a (tile of BM = 32 WAVES rows, key head, cut).  A wave has 32 rows as columns of 32 x 32 x 16 matrix instructions and walks the tokens in steps of
 // BN = 32 NSUB: scores S = K Q^T (row operand: keys from LDS as they lie), running maximum and sum a column, O^T = V^T P^T, where the weights
 // are the column operand as the first product leaves them, if a step's tokens are counted so that a lane's half h has tokens 4 h .. 4 h + 3 of
@@ -94,7 +57,7 @@ template <int BM> __device__ __forceinline__ bool find_tile(const ChunkArgs &a, 
 // Keys and values of a step come through registers into one of two places in LDS (16-byte pieces in an order that spreads rows over the banks; 8-bit
 // floats become 16-bit numbers on the way) while the other is multiplied; the cache rows of the tokens are looked up two steps ahead.
 // The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled.
-template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a, int places)
+template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a)
 {
     constexpr int DP = 32 * ND, BM = 32 * WAVES, BN = 32 * NSUB, THREADS = 64 * WAVES, PIECES = DP / 8, STRIDE = DP * 2;
     constexpr int UNITS = E8 ? BN * PIECES / 2 : BN * PIECES, PER = (UNITS + THREADS - 1) / THREADS, IN_ROW = E8 ? PIECES / 2 : PIECES;
@@ -111,9 +74,9 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
     uint32_t id = blockIdx.x;
     const int kvh = id % a.c.kv_heads, head0 = kvh * group;
     id /= a.c.kv_heads;
-    const int cut = id % a.splits, place = places - 1 - (int)(id / a.splits); // (the last tiles of a run have most to do)
-    Tile t;
-    if (!find_tile<BM>(a, place, group, t)) return;
+    const int cut = id % a.splits, place = a.places - 1 - (int)(id / a.splits); // (the last tiles of a run have most to do)
+    RunTile t;
+    if (!find_run_tile<BM>(a, place, group, t)) return;
 
     // the lane's row
     const int row = 32 * wave + r;
@@ -468,29 +431,25 @@ template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_ke
     if (lane == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-int chunk_tile_rows(int head_dim, int few) { return 128; }
-
 int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream)
 {
     hipStream_t st = (hipStream_t)stream;
-    const int group = a.heads / a.c.kv_heads, D = a.c.head_dim;
-    const long places = (long)a.T * group / chunk_tile_rows(D, a.few) + a.c.sequences;
-    if (int rc = check_grid("chunk attention", (uint64_t)places * a.splits * a.c.kv_heads, 256)) return rc;
-    const dim3 grid((unsigned)(places * a.splits * a.c.kv_heads)), block(256);
+    const int D = a.c.head_dim;
+    const uint64_t workgroups = (uint64_t)a.places * a.splits * a.c.kv_heads;
+    if (int rc = check_grid("chunk attention", workgroups, 2 * kChunkRows)) return rc;
+    const dim3 grid((unsigned)workgroups), block(2 * kChunkRows);
     auto run = [&](auto dtc, auto e8c) {
         constexpr int DT = decltype(dtc)::value;
         constexpr bool E8 = decltype(e8c)::value;
         auto width = [&](auto ndc) {
-            constexpr int ND = decltype(ndc)::value;
-            constexpr int OCC = ND <= 4 ? 2 : 1, NSUB = ND <= 4 ? 2 : 1;
-            if (D == 32 * ND) hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, NSUB, 4, OCC, true>), grid, block, 0, st, a, (int)places);
-            else hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, NSUB, 4, OCC, false>), grid, block, 0, st, a, (int)places);
+            constexpr int ND = decltype(ndc)::value, OCC = ND <= 4 ? 2 : 1, NSUB = ND <= 4 ? 2 : 1;
+            if (D == 32 * ND) hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, NSUB, kChunkRows / 32, OCC, true>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((chunk_attention_kernel<DT, E8, ND, NSUB, kChunkRows / 32, OCC, false>), grid, block, 0, st, a);
         };
         if (D <= 64) width(std::integral_constant<int, 2>{});
         else if (D <= 96) width(std::integral_constant<int, 3>{});
         else if (D <= 128) width(std::integral_constant<int, 4>{});
         else width(std::integral_constant<int, 8>{});
-        if (a.splits > 1) hipLaunchKernelGGL((chunk_attention_join_kernel<DT>), dim3((unsigned)(((size_t)a.T * a.heads + 3) / 4)), dim3(256), 0, st, a);
     };
     auto cache = [&](auto dtc) {
         if (a.c.k_scale) run(dtc, std::true_type{});
@@ -498,6 +457,17 @@ int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream)
     };
     if (dt == NPAS_BF16) cache(std::integral_constant<int, NPAS_BF16>{});
     else cache(std::integral_constant<int, NPAS_F16>{});
+    return launched("chunk attention");
+}
+
+int launch_chunk_join(int dt, const ChunkArgs &a, void *stream)
+{
+    hipStream_t st = (hipStream_t)stream;
+    const uint64_t workgroups = ((uint64_t)a.T * a.heads + 3) / 4;
+    if (int rc = check_grid("chunk attention", workgroups, 256)) return rc;
+    const dim3 grid((unsigned)workgroups), block(256);
+    if (dt == NPAS_BF16) hipLaunchKernelGGL((chunk_attention_join_kernel<NPAS_BF16>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((chunk_attention_join_kernel<NPAS_F16>), grid, block, 0, st, a);
     return launched("chunk attention");
 }
 

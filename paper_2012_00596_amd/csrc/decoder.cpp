@@ -43,14 +43,6 @@ int check_cache(const npas_kv_cache *c, const npas_kv_scales *scales, int heads,
     return NPAS_OK;
 }
 
-} // namespace npas
-
-using namespace npas;
-
-namespace {
-
-bool storage(int dt) { return dt == NPAS_F32 || dt == NPAS_BF16 || dt == NPAS_F16; }
-
 // How a launch cuts the tokens.  A pair is a sequence's key head (with up to 16 of its query heads): one workgroup a pair and cut.
 //   - Up to kSingle elements of keys a pair one cut: the joining launch takes longer to issue (1.6 to 2.4 us) than it saves (from call to call: 16
 //     pairs of 777 tokens, head_dim 64, 8.0 us in one cut, 9.3 in seven; replayed from a graph 8.2 and 7.1; 128 pairs of 300 tokens,
@@ -62,16 +54,11 @@ bool storage(int dt) { return dt == NPAS_F32 || dt == NPAS_BF16 || dt == NPAS_F1
 //     up to 8192 tokens 227 us, in one cut 225).
 // Cuts follow max_length, not the lengths, which are on the device: a launch for much longer sequences than it meets leaves compute units idle
 // (8 pairs of 4096 tokens, head_dim 128, 8.7 us at max_length 4096, 11.7 at 32768, 25.5 at 131072; 128 pairs of 2048 26 us, 65 at 32768).
-struct Cuts {
-    int chunk, splits, waves;
-    size_t stat_at, need, bytes; // (maximum, sum) pairs lie behind the sums; need: of this launch, bytes: enough for any window
-};
-Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
+Cuts plan_cuts(const CacheArgs &c, long pairs, size_t rows, int max_length, int window)
 {
     constexpr long kWorkgroups = 512, kLeast = 128, kMost = 2048, kSingle = 65536;
     const long room = (long)c.table_stride * c.page_size, longest = max_length < room ? max_length : room;
     const long n = window > 0 && window < longest ? window : longest;
-    const long group = heads / c.kv_heads, pairs = (long)c.sequences * c.kv_heads * ((group + 15) / 16);
     Cuts k{};
     const bool single = n * c.head_dim <= kSingle;
     k.waves = single && c.head_dim <= 128 && pairs <= 256 ? 8 : 4;
@@ -90,12 +77,24 @@ Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
     if (most > (share > capped ? share : capped)) most = share > capped ? share : capped;
     if (most > kMaxSplits) most = kMaxSplits;
     if (longest * c.head_dim <= kSingle) most = 1;
-    const size_t rows = (size_t)c.sequences * heads;
     k.stat_at = rows * k.splits * c.head_dim * 4;
     if (k.splits > 1) k.need = rows * k.splits * (c.head_dim * 4 + 8);
     if (most > 1) k.bytes = rows * most * (c.head_dim * 4 + 8);
     return k;
 }
+
+} // namespace npas
+
+using namespace npas;
+
+namespace {
+
+Cuts plan_cuts(const CacheArgs &c, int heads, int max_length, int window)
+{
+    const long group = heads / c.kv_heads;
+    return npas::plan_cuts(c, (long)c.sequences * c.kv_heads * ((group + 15) / 16), (size_t)c.sequences * heads, max_length, window);
+}
+bool storage(int dt) { return dt == NPAS_F32 || dt == NPAS_BF16 || dt == NPAS_F16; }
 
 int paged_attention(const npas_kv_cache *cache, const npas_kv_scales *scales, const void *q_dev, int64_t q_stride, void *y_dev, float *lse_dev,
                     int heads, const int32_t *length_dev, int max_length, int window, float scale, void *workspace_dev, size_t workspace_bytes,

@@ -51,6 +51,9 @@ struct AttentionArgs {
     int chunk, splits, waves; // waves of a workgroup, 4 or 8
     float *part;
     float2 *part_stat;
+    // runs of new tokens: rows [T][heads] of q and y, start [sequences + 1], workgroups a key head and cut
+    const int32_t *start;
+    int T, places;
 };
 constexpr int kMaxSplits = 512;
 
@@ -82,12 +85,18 @@ struct ChunkArgs {
     int T, heads, max_length, window;
     float scale;
     // cuts of `chunk` tokens; more than one: unnormalised sums [row][cut][head_dim] and (maximum, sum) of each, rows [T][heads]
-    int chunk, splits, few; // few: the form for runs of few rows
+    int chunk, splits, places; // places: workgroups a key head and cut
     float *part;
     float2 *part_stat;
 };
-// Rows (tokens x query heads of a key head) of a workgroup's tile.
-int chunk_tile_rows(int head_dim, int few);
+constexpr int kChunkRows = 128; // (token, query head of a key head) of a workgroup's tile
+
+// How a launch of single tokens cuts the tokens; `pairs`: workgroups a cut, `rows`: of y.
+struct Cuts {
+    int chunk, splits, waves;
+    size_t stat_at, need, bytes; // (maximum, sum) pairs lie behind the sums; need: of this launch, bytes: enough for any window
+};
+Cuts plan_cuts(const CacheArgs &c, long pairs, size_t rows, int max_length, int window);
 
 int launch_gated_residual_norm(int dt, const NormArgs &a, void *stream);
 int launch_kv_append(int dt, const AppendArgs &a, void *stream);
@@ -95,6 +104,8 @@ int launch_paged_attention(int dt, const AttentionArgs &a, void *stream);
 int launch_kv_write(int dt, const WriteArgs &a, void *stream);
 int launch_kv_read(int dt, const ReadArgs &a, void *stream);
 int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream);
+int launch_short_runs(int dt, const AttentionArgs &a, int groups, void *stream); // groups of 16 rows
+int launch_chunk_join(int dt, const ChunkArgs &a, void *stream);
 
 // Arguments that the calls on a cache share.  scales NULL: a cache of 16 bits; dt: storage type of the rows outside.
 int check_cache(const npas_kv_cache *c, const npas_kv_scales *scales, int heads, CacheArgs *out, int *dt);

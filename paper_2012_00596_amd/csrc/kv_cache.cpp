@@ -6,12 +6,13 @@ using namespace npas;
 
 namespace {
 
-// How a launch takes the rows and cuts the tokens.
-//   few: tiles of few rows, whose waves part the tokens among them, where the mean run has no more rows than that.
-//   Where the tiles do not fill the card, a tile's tokens are cut over workgroups, at least kLeast each.
+// How a launch takes the rows and cuts the tokens.  Rows: (token, query head) of a key head.
+//   - Runs of up to 32 rows on average: the kernel of single tokens with one or two groups of 16 rows, cut as that is.
+//   - Longer ones: tiles of kChunkRows; where they do not fill the card, a tile's tokens are cut over workgroups, at least kLeast each.
 struct ChunkPlan {
-    int few, chunk, splits;
-    size_t stat_at, need, bytes; // (maximum, sum) pairs lie behind the sums; need: of this launch, bytes: enough for any window
+    int groups; // of 16 rows; 0: tiles of kChunkRows
+    long places;
+    Cuts cuts;
 };
 ChunkPlan plan_chunks(const CacheArgs &c, int T, int heads, int max_length, int window)
 {
@@ -19,26 +20,27 @@ ChunkPlan plan_chunks(const CacheArgs &c, int T, int heads, int max_length, int 
     const long room = (long)c.table_stride * c.page_size, longest = max_length < room ? max_length : room;
     const long group = heads / c.kv_heads, rows = (long)T * group, mean = (rows + c.sequences - 1) / c.sequences;
     ChunkPlan k{};
-    k.few = mean <= 48;
-    const long tile = chunk_tile_rows(c.head_dim, k.few), tiles = c.sequences * ((mean + tile - 1) / tile);
-    const long n = window > 0 && window < longest - tile ? window + tile : longest; // tokens that a tile's rows see
+    k.groups = mean <= 16 || (mean <= 32 && c.head_dim > 128) ? 1 : mean <= 32 ? 2 : 0;
+    const long tile = k.groups ? 16 * k.groups : kChunkRows, tiles = c.sequences * ((mean + tile - 1) / tile);
+    k.places = rows / tile + c.sequences;
+    const long seen = window > 0 && window < longest - tile ? window + tile : longest; // tokens that a tile's rows see
+    if (k.groups) {
+        k.cuts = plan_cuts(c, tiles * c.kv_heads, (size_t)T * heads, max_length, (int)seen);
+        if (k.groups == 2) k.cuts.waves = 4;
+        return k;
+    }
     long want = (kWorkgroups + tiles * c.kv_heads - 1) / (tiles * c.kv_heads); // cuts
     if (want > kMost) want = kMost;
-    auto cuts = [&](long tokens, long &chunk) {
-        chunk = (tokens + want - 1) / want;
-        if (chunk < kLeast) chunk = kLeast;
-        chunk = (chunk + 127) / 128 * 128;
-        return (tokens + chunk - 1) / chunk;
-    };
-    long chunk, most;
-    k.splits = (int)cuts(n, chunk);
-    k.chunk = (int)chunk;
-    most = (longest + kLeast - 1) / kLeast; // over all windows
-    if (most > want) most = want;
+    long chunk = (seen + want - 1) / want, most = (longest + kLeast - 1) / kLeast;
+    if (chunk < kLeast) chunk = kLeast;
+    chunk = (chunk + 127) / 128 * 128;
+    if (most > want) most = want; // over all windows
+    k.cuts.chunk = (int)chunk;
+    k.cuts.splits = (int)((seen + chunk - 1) / chunk);
     const size_t all = (size_t)T * heads, each = (size_t)c.head_dim * 4 + 8;
-    k.stat_at = all * k.splits * c.head_dim * 4;
-    if (k.splits > 1) k.need = all * k.splits * each;
-    if (most > 1) k.bytes = all * most * each;
+    k.cuts.stat_at = all * k.cuts.splits * c.head_dim * 4;
+    if (k.cuts.splits > 1) k.cuts.need = all * k.cuts.splits * each;
+    if (most > 1) k.cuts.bytes = all * most * each;
     return k;
 }
 
@@ -114,7 +116,7 @@ size_t npas_chunk_attention_workspace_bytes(const npas_kv_cache *cache, const np
     CacheArgs c;
     int dt;
     if (check_cache(cache, scales, heads, &c, &dt) || check_chunk(c, T, heads, max_length)) return 0;
-    return plan_chunks(c, T, heads, max_length, 0).bytes;
+    return plan_chunks(c, T, heads, max_length, 0).cuts.bytes;
 }
 
 int npas_chunk_attention(const npas_kv_cache *cache, const npas_kv_scales *scales, const void *q_dev, int64_t q_stride, void *y_dev,
@@ -138,16 +140,25 @@ int npas_chunk_attention(const npas_kv_cache *cache, const npas_kv_scales *scale
         return NPAS_E_SHAPE;
     }
     const ChunkPlan plan = plan_chunks(a.c, T, heads, max_length, window);
-    if (plan.need && (!workspace_dev || workspace_bytes < plan.need || misaligned(workspace_dev, 16))) {
-        set_error("chunk attention needs %zu bytes of workspace at a multiple of 16, got %zu at %p", plan.need, workspace_bytes, workspace_dev);
+    const Cuts &cuts = plan.cuts;
+    if (cuts.need && (!workspace_dev || workspace_bytes < cuts.need || misaligned(workspace_dev, 16))) {
+        set_error("chunk attention needs %zu bytes of workspace at a multiple of 16, got %zu at %p", cuts.need, workspace_bytes, workspace_dev);
         return NPAS_E_WORKSPACE;
     }
     a.q = q_dev; a.y = y_dev; a.lse = lse_dev; a.q_stride = q_stride; a.start = start_dev; a.length = length_dev;
     a.T = T; a.heads = heads; a.max_length = max_length; a.window = window; a.scale = scale;
-    a.chunk = plan.chunk; a.splits = plan.splits; a.few = plan.few;
+    a.chunk = cuts.chunk; a.splits = cuts.splits; a.places = (int)plan.places;
     a.part = (float *)workspace_dev;
-    a.part_stat = (float2 *)((uint8_t *)workspace_dev + plan.stat_at);
-    return launch_chunk_attention(dt, a, hip_stream);
+    a.part_stat = (float2 *)((uint8_t *)workspace_dev + cuts.stat_at);
+    if (plan.groups) {
+        AttentionArgs r{};
+        r.c = a.c; r.q = a.q; r.y = a.y; r.lse = a.lse; r.q_stride = a.q_stride; r.start = a.start; r.length = a.length;
+        r.T = T; r.heads = heads; r.max_length = max_length; r.window = window; r.scale = scale;
+        r.chunk = a.chunk; r.splits = a.splits; r.waves = cuts.waves; r.places = a.places;
+        r.part = a.part; r.part_stat = a.part_stat;
+        if (int rc = launch_short_runs(dt, r, plan.groups, hip_stream)) return rc;
+    } else if (int rc = launch_chunk_attention(dt, a, hip_stream)) return rc;
+    return a.splits > 1 ? launch_chunk_join(dt, a, hip_stream) : NPAS_OK;
 }
 
 } // extern "C"
