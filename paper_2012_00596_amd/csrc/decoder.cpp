@@ -56,7 +56,8 @@ int check_cache(const npas_kv_cache *c, const npas_kv_scales *scales, int heads,
 // (8 pairs of 4096 tokens, head_dim 128, 8.7 us at max_length 4096, 11.7 at 32768, 25.5 at 131072; 128 pairs of 2048 26 us, 65 at 32768).
 Cuts plan_cuts(const CacheArgs &c, long pairs, size_t rows, int max_length, int window)
 {
-    constexpr long kWorkgroups = 512, kLeast = 128, kMost = 2048, kSingle = 65536;
+    constexpr long kWorkgroups = 512, kLeast = 128, kSingle = 65536;
+    const long kMost = c.k_scale ? 1024 : 2048;
     const long room = (long)c.table_stride * c.page_size, longest = max_length < room ? max_length : room;
     const long n = window > 0 && window < longest ? window : longest;
     Cuts k{};

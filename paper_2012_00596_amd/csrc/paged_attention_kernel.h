@@ -63,11 +63,14 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
     uint32_t id = blockIdx.x;
     const int kv = id % a.c.kv_heads;
     id /= a.c.kv_heads;
+    // Workgroups go to the compute units in turn, so the cuts of a sequence start at one or another: in their order, the last, often empty ones would all meet
+    // the same units (@@).
+    auto turned = [&](uint32_t n) { return (int)((id % a.splits + (n * 0x9e3779b1u >> 16)) % a.splits); };
     int h0 = 0, split, s, first, count; // h0: first of the group's heads here
     RunTile tile_of_run{};
     int at_first = 0, at_last = 0; // positions of the first and the last row
     if constexpr (RUNS) {
-        split = id % a.splits;
+        split = turned(id / a.splits);
         if (!find_run_tile<16 * G>(a, (int)(id / a.splits), group, tile_of_run)) return;
         s = tile_of_run.s;
         at_first = tile_of_run.at0 + tile_of_run.row0 / group;
@@ -77,7 +80,8 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
     } else {
         h0 = id % head_tiles * 16;
         id /= head_tiles;
-        split = id % a.splits, s = id / a.splits;
+        s = id / a.splits;
+        split = turned(s);
         token_range(a, s, first, count);
     }
     const long from = (long)split * a.chunk;
