@@ -414,14 +414,23 @@ template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_ke
     for (int w = 32; w; w >>= 1) m = fmaxf(m, __shfl_xor(m, w));
     float l = 0.f;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < a.splits; ++i) {
-        const float2 x = stat[i];
-        if (x.x == -INFINITY) continue;
-        const float c = __builtin_amdgcn_exp2f(x.x - m);
-        l += c * x.y;
-        if (lane * 4 < D) {
-            const float4 v = *reinterpret_cast<const float4 *>(a.part + (row * a.splits + i) * D + lane * 4);
-            y.x += c * v.x, y.y += c * v.y, y.z += c * v.z, y.w += c * v.w;
+    constexpr int SIDE = 4; // cuts on their way
+    for (int i0 = 0; i0 < a.splits; i0 += SIDE) {
+        float2 x[SIDE];
+        float4 v[SIDE];
+#pragma unroll
+        for (int k = 0; k < SIDE; ++k) x[k] = stat[min(i0 + k, a.splits - 1)];
+#pragma unroll
+        for (int k = 0; k < SIDE; ++k) {
+            if (i0 + k >= a.splits) x[k].x = -INFINITY;
+            v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (x[k].x != -INFINITY && lane * 4 < D) v[k] = *reinterpret_cast<const float4 *>(a.part + (row * a.splits + i0 + k) * D + lane * 4);
+        }
+#pragma unroll
+        for (int k = 0; k < SIDE; ++k) {
+            const float c = x[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[k].x - m);
+            l += x[k].x == -INFINITY ? 0.f : c * x[k].y;
+            y.x += c * v[k].x, y.y += c * v[k].y, y.z += c * v[k].z, y.w += c * v[k].w;
         }
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;

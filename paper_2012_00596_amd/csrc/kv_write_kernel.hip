@@ -26,14 +26,39 @@ __device__ __forceinline__ Place place_of(const CacheArgs &c, const int32_t *seq
     return p;
 }
 
+// Another lane's value by a fixed pattern within 16 lanes, without LDS.
+template <int CTRL> __device__ __forceinline__ uint32_t lane16(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true); }
+template <int CTRL> __device__ __forceinline__ float lane16(float x) { return __uint_as_float(lane16<CTRL>(__float_as_uint(x))); }
+constexpr int kLaneXor1 = 0xb1, kLaneXor2 = 0x4e, kQuadMirror = 0x1b, kMirror8 = 0x141, kMirror16 = 0x140, kTurn8 = 0x128;
+// Sum over P lanes, the same bits in each: a tree whose steps add what both sides add.
+template <int P> __device__ __forceinline__ float lanes_sum(float s)
+{
+    s += lane16<kLaneXor1>(s);
+    s += lane16<kLaneXor2>(s);
+    s += lane16<kMirror8>(s);
+    if constexpr (P >= 16) s += lane16<kMirror16>(s);
+    if constexpr (P >= 32) s += __shfl_xor(s, 16);
+    return s;
+}
+// The value of the lane P / 2 away, of P.
+template <int P> __device__ __forceinline__ float far_half(float x)
+{
+    if constexpr (P == 8) return lane16<kQuadMirror>(lane16<kMirror8>(x));
+    else if constexpr (P == 16) return lane16<kTurn8>(x);
+    else return __shfl_xor(x, 16);
+}
+
+// How a rotation's partners are found: in the lane itself (PAIRS), half a head away, some lanes away, or through LDS.
+enum { PAIRS, FAR_HALF, LANES, LDS };
+
 // One workgroup a token.  P lanes, a power of two, hold a head, eight consecutive elements each; heads follow each other (queries, keys, values), four of a
 // lane's on their way at once.  A lane's elements are the same in every head, so that its angles and weights are read once.
-// The sum of squares is a tree over the P lanes; a rotation's partners, where they are another lane's, come by a shuffle (WHOLE: half of rot_dim is a multiple
-// of eight) or through LDS.  A block of 8-bit floats is four lanes.
-template <int DT, bool E8, bool PAIRS, bool WHOLE, int P> __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a)
+// The sum of squares is a tree over the P lanes.  A block of 8-bit floats is four lanes.
+template <int DT, bool E8, int ROT, int P> __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a)
 {
     constexpr int SIDE = 4; // heads of a lane on their way
-    __shared__ __align__(16) float pass[PAIRS || WHOLE ? 1 : 2048];
+    __shared__ __align__(16) float pass[ROT == LDS ? 2048 : 1];
+    constexpr bool WHOLE = ROT == FAR_HALF || ROT == LANES; // half of rot_dim is a multiple of eight
     const int t = blockIdx.x, D = a.c.head_dim, half = a.rot_dim / 2, in_head = threadIdx.x % P, d = in_head * 8, groups = blockDim.x / P;
     const Place at = place_of(a.c, a.sequence, a.position, t, a.rot_dim ? (uint32_t)a.positions : 0x80000000u);
     const bool mine = d < D, rotated = mine && d < a.rot_dim; // (WHOLE or not, a vector may pass the end of the rotated part)
@@ -41,7 +66,7 @@ template <int DT, bool E8, bool PAIRS, bool WHOLE, int P> __global__ __launch_bo
     float cs[8], sn[8], wq[8], wk[8];
     if (rotated) {
         const float *row = a.cos_sin + (size_t)at.position * a.rot_dim;
-        if constexpr (PAIRS) {
+        if constexpr (ROT == PAIRS) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int i = d / 2 + k;
@@ -59,7 +84,7 @@ template <int DT, bool E8, bool PAIRS, bool WHOLE, int P> __global__ __launch_bo
                 cs[k] = e < a.rot_dim ? row[i] : 1.f;
                 sn[k] = e < a.rot_dim ? row[half + i] : 0.f;
             }
-        if constexpr (!PAIRS)
+        if constexpr (ROT != PAIRS)
 #pragma unroll
             for (int k = 0; k < 8; ++k) sn[k] = d + k < half ? -sn[k] : sn[k];
     }
@@ -87,14 +112,12 @@ template <int DT, bool E8, bool PAIRS, bool WHOLE, int P> __global__ __launch_bo
                 float s = 0.f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) s = fmaf(x[j][k], x[j][k], s);
-#pragma unroll
-                for (int o = P / 2; o; o >>= 1) s += __shfl_xor(s, o);
-                const float r = 1.f / sqrtf(s / (float)D + a.eps);
+                const float r = 1.f / sqrtf(lanes_sum<P>(s) / (float)D + a.eps);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) x[j][k] = mine ? x[j][k] * r * (is_q ? wq[k] : wk[k]) : 0.f;
             }
             if (a.rot_dim && (is_q || is_k)) {
-                if constexpr (PAIRS) {
+                if constexpr (ROT == PAIRS) {
                     if (rotated)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
@@ -104,7 +127,10 @@ template <int DT, bool E8, bool PAIRS, bool WHOLE, int P> __global__ __launch_bo
                         }
                 } else {
                     float p[8];
-                    if constexpr (WHOLE) {
+                    if constexpr (ROT == FAR_HALF) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) p[k] = far_half<P>(x[j][k]);
+                    } else if constexpr (ROT == LANES) {
                         const int from = (d < half ? in_head + half / 8 : in_head - half / 8) & (P - 1);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) p[k] = __shfl(x[j][k], from, P);
@@ -143,8 +169,8 @@ template <int DT, bool E8, bool PAIRS, bool WHOLE, int P> __global__ __launch_bo
                 uint32_t top = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[j][k]) & 0x7fffffffu);
-                top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-                top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+                top = max(top, lane16<kLaneXor1>(top));
+                top = max(top, lane16<kLaneXor2>(top));
                 const uint32_t byte = scale8_of<DT>(top);
                 const uint2 codes = to_e4m3x8<DT>(x[j], byte);
                 if (mine) {
@@ -166,9 +192,10 @@ int launch_kv_write(int dt, const WriteArgs &a, void *stream)
     auto form = [&](auto dtc, auto e8c, auto lanesc) {
         constexpr int DT = decltype(dtc)::value, P = decltype(lanesc)::value;
         constexpr bool E8 = decltype(e8c)::value;
-        if (a.pairs) hipLaunchKernelGGL((kv_write_kernel<DT, E8, true, true, P>), grid, block, 0, st, a);
-        else if (a.rot_dim % 16 == 0) hipLaunchKernelGGL((kv_write_kernel<DT, E8, false, true, P>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((kv_write_kernel<DT, E8, false, false, P>), grid, block, 0, st, a);
+        if (a.pairs) hipLaunchKernelGGL((kv_write_kernel<DT, E8, PAIRS, P>), grid, block, 0, st, a);
+        else if (a.rot_dim == 8 * P) hipLaunchKernelGGL((kv_write_kernel<DT, E8, FAR_HALF, P>), grid, block, 0, st, a);
+        else if (a.rot_dim % 16 == 0) hipLaunchKernelGGL((kv_write_kernel<DT, E8, LANES, P>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((kv_write_kernel<DT, E8, LDS, P>), grid, block, 0, st, a);
     };
     auto width = [&](auto dtc, auto e8c) {
         if (lanes == 8) form(dtc, e8c, std::integral_constant<int, 8>{});

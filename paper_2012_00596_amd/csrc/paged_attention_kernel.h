@@ -53,8 +53,9 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
 {
     constexpr int G = RUNS ? RUNS : 1; // groups of 16 columns
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
-    constexpr int PITCH = DP + 4, PARTS = 3;
-    constexpr float TOP = DT == NPAS_BF16 ? 1.f : 32768.f; // the largest weight
+    constexpr int PITCH = DP + 4, PARTS = RUNS ? 2 : 3;
+    constexpr float GROW = !RUNS ? 0.f : DT == NPAS_BF16 ? 8.f : 4.f; // the maximum in use follows a row's scores where one exceeds it by 2^GROW
+    constexpr float TOP = DT == NPAS_BF16 ? 1.f : RUNS ? 2048.f : 32768.f; // the largest weight is TOP 2^GROW
     __shared__ __align__(16) uint32_t rows[kRows];
     __shared__ float sm[NW][16], sl[NW][16];
     __shared__ __align__(16) float so[NW * 16 * PITCH];
@@ -282,14 +283,25 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
                     if (!sees(g, j0 + 16 * (i >> 2) + 4 * q + (i & 3))) hidden |= 1u << i;
             }
             float x[8], top = -INFINITY;
+            if constexpr (RUNS) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = hidden >> i & 1 ? -INFINITY : (i < 4 ? c0[g][i] : c1[g][i - 4]) * to2;
-                top = fmaxf(top, x[i]);
-            }
+                for (int i = 0; i < 8; ++i) x[i] = (i < 4 ? c0[g][i] : c1[g][i - 4]) * to2;
+                if (__any(hidden != 0)) {
+                    asm volatile("" : : : "memory");
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = hidden >> i & 1 ? -INFINITY : x[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+            } else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] = hidden >> i & 1 ? -INFINITY : (i < 4 ? c0[g][i] : c1[g][i - 4]) * to2;
+                    top = fmaxf(top, x[i]);
+                }
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            if (__any(top > m[g])) { // (an infinite score has an infinite weight, and so has the sum: finite maxima keep these from being NaN)
+            if (__any(top > m[g] + GROW)) { // (an infinite score has an infinite weight, and so has the sum: finite maxima keep these from being NaN)
                 const float now = fminf(fmaxf(m[g], top), FLT_MAX), c = m[g] == -INFINITY ? (RUNS ? 1.f : 0.f) : __builtin_amdgcn_exp2f(m[g] - now);
                 m[g] = now;
                 l[g] *= c;
