@@ -327,7 +327,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
                 }
 #pragma unroll
                 for (int u = 0; u < PER; ++u)
-                    if (more && u * PARTS * ND / PER == part * ND + dt) {
+                    if (more && u * PARTS * ND / PER / 2 == part * ND + dt) {
                         load(1 - parity, u, 1);
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -348,11 +348,12 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
         }
         store(0);
         if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        if (steps > 1) rows_of_step(1);
+        uint32_t hole_next = holes[0];
         auto step = [&](int i, auto parity, auto morec) __attribute__((always_inline)) {
             constexpr bool more = decltype(morec)::value; // another follows
             __syncthreads();
-            if (more) rows_of_step(i + 1);
-            const bool hidden = parted(i) || hole(i);
+            const bool hidden = parted(i) || __builtin_amdgcn_readfirstlane(hole_next);
             if (hidden) {
                 if (!E8) look_for_odd(i);
                 if (__builtin_amdgcn_readfirstlane(odd[i & 1])) part_values(i);
@@ -362,7 +363,11 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
             const bool ask = more && i % AHEAD == 0 && (long)next * AHEAD < steps;
             const int page = ask ? page_of(next) : -1;
             compute(i, parity, hidden, morec);
-            if (more) store(i + 1);
+            if (more) {
+                store(i + 1);
+                rows_of_step(i + 2); // (where there is such a step; the tokens were looked up at least a step ago)
+                hole_next = holes[(i + 1) % (2 * AHEAD)];
+            }
             if (ask) look_up(next, page);
             if (!E8) asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); // what is on its way into LDS
         };

@@ -62,7 +62,7 @@ template <int DT, bool E8, int ROT, int P> __global__ __launch_bounds__(256) voi
     const int t = blockIdx.x, D = a.c.head_dim, half = a.rot_dim / 2, in_head = threadIdx.x % P, d = in_head * 8, groups = blockDim.x / P;
     const Place at = place_of(a.c, a.sequence, a.position, t, a.rot_dim ? (uint32_t)a.positions : 0x80000000u);
     const bool mine = d < D, rotated = mine && d < a.rot_dim; // (WHOLE or not, a vector may pass the end of the rotated part)
-    const int nq = a.q ? a.heads : 0, units = nq + (at.stored ? 2 * a.c.kv_heads : 0);
+    const int nq = a.q ? a.heads : 0, units = nq + 2 * a.c.kv_heads; // (all are read: that need not wait for the page)
     float cs[8], sn[8], wq[8], wk[8];
     if (rotated) {
         const float *row = a.cos_sin + (size_t)at.position * a.rot_dim;
@@ -164,6 +164,7 @@ template <int DT, bool E8, int ROT, int P> __global__ __launch_bounds__(256) voi
                 if (mine) store8<DT>(a.q_out, ((size_t)t * a.heads + head) * D + d, 8, x[j]);
                 continue;
             }
+            if (!at.stored) continue;
             const size_t row = at.row + (size_t)head * a.c.page_size;
             if constexpr (E8) {
                 uint32_t top = 0;
