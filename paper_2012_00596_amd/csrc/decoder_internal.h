@@ -64,7 +64,7 @@ struct WriteArgs {
     int64_t q_stride, k_stride, v_stride;
     const int32_t *sequence, *position;
     const float *q_weight, *k_weight, *cos_sin;
-    float eps;
+    float eps, inv_d;
     int T, heads, positions, rot_dim, pairs;
 };
 

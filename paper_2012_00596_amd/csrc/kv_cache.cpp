@@ -84,7 +84,7 @@ int npas_kv_write(const npas_kv_cache *cache, const npas_kv_scales *scales, cons
     a.q = q_dev; a.k = k_dev; a.v = v_dev; a.q_out = q_out_dev;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
     a.sequence = sequence_dev; a.position = position_dev;
-    a.q_weight = q_weight_dev; a.k_weight = k_weight_dev; a.cos_sin = cos_sin_dev; a.eps = eps;
+    a.q_weight = q_weight_dev; a.k_weight = k_weight_dev; a.cos_sin = cos_sin_dev; a.eps = eps; a.inv_d = (float)(1.0 / a.c.head_dim);
     a.T = T; a.heads = heads; a.positions = positions; a.rot_dim = rot_dim; a.pairs = kind == NPAS_ROTATE_PAIRS;
     return launch_kv_write(dt, a, hip_stream);
 }

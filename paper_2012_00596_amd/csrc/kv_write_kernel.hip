@@ -63,7 +63,7 @@ template <int DT, bool E8, int ROT, int P> __global__ __launch_bounds__(256) voi
     const Place at = place_of(a.c, a.sequence, a.position, t, a.rot_dim ? (uint32_t)a.positions : 0x80000000u);
     const bool mine = d < D, rotated = mine && d < a.rot_dim; // (WHOLE or not, a vector may pass the end of the rotated part)
     const int nq = a.q ? a.heads : 0, units = nq + 2 * a.c.kv_heads; // (all are read: that need not wait for the page)
-    float cs[8], sn[8], wq[8], wk[8];
+    float cs[8] = {}, sn[8] = {}, wq[8] = {}, wk[8] = {};
     if (rotated) {
         const float *row = a.cos_sin + (size_t)at.position * a.rot_dim;
         if constexpr (ROT == PAIRS) {
@@ -112,9 +112,15 @@ template <int DT, bool E8, int ROT, int P> __global__ __launch_bounds__(256) voi
                 float s = 0.f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) s = fmaf(x[j][k], x[j][k], s);
-                const float r = 1.f / sqrtf(lanes_sum<P>(s) / (float)D + a.eps);
+                const float r = __builtin_amdgcn_rsqf(fmaf(lanes_sum<P>(s), a.inv_d, a.eps)); // (an ulp; what lies behind the head is zero and stays so)
+                if (is_q) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[j][k] = mine ? x[j][k] * r * (is_q ? wq[k] : wk[k]) : 0.f;
+                    for (int k = 0; k < 8; ++k) x[j][k] *= r * wq[k];
+                } else {
+                    asm volatile(""); // (two paths, one of which a wave mostly takes, not a choice for every weight)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[j][k] *= r * wk[k];
+                }
             }
             if (a.rot_dim && (is_q || is_k)) {
                 if constexpr (ROT == PAIRS) {
