@@ -86,7 +86,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
     const size_t out_row = (size_t)(t.token0 + token) * a.heads + head;
     // tokens that some row of the tile sees, and this cut's share
     const int last_row = min(t.rows, BM) - 1, at_first = t.at0 + t.row0 / group, at_last = t.at0 + (t.row0 + last_row) / group;
-    const int end = max(0, at_last + 1), from0 = a.window > 0 ? max(0, at_first - a.window + 1) : 0;
+    const int end = max(0, at_last + 1), from0 = a.window > 0 ? (int)max(0l, (long)at_first - a.window + 1) : 0;
     const int from = (int)min((long)end, from0 + (long)cut * a.chunk), to = (int)min((long)end, (long)from + a.chunk);
     const int steps = (to - from + BN - 1) / BN;
 
@@ -127,8 +127,9 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
     auto rows_of = [&](int i) { return ring + i % (2 * AHEAD) * BN; };
     // Every row sees every token of the steps lo .. hi - 1.
     const int hi = (int)max(0l, min((long)steps, ((long)at_first + 1 - from) >> (BN == 64 ? 6 : 5)));
-    const int lo = a.window > 0 ? (int)max(0l, min((long)steps, ((long)at_last - a.window - from) / BN + 1)) : 0;
-    auto parted = [&](int i) { return i >= hi || (i < lo && at_last - a.window >= from); };
+    const long behind_all = (long)at_last - a.window - from; // the last token that some row has left behind
+    const int lo = a.window > 0 && behind_all >= 0 ? (int)min((long)steps, behind_all / BN + 1) : 0;
+    auto parted = [&](int i) { return i >= hi || i < lo; };
     auto hole = [&](int i) { return __builtin_amdgcn_readfirstlane(holes[i % (2 * AHEAD)]) != 0; };
     // The next step's keys and values are asked for a part at a time, between the products: a wave that asks for all at once stands still while the compute unit
     // takes them in, 64 bytes a cycle.  A part is 64 pieces of the wave, or 64 sixteens of 8-bit floats; its address is one multiplication and addition.
@@ -188,7 +189,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
     };
     // the tokens of 32 from step i's sub-step u that the lane's row sees, a bit each
     auto seen = [&](int i, int u) __attribute__((always_inline)) {
-        const long base = (long)from + (long)i * BN + 32 * u, past = at - base, before = a.window > 0 ? at - a.window + 1 - base : 0;
+        const long base = (long)from + (long)i * BN + 32 * u, past = at - base, before = a.window > 0 ? (long)at - a.window + 1 - base : 0;
         uint32_t bits = ~gone[i % (2 * AHEAD) * NSUB + u];
         if (past < 31) bits &= past < 0 ? 0u : (2u << past) - 1u;
         if (before > 0) bits &= before > 31 ? 0u : ~0u << before;

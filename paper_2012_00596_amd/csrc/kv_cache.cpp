@@ -35,6 +35,9 @@ ChunkPlan plan_chunks(const CacheArgs &c, int T, int heads, int max_length, int 
     if (chunk < kLeast) chunk = kLeast;
     chunk = (chunk + 127) / 128 * 128;
     if (most > want) most = want; // over all windows
+    constexpr long kEnd = 0x7fffff80; // (2^31 - 1 tokens in one cut would be rounded past it)
+    if (chunk > kEnd) chunk = kEnd;
+    if (longest > kEnd && most < 2) most = 2;
     k.cuts.chunk = (int)chunk;
     k.cuts.splits = (int)((seen + chunk - 1) / chunk);
     const size_t all = (size_t)T * heads, each = (size_t)c.head_dim * 4 + 8;

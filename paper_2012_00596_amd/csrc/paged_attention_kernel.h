@@ -76,7 +76,7 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
         s = tile_of_run.s;
         at_first = tile_of_run.at0 + tile_of_run.row0 / group;
         at_last = tile_of_run.at0 + (tile_of_run.row0 + min(tile_of_run.rows, 16 * G) - 1) / group;
-        first = a.window > 0 ? max(0, at_first - a.window + 1) : 0;
+        first = a.window > 0 ? (int)max(0l, (long)at_first - a.window + 1) : 0;
         count = max(0, at_last + 1 - first);
     } else {
         h0 = id % head_tiles * 16;

@@ -2,7 +2,8 @@
 and single tokens one after another, as a server makes the calls; refusals.
 
 Tolerances: a score is off by D fp32 roundoffs of its terms' magnitudes, so a weight by twice that of the largest score; it is rounded once to the
-storage type (U; fp16 weights below 2^-29 of the largest by 2^-40 of it); sums and exponentials STEPS; the result is rounded once."""
+storage type (U; fp16 weights are held from 2^11 down, or up to 2^15 until the maximum in use follows, and numbers below 2^-14
+are off by up to 2^-25: by 2^-36 of the largest weight, which is 2^11 or more); sums and exponentials STEPS; the result is rounded once."""
 import numpy as np
 import pytest
 
@@ -69,7 +70,7 @@ def _check(torch, ref, y, lse, dt, most, untouched=None):
     assert bool((got[none] == 0).all()) and bool((le[none] == -float("inf")).all()), "a row without tokens is not zero"
     odd = ~torch.isfinite(ry)
     assert bool((~torch.isfinite(got[odd])).all()) and bool((got[odd] == ry[odd])[~torch.isnan(ry[odd]) & ~torch.isnan(got[odd])].all())
-    steps = 2 * ds[..., None] + STEPS + U[dt] + (most * 2.0 ** -40 if dt == npas.F16 else 0.0)
+    steps = 2 * ds[..., None] + STEPS + U[dt] + (most * 2.0 ** -36 if dt == npas.F16 else 0.0)
     bad = ~((got - ry).abs() <= U[dt] * ry.abs() + TINY[dt] + steps * w) & ~odd
     assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()} off, worst {float((got - ry).abs()[~odd].nan_to_num(9e9).max())}, first {torch.nonzero(bad)[0].tolist()}"
     fine = ~none
@@ -265,6 +266,142 @@ def test_chunk_beyond_32_bit_offsets(torch):
     ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
     npas.chunk_attention(cache, q.cuda(), y, 93, H, starts.cuda(), n.cuda(), 150, D ** -0.5, lse=lse, workspace=ws, workspace_bytes=need)
     _check(torch, _chunk64(torch, q, *small, table - last, starts, n, D ** -0.5, 0, 150), y, lse, dt, 150)
+
+
+@gpu
+@pytest.mark.parametrize("H,KV,D,runs", [(4, 2, 64, [(3, 40), (2, 300)]), (8, 2, 128, [(100, 150), (64, 64)]), (2, 1, 256, [(70, 70), (4, 20)])])
+def test_nan_blocks_of_8_bit_values_reach_the_rows_that_see_them(torch, H, KV, D, runs):
+    dt = npas.BF16
+    cache, _, table, starts, n, top = _make(torch, (H, KV, D, 16, runs, 0, dt, True, False))
+    for s, (new, length) in enumerate(runs):
+        for back, block in ((new - 1, 0), (1, D // 32 - 1)):
+            j = length - 1 - back
+            at = (int(table[s, j // 16]), KV - 1, j % 16)
+            cache.v[at][32 * block:32 * block + 32] = 0x7f
+            cache.v_scale[at][block] = 255
+    k, v = c8.dequantise(cache.k.cpu(), cache.k_scale.cpu()), c8.dequantise(cache.v.cpu(), cache.v_scale.cpu())
+    T = int(starts[-1])
+    q = _rand(torch, 5, (T, H, D), dt)
+    need = npas.chunk_attention_workspace_bytes(cache, T, H, top)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    y, lse = torch.empty_like(q, device="cuda"), torch.empty((T, H), device="cuda")
+    npas.chunk_attention(cache, q.cuda(), y, T, H, starts.cuda(), n.cuda(), top, D ** -0.5, lse=lse, workspace=ws, workspace_bytes=need)
+    ref = _chunk64(torch, q, k, v, table, starts, n, D ** -0.5, 0, top)
+    assert bool(torch.isnan(ref[0]).any()) and bool(torch.isfinite(ref[0]).any())
+    _check(torch, ref, y, lse, dt, top)
+
+
+@gpu
+@pytest.mark.parametrize("e8", [False, True])
+@pytest.mark.parametrize("runs,D", [([(3, 200), (2, 90)], 64), ([(90, 200), (64, 64)], 128), ([(90, 200), (64, 64)], 80), ([(40, 90)], 256)])
+def test_missing_pages_bring_nothing_in(torch, runs, D, e8):
+    """The first page of the cache, which stands in for what is missing, holds NaN and infinities and is no sequence's."""
+    H, KV, page, dt = 4, 2, 16, npas.BF16
+    cache, (k, v), table, starts, n, top = _make(torch, (H, KV, D, page, runs, 0, dt, e8, False))
+    table = table.clone()
+    table[table == 0] = int(max(set(range(k.shape[0])) - set(table.flatten().tolist())))      # (page 0 out of use; its place in another, NaN)
+    table[:, 1] = -1
+    table[0, 3 % table.shape[1]] = k.shape[0]
+    if e8:
+        cache.k[0], cache.v[0], cache.k_scale[0], cache.v_scale[0] = 0x7f, 0x7f, 255, 255
+        cache = npas.KvCache8(cache.k, cache.v, cache.k_scale, cache.v_scale, table.cuda(), dt)
+    else:
+        cache.k[0], cache.v[0] = float("nan"), float("inf")
+        cache = npas.KvCache(cache.k, cache.v, table.cuda(), dt)
+    lost = set((table[s, j]).item() for s in range(len(runs)) for j in range(table.shape[1]))
+    for p in lost & set(range(k.shape[0])):                  # pages that nobody wrote in this table's use of them become zeros
+        for parts in ((cache.k, cache.v),):
+            for t in parts:
+                x = t[p].float() if not e8 else None
+                if e8:
+                    t[p][t[p] == 0x7f] = 0
+                else:
+                    t[p] = torch.nan_to_num(x, 0.0).to(t.dtype)
+        if e8:
+            for t in (cache.k_scale, cache.v_scale):
+                t[p][t[p] == 255] = 127
+    k, v = (c8.dequantise(cache.k.cpu(), cache.k_scale.cpu()), c8.dequantise(cache.v.cpu(), cache.v_scale.cpu())) if e8 else (cache.k.cpu(), cache.v.cpu())
+    T = int(starts[-1])
+    q = _rand(torch, 5, (T, H, D), dt)
+    need = npas.chunk_attention_workspace_bytes(cache, T, H, top)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    y, lse = torch.empty_like(q, device="cuda"), torch.empty((T, H), device="cuda")
+    npas.chunk_attention(cache, q.cuda(), y, T, H, starts.cuda(), n.cuda(), top, D ** -0.5, lse=lse, workspace=ws, workspace_bytes=need)
+    _check(torch, _chunk64(torch, q, k, v, table, starts, n, D ** -0.5, 0, top), y, lse, dt, top)
+    assert bool(torch.isfinite(y).all())
+
+
+@gpu
+@pytest.mark.parametrize("runs", [[(5, 3), (40, 20), (1, 0)], [(3, 400), (200, 260)]])
+def test_the_largest_windows_and_runs_longer_than_their_sequence(torch, runs):
+    H, KV, D, dt = 4, 2, 64, npas.F16
+    cache, (k, v), table, starts, n, top = _make(torch, (H, KV, D, 16, runs, 0, dt, False, False))
+    T = int(starts[-1])
+    q = _rand(torch, 5, (T, H, D), dt)
+    need = npas.chunk_attention_workspace_bytes(cache, T, H, top)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    for window in (1, 2 ** 31 - 1):
+        y, lse = torch.empty_like(q, device="cuda"), torch.empty((T, H), device="cuda")
+        npas.chunk_attention(cache, q.cuda(), y, T, H, starts.cuda(), n.cuda(), top, 0.1, window=window, lse=lse, workspace=ws, workspace_bytes=need)
+        _check(torch, _chunk64(torch, q, k, v, table, starts, n, 0.1, window, top), y, lse, dt, top)
+
+
+@gpu
+@pytest.mark.parametrize("T", [2, 40])
+@pytest.mark.parametrize("window", [0, 1000])
+def test_runs_at_the_longest_length(torch, T, window):
+    """2^31 - 1 tokens, by both forms: one page stands in every place of the table.  A lane adds up to 2^23 weights in turn, each addition 2^-24 of what
+    is there: half of the sum at most."""
+    D, page, places, dt = 16, 2 ** 15, 2 ** 16, npas.F16
+    k, v = _rand(torch, 90, (1, 1, page, D), dt), (_rand(torch, 91, (1, 1, page, D), dt) + 1).half()
+    q, n = _rand(torch, 92, (T, 1, D), dt), 2 ** 31 - 1
+    cache = npas.KvCache(k.cuda(), v.cuda(), torch.zeros((1, places), dtype=torch.int32, device="cuda"), dt)
+    need = npas.chunk_attention_workspace_bytes(cache, T, 1, n)
+    y, lse = torch.empty((T, 1, D), dtype=torch.float16, device="cuda"), torch.empty((T, 1), device="cuda")
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    npas.chunk_attention(cache, q.cuda(), y, T, 1, torch.tensor([0, T], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda(), n, 0.25,
+                         window=window, lse=lse, workspace=ws, workspace_bytes=need)
+    x = torch.exp(0.25 * q[:, 0].double() @ k[0, 0].double().t())             # [T][page]
+    for t in range(T):
+        at = n - T + t
+        if window:
+            times = torch.bincount(torch.arange(at - window + 1, at + 1) % page, minlength=page).double()
+        else:
+            times = torch.full((page,), float((at + 1) // page), dtype=torch.float64)
+            times[:(at + 1) % page] += 1
+        p = times * x[t]
+        want, mag = p @ v[0, 0].double() / p.sum(), p @ v[0, 0].double().abs() / p.sum()
+        assert bool(((y[t, 0].double().cpu() - want).abs() <= (2 ** -10 if window else 0.5) * mag).all()), (t, y[t, 0], want)
+        assert abs(float(lse[t]) - float(torch.log(p.sum()))) <= (1e-4 if window else 0.5)
+
+
+@gpu
+def test_two_streams_at_once(torch):
+    """Prompts and drafts on two streams, a workspace each, many times over: what one stream alone gives."""
+    cases = [(8, 2, 128, 16, [(200, 600), (30, 30)], 0, npas.BF16, False, False), (8, 2, 128, 16, [(3, 3000), (2, 900)], 0, npas.BF16, True, False)]
+    made = []
+    for case in cases:
+        cache, _, _, starts, n, top = _make(torch, case)
+        T, H, D = int(starts[-1]), case[0], case[2]
+        need = npas.chunk_attention_workspace_bytes(cache, T, H, top)
+        made.append((cache, _rand(torch, 5, (T, H, D), case[6]).cuda(), torch.empty((T, H, D), dtype=torch.bfloat16, device="cuda"), T, H, starts.cuda(), n.cuda(),
+                     top, torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"), need, torch.cuda.Stream()))
+
+    def call(cache, q, y, T, H, starts, n, top, ws, need, stream):
+        npas.chunk_attention(cache, q, y, T, H, starts, n, top, 0.09, workspace=ws, workspace_bytes=need, stream=stream.cuda_stream)
+    torch.cuda.synchronize()
+    alone = []
+    for m in made:
+        call(*m)
+        torch.cuda.synchronize()
+        alone.append(m[2].clone())
+        m[2].zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for m in made:
+            call(*m)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, m[2]) for a, m in zip(alone, made))
 
 
 # ---- together ----------------------------------------------------------------------
