@@ -5,6 +5,7 @@
 #include "cache8.h"
 #include "decoder_internal.h"
 #include "device_util.h"
+#include "join_cuts.h"
 #include "run_tiles.h"
 
 namespace npas {
@@ -54,9 +55,17 @@ __device__ __forceinline__ float over_halves(float x)
 // BN = 32 NSUB: scores S = K Q^T (row operand: keys from LDS as they lie), running maximum and sum a column, O^T = V^T P^T, where the weights
 // are the column operand as the first product leaves them, if a step's tokens are counted so that a lane's half h has tokens 4 h .. 4 h + 3 of
 // each eight; the values come out of LDS turned round.
-// Keys and values of a step come through registers into one of two places in LDS (16-byte pieces in an order that spreads rows over the banks; 8-bit
-// floats become 16-bit numbers on the way) while the other is multiplied; the cache rows of the tokens are looked up two steps ahead.
-// The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled.
+// Keys and values of a step come into one of two places in LDS while the other is multiplied, 16-byte pieces in an order that spreads rows over the banks (2048
+// tokens on 63000 2.41 ms without, 2.34 with): 16-bit numbers straight from memory, 8-bit floats through registers, where they become 16-bit numbers.  Loads are
+// issued a part at a time between the products (8191 prompt tokens all at once 182 us, so 172).  The cache rows of 4 or 8 steps' tokens are looked up at
+// once, a token a thread, in the step before they are needed.
+// The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled; a weight is rounded once to the 16-bit
+// type that its product takes, which the result, rounded to the same type, is not much worse for (half a step of each weight).  Masks, absent tokens and
+// values that are not finite are branches that the steps which every row sees whole do not have (8191 prompt tokens 343 us with selects everywhere, 183).
+// Bound by the matrix cores and the vector instructions beside them: an exponential and a rounding a score.  One sequence's 2048 tokens on 63000, 32 query and 8 key heads
+// of 128 in 8 bits: 2.29 ms (938 TFLOP/s; a large library product 1250), at the 2.15 GHz that the card then runs at; 8191 tokens of five prompts in
+// 16 bits 162 us (675 TFLOP/s), where the diagonal's half-empty steps and the last, partial round of workgroups count.
+// BN is 64 tokens for heads of up to 128, two workgroups a compute unit; 32 for longer ones, whose tiles fill LDS and registers.
 template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a)
 {
     constexpr int DP = 32 * ND, BM = 32 * WAVES, BN = 32 * NSUB, THREADS = 64 * WAVES, PIECES = DP / 8, STRIDE = DP * 2;
@@ -405,7 +414,8 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
     if (h == 0 && a.lse) a.lse[out_row] = l != 0.f ? (m - TOP + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// One wave a row: the cuts' sums, rescaled to the largest maximum and added in their order.
+// One wave a row, for up to 16 cuts: their sums, rescaled to the largest maximum and added in their order (64 tokens of 32 heads in 4 to 11 cuts: the whole call
+// 18 to 22 us, with a workgroup a row as more cuts have it 20 to 25; in 118 cuts, read in this way, 61, in that 28).  The bytes of the sums bound it.
 template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_kernel(ChunkArgs a)
 {
     const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -478,6 +488,7 @@ int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream)
 int launch_chunk_join(int dt, const ChunkArgs &a, void *stream)
 {
     hipStream_t st = (hipStream_t)stream;
+    if (a.splits > 16) return launch_join("chunk attention", dt, a, (uint64_t)a.T * a.heads, st);
     const uint64_t workgroups = ((uint64_t)a.T * a.heads + 3) / 4;
     if (int rc = check_grid("chunk attention", workgroups, 256)) return rc;
     const dim3 grid((unsigned)workgroups), block(256);

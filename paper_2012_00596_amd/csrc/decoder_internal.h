@@ -56,6 +56,7 @@ struct AttentionArgs {
     int T, places;
 };
 constexpr int kMaxSplits = 512;
+inline unsigned join_threads(int splits) { return splits <= 16 ? 64 : kMaxSplits; } // of a workgroup that joins a row's cuts
 
 struct WriteArgs {
     CacheArgs c;

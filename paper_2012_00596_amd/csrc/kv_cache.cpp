@@ -1,5 +1,7 @@
 // C-ABI calls on the paged cache beside those of a decode step: argument checks, plans and launches of the write with norms, the read of 8-bit
 // floats and the attention of runs of tokens.
+#include <cmath>
+
 #include "decoder_internal.h"
 
 using namespace npas;
@@ -7,8 +9,15 @@ using namespace npas;
 namespace {
 
 // How a launch takes the rows and cuts the tokens.  Rows: (token, query head) of a key head.
-//   - Runs of up to 32 rows on average: the kernel of single tokens with one or two groups of 16 rows, cut as that is.
-//   - Longer ones: tiles of kChunkRows; where they do not fill the card, a tile's tokens are cut over workgroups, at least kLeast each.
+//   - Runs of up to 32 rows on average (of heads longer than 128: 16, and up to 32 in tiles of 16, which is all that the registers hold): the kernel of single
+//     tokens with one or two groups of 16 rows, cut as that is.  32 sequences of 5 tokens, 4 query heads a key head, in 8 bits 62 us, in tiles of kChunkRows
+//     86; 5 tokens of one sequence 9.3 and 11.2; in 16 bits, which tiles take straight from memory, both are near alike (16 sequences of 8 tokens on 4000
+//     54 and 54, 64 of 3 on 2000 59 and 53).
+//   - Longer ones: tiles of kChunkRows.  Where they do not fill the card, a tile's tokens are cut for kWorkgroups in all, two a compute unit (256 tokens on 30000,
+//     4 key heads and 8 query heads each: 149 us; for 1024 163, for 256 168).
+//   - A cut more costs each row head_dim floats written and read, a token more in a cut its walk: their sum is least at a length that goes with the root of
+//     rows and tokens (64 tokens of 32 heads on 8192: 32 cuts of 256 35 us, 16 of 512 30, 8 of 1024 36; on 30000, 8 heads, 256 each 28 to 31, 512 28), and
+//     kLeast at the least (on 1000: 256 each 18 us, 512 22).
 struct ChunkPlan {
     int groups; // of 16 rows; 0: tiles of kChunkRows
     long places;
@@ -32,6 +41,8 @@ ChunkPlan plan_chunks(const CacheArgs &c, int T, int heads, int max_length, int 
     long want = (kWorkgroups + tiles * c.kv_heads - 1) / (tiles * c.kv_heads); // cuts
     if (want > kMost) want = kMost;
     long chunk = (seen + want - 1) / want, most = (longest + kLeast - 1) / kLeast;
+    const long paid = (long)std::sqrt((double)seen * T * heads * 0.01);
+    if (chunk < paid) chunk = paid;
     if (chunk < kLeast) chunk = kLeast;
     chunk = (chunk + 127) / 128 * 128;
     if (most > want) most = want; // over all windows
@@ -153,6 +164,8 @@ int npas_chunk_attention(const npas_kv_cache *cache, const npas_kv_scales *scale
     a.chunk = cuts.chunk; a.splits = cuts.splits; a.places = (int)plan.places;
     a.part = (float *)workspace_dev;
     a.part_stat = (float2 *)((uint8_t *)workspace_dev + cuts.stat_at);
+    if (a.splits > 1)
+        if (int rc = check_grid("chunk attention", (uint64_t)T * heads, join_threads(a.splits))) return rc;
     if (plan.groups) {
         AttentionArgs r{};
         r.c = a.c; r.q = a.q; r.y = a.y; r.lse = a.lse; r.q_stride = a.q_stride; r.start = a.start; r.length = a.length;

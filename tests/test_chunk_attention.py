@@ -174,6 +174,19 @@ def test_rows_of_no_sequence_stay(torch, e8):
 
 
 @gpu
+@pytest.mark.parametrize("case", [
+    (8, 1, 128, 16, [(6, 9000), (0, 0), (7, 130), (5, 1)], 0, npas.BF16, False, False),
+    (8, 1, 64, 16, [(9, 8000), (1, 30)], 5000, npas.F16, True, True),
+    (2, 1, 256, 64, [(40, 7000)], 0, npas.BF16, True, False),
+    (4, 1, 80, 16, [(4, 9000), (2, 50), (0, 7)], 0, npas.F16, False, True),
+    (4, 1, 128, 16, [(3, 9000), (2, 50)], 6000, npas.BF16, True, False)], ids=str)
+def test_many_cuts(torch, case):
+    """More than 16 cuts, most of them empty for the short sequences; rows of no sequence on both sides."""
+    print(f"cuts {case}", flush=True)
+    _run(torch, case, before=3, after=5)
+
+
+@gpu
 @pytest.mark.parametrize("scale", [0.0, -0.3, 40.0])
 def test_scales_of_every_sign_and_large_scores(torch, scale):
     _run(torch, (4, 2, 64, 16, [(40, 90), (2, 300)], 0, npas.BF16, False, False), scale=scale)
