@@ -438,14 +438,14 @@ template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_ke
         for (int k = 0; k < SIDE; ++k) x[k] = stat[min(i0 + k, a.splits - 1)];
 #pragma unroll
         for (int k = 0; k < SIDE; ++k) {
-            if (i0 + k >= a.splits) x[k].x = -INFINITY;
+            if (i0 + k >= a.splits) x[k] = make_float2(-INFINITY, 0.f);
             v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (x[k].x != -INFINITY && lane * 4 < D) v[k] = *reinterpret_cast<const float4 *>(a.part + (row * a.splits + i0 + k) * D + lane * 4);
         }
 #pragma unroll
         for (int k = 0; k < SIDE; ++k) {
             const float c = x[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[k].x - m);
-            l += x[k].x == -INFINITY ? 0.f : c * x[k].y;
+            l += c * x[k].y; // (zero, or NaN from a cut whose scores all are)
             y.x += c * v[k].x, y.y += c * v[k].y, y.z += c * v[k].z, y.w += c * v[k].w;
         }
     }

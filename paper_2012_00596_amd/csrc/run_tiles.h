@@ -39,7 +39,7 @@ template <int BM, typename Args> __device__ __forceinline__ bool find_run_tile(c
     if (n > room) n = (int)room;
     t.length = n;
     t.at0 = n - run;
-    return t.rows > 0;
+    return t.rows > 0 && t.row0 >= 0; // (starts that fall, which no call has, lead to places before a run's first)
 }
 
 } // namespace npas

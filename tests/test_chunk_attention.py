@@ -227,6 +227,40 @@ def test_infinities_and_nan_reach_the_rows_that_see_them(torch, H, KV, D, runs, 
 
 
 @gpu
+@pytest.mark.parametrize("e8", [False, True])
+@pytest.mark.parametrize("T,n", [(40, 200), (40, 1000), (40, 6000), (3, 200), (3, 1200), (3, 3000)])
+def test_nan_scores_make_their_rows_nan(torch, T, n, e8):
+    """One cut, some and many: a NaN in a query makes that head's row NaN alone, one in a key every row that sees it, also where a cut has no other score."""
+    H, KV, D, page = 8, 1, 64, 16
+    case = (H, KV, D, page, [(T, n)], 0, npas.BF16, e8, False)
+    cache, _, _, starts, length, top = _make(torch, case)
+    need = npas.chunk_attention_workspace_bytes(cache, T, H, top)
+    ws = torch.full((max(need, 16) // 4 + 1,), float("nan"), device="cuda")
+    q = _rand(torch, 79, (T, H, D), npas.BF16)
+
+    def run(q):
+        y, lse = torch.full((T, H, D), 7.0, dtype=q.dtype, device="cuda"), torch.full((T, H), 7.0, device="cuda")
+        npas.chunk_attention(cache, q.cuda(), y, T, H, starts.cuda(), length.cuda(), top, 0.125, lse=lse, workspace=ws, workspace_bytes=need)
+        return y.cpu(), lse.cpu()
+
+    clean = run(q)
+    bad = q.clone()
+    bad[1, 5, 7] = float("nan")
+    y, lse = run(bad)
+    assert bool(torch.isnan(y[1, 5]).all()) and bool(torch.isnan(lse[1, 5]))
+    y[1, 5], lse[1, 5] = clean[0][1, 5], clean[1][1, 5]
+    assert torch.equal(y, clean[0]) and torch.equal(lse, clean[1])
+    # every key up to the middle (whole cuts of them): all later tokens see one
+    pages = cache.page_table[0, :n // 2 // page].long()
+    if e8:
+        cache.k[pages], cache.k_scale[pages] = 0x7f, 255
+    else:
+        cache.k[pages] = float("nan")
+    y, lse = run(q)
+    assert bool(torch.isnan(y).all()) and bool(torch.isnan(lse).all())
+
+
+@gpu
 def test_infinite_scores(torch):
     """As for one token: a score of plus infinity makes the row NaN and its lse infinite, minus infinity has no weight, all of them give zero."""
     H = KV = 1
@@ -260,6 +294,22 @@ def test_lengths_are_cut(torch):
         ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
         npas.chunk_attention(cache, q.cuda(), y, 50, H, starts.cuda(), n.cuda(), most, 1.0, lse=lse, workspace=ws, workspace_bytes=need)
         _check(torch, _chunk64(torch, q, k, v, table, starts, n, 1.0, 0, most), y, lse, dt, most, 7.0)
+
+
+@gpu
+@pytest.mark.parametrize("H", [2, 16])
+def test_starts_that_fall_write_no_other_rows(torch, H):
+    """No call has such starts; what they give is undefined, but nothing outside y's rows is written."""
+    KV, D, page, dt, T = 1, 64, 16, npas.BF16, 40
+    k, v = (_rand(torch, 76 + i, (20, KV, page, D), dt) for i in range(2))
+    cache = npas.KvCache(k.cuda(), v.cuda(), torch.arange(20, dtype=torch.int32).reshape(4, 5).cuda(), dt)
+    q = _rand(torch, 78, (T, H, D), dt).cuda()
+    for starts in ([30, 0, 10, 10, 5], [40, 40, 0, 40, 0], [7, -9, 90, 3, 40]):
+        y, lse = torch.full((T + 200, H, D), 7.0, dtype=q.dtype, device="cuda"), torch.full((T + 200, H), 7.0, device="cuda")
+        npas.chunk_attention(cache, q, y[100:100 + T], T, H, torch.tensor(starts, dtype=torch.int32).cuda(), torch.full((4,), 60, dtype=torch.int32).cuda(),
+                             80, 0.1, lse=lse[100:100 + T])
+        for x in (y, lse):
+            assert bool((x[:100] == 7.0).all()) and bool((x[100 + T:] == 7.0).all())
 
 
 @gpu
