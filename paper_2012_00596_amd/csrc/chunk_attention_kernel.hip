@@ -36,13 +36,9 @@ template <int DT> __device__ __forceinline__ bool not_finite2(uint32_t w)
     return (w & e) == e || (w >> 16 & e) == e;
 }
 
-// The largest of three, one instruction; a NaN is left out, as fmaxf leaves it.
-__device__ __forceinline__ float max3(float x, float y, float z)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
-    return r;
-}
+// The largest of three; a NaN is left out.  (Becomes one instruction.  Not an asm statement: the compiler would not keep its distance from the matrix
+// instruction whose results it reads.)
+__device__ __forceinline__ float max3(float x, float y, float z) { return fmaxf(fmaxf(x, y), z); }
 
 // The larger of a lane's and its partner's in the other half of the wave.
 __device__ __forceinline__ float over_halves(float x)
