@@ -29,6 +29,26 @@ __device__ __forceinline__ uint2 read_columns(const uint8_t *p)
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
 }
 
+// The first 16-bit part of two weights, below them or equal, and what is left of them in their place: never zero where the weight is not (of fp16 weights, down
+// to 2^-14), as an infinite value times a part of zero would be NaN.
+template <int DT> __device__ __forceinline__ uint32_t part_below2(float &a, float &b)
+{
+    if constexpr (DT == NPAS_BF16) {
+        // (what is taken away is smaller than the part by 2^-24 of it: the weight counts as larger by that, in the one instruction that the difference takes)
+        const uint32_t u = __float_as_uint(a), w = __float_as_uint(b);
+        constexpr float c = 1.f - 0x1p-24f;
+        a = fmaf(__uint_as_float(u & 0xffff0000u), -c, a);
+        b = fmaf(__uint_as_float(w & 0xffff0000u), -c, b);
+        return __builtin_amdgcn_perm(w, u, 0x07060302u);
+    } else {
+        const uint32_t u = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u), w = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);
+        const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(u), __uint_as_float(w)));
+        a -= from_storage<DT>((uint16_t)x);
+        b -= from_storage<DT>((uint16_t)(x >> 16));
+        return x;
+    }
+}
+
 // Whether one of the two numbers is an infinity or a NaN.
 template <int DT> __device__ __forceinline__ bool not_finite2(uint32_t w)
 {
@@ -51,22 +71,25 @@ __device__ __forceinline__ float over_halves(float x)
 // BN = 32 NSUB: scores S = K Q^T (row operand: keys from LDS as they lie), running maximum and sum a column, O^T = V^T P^T, where the weights
 // are the column operand as the first product leaves them, if a step's tokens are counted so that a lane's half h has tokens 4 h .. 4 h + 3 of
 // each eight; the values come out of LDS turned round.
-// Keys and values of a step come into one of two places in LDS while the other is multiplied, 16-byte pieces in an order that spreads rows over the banks (2048
-// tokens on 63000 2.41 ms without, 2.34 with): 16-bit numbers straight from memory, 8-bit floats through registers, where they become 16-bit numbers.  Loads are
-// issued a part at a time between the products (8191 prompt tokens all at once 182 us, so 172).  The cache rows of 4 or 8 steps' tokens are looked up at
-// once, a token a thread, in the step before they are needed.
-// The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled; a weight is rounded once to the 16-bit
-// type that its product takes, which the result, rounded to the same type, is not much worse for (half a step of each weight).  Masks, absent tokens and
-// values that are not finite are branches that the steps which every row sees whole do not have (8191 prompt tokens 343 us with selects everywhere, 183).
-// Bound by the matrix cores and the vector instructions beside them: an exponential and a rounding a score.  One sequence's 2048 tokens on 63000, 32 query and 8 key heads
-// of 128 in 8 bits: 2.29 ms (938 TFLOP/s; a large library product 1250), at the 2.15 GHz that the card then runs at; 8191 tokens of five prompts in
-// 16 bits 162 us (675 TFLOP/s), where the diagonal's half-empty steps and the last, partial round of workgroups count.
+// Keys and values of a step come into one of two places in LDS while the other is multiplied, 16-byte pieces in an order that spreads rows over the banks:
+// 16-bit numbers straight from memory, 8-bit floats through registers, where they become 16-bit numbers.  Loads are issued a part at a time between the
+// products.  The cache rows of 4 or 8 steps' tokens are looked up at once, a token a thread, in the step before they are needed.
+// The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled.  A weight enters the second product as
+// 16-bit numbers whose sum it is, three in bf16 and two in fp16 (22 bits), so that results are those of fp32 weights; one rounded number took 162 us for
+// the prompts below, 76 and 2280 for the other cases of its kind.  Masks, absent tokens and values that are not finite are branches that the steps which every
+// row sees whole do not have.
+// (Measured with one number a weight: the banks, 2048 tokens on 63000 2.41 -> 2.34 ms; loads by parts, 8191 prompt tokens 182 -> 172 us; branches for selects,
+// 343 -> 183.)
+// Bound by the matrix cores: one sequence's 2048 tokens on 63000, 32 query and 8 key heads of 128 in 8 bits: 3.71 ms, its instructions at 1160 TFLOP/s (a large
+// library product 1250); 8191 tokens of five prompts in 16 bits 236 us (930 TFLOP/s), where the diagonal's half-empty steps and the last, partial round of
+// workgroups count.
 // BN is 64 tokens for heads of up to 128, two workgroups a compute unit; 32 for longer ones, whose tiles fill LDS and registers.
 template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a)
 {
     constexpr int DP = 32 * ND, BM = 32 * WAVES, BN = 32 * NSUB, THREADS = 64 * WAVES, PIECES = DP / 8, STRIDE = DP * 2;
     constexpr int UNITS = E8 ? BN * PIECES / 2 : BN * PIECES, PER = (UNITS + THREADS - 1) / THREADS, IN_ROW = E8 ? PIECES / 2 : PIECES;
     constexpr float GROW = DT == NPAS_BF16 ? 8.f : 4.f, TOP = DT == NPAS_BF16 ? 0.f : 11.f; // a weight is at most 2^(TOP + GROW)
+    constexpr int PARTS = DT == NPAS_BF16 ? 3 : 2; // 16-bit numbers that a weight is taken apart into
     __shared__ __align__(16) uint8_t kbuf[2][BN * STRIDE], vbuf[2][BN * STRIDE];
     constexpr int AHEAD = THREADS / BN; // steps whose tokens are looked up at once, one a thread
     __shared__ uint32_t ring[2 * THREADS], gone[2 * THREADS / 32], holes[2 * AHEAD]; // cache rows of tokens; a bit a token that is not there; whether a step has such
@@ -293,47 +316,62 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
             for (int dt = 0; dt < ND; ++dt) o[dt] *= c;
         }
         const float base = m == -INFINITY ? 0.f : m - TOP;
-        // 16 tokens at a time; between the products of one such part the next one's values are read and its weights formed
-        constexpr int PARTS = 2 * NSUB;
-        uint4 pf[2], vf[2][ND];
-        float p[8];
-        auto weigh = [&](int part, int k) __attribute__((always_inline)) {
-            p[k] = __builtin_amdgcn_exp2f(fmaf(sc[part >> 1][8 * (part & 1) + k], mul, -base));
-            l += p[k];
+        // 16 tokens at a time; between the products of one such part the next one's weights are formed, and its values read as soon as these have been multiplied
+        constexpr int STRETCHES = 2 * NSUB;
+        uint32_t pf[2][PARTS][4];
+        uint4 vf[ND];
+        // two weights of a stretch: formed, then taken apart, a part a step
+        float rest[8];
+        auto weigh = [&](int x, int pair) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 2 * pair; k < 2 * pair + 2; ++k) {
+                rest[k] = __builtin_amdgcn_exp2f(fmaf(sc[x >> 1][8 * (x & 1) + k], mul, -base));
+                l += rest[k];
+            }
         };
-        auto pack = [&](int part) __attribute__((always_inline)) {
-            pf[part & 1] = make_uint4(pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7]));
+        auto take = [&](int x, int pair, int n) __attribute__((always_inline)) {
+            float &a = rest[2 * pair], &b = rest[2 * pair + 1];
+            pf[x & 1][n][pair] = n < PARTS - 1 ? part_below2<DT>(a, b) : pack2<DT>(a, b);
         };
-        auto read = [&](int part, int dt) __attribute__((always_inline)) {
+        auto read = [&](int x, int dt) __attribute__((always_inline)) {
             uint2 v[2];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const int key = 16 * part + 8 * y + 4 * h + (lane >> 2 & 3), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+                const int key = 16 * x + 8 * y + 4 * h + (lane >> 2 & 3), piece = 4 * dt + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
                 v[y] = read_columns(vb + key * STRIDE + value_piece(key, piece) + (lane & 1) * 8);
             }
-            vf[part & 1][dt] = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+            vf[dt] = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
         };
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) read(0, dt);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) weigh(0, k);
-        pack(0);
+        for (int pair = 0; pair < 4; ++pair) {
+            weigh(0, pair);
+#pragma unroll
+            for (int n = 0; n < PARTS; ++n) take(0, pair, n);
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
+        for (int x = 0; x < STRETCHES; ++x) {
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
-                o[dt] = mfma32<DT>(vf[part & 1][dt], pf[part & 1], o[dt]);
-                if (part + 1 < PARTS) {
-                    read(part + 1, dt);
 #pragma unroll
-                    for (int k = 8 * dt / ND; k < 8 * (dt + 1) / ND; ++k) weigh(part + 1, k);
-                    if (dt + 1 == ND) pack(part + 1);
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int n = 0; n < PARTS; ++n) {
+                    const uint32_t (&w)[4] = pf[x & 1][n];
+                    o[dt] = mfma32<DT>(vf[dt], make_uint4(w[0], w[1], w[2], w[3]), o[dt]);
+                    if (x + 1 < STRETCHES) {
+#pragma unroll
+                        for (int pair = 4 * dt / ND; pair < 4 * (dt + 1) / ND; ++pair) {
+                            if (n == 0) weigh(x + 1, pair);
+                            take(x + 1, pair, n);
+                        }
+                        if (n + 1 == PARTS) read(x + 1, dt);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < PER; ++u)
-                    if (more && u * PARTS * ND / PER / 2 == part * ND + dt) {
+                    if (more && u * STRETCHES * ND / PER / 2 == x * ND + dt) {
                         load(1 - parity, u, 1);
                         __builtin_amdgcn_sched_barrier(0);
                     }

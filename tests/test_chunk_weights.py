@@ -1,0 +1,105 @@
+"""Attention of runs where a weight's last bits, an infinite value or a single token decide: as test_attention_weights has it for one token.  By the mean
+run (of heads that share none) 2 rows go through the kernel of short runs with one group of rows, 20 with two, 40 and 150 through tiles.
+
+Bounds: those of test_attention_weights.  Parts of a bf16 weight are taken so that it counts as larger by up to u (2^-24) of itself: 10.4 u + u, still within 12.
+A fp16 weight is two parts, the first below it by up to 2^-10, the second off by 2^-12 of that: 4 u more."""
+import numpy as np
+import pytest
+
+import paper_2012_00596_amd as npas
+from tests import test_chunk_attention as runs
+from tests.test_attention_weights import TINY, U, _cancelling, _counts, _counts_hold, _outside, _round, _td, torch, u  # noqa: F401
+
+from . import cache8_reference as c8
+
+gpu = pytest.mark.gpu
+MORE = {npas.BF16: 0, npas.F16: 4}
+
+
+def _runs(torch, dt, q, k, v, page, lengths, scale, window=0, e8=False):
+    """q [S][T][H][D]: the last T tokens of each sequence; k, v [S][tokens][KV][D] laid into pages in random order -> y, lse [S][T][..] on the CPU."""
+    S, T, H, D = q.shape
+    tokens, KV = k.shape[1:3]
+    columns = -(-tokens // page)
+    order = torch.from_numpy(np.random.default_rng(tokens).permutation(S * columns))
+    pages = []
+    for x in (k, v):
+        full = torch.zeros((S, columns * page, KV, D), dtype=torch.float64)
+        full[:, :tokens] = x
+        full = full.reshape(S * columns, page, KV, D).transpose(1, 2)
+        out = torch.empty_like(full)
+        out[order] = full
+        pages.append(out.contiguous())
+    table = order.int().reshape(S, columns).cuda()
+    if e8:
+        (kc, ks), (vc, vs) = (c8.quantise(x, dt) for x in pages)
+        cache = npas.KvCache8(kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda(), table, dt)
+    else:
+        cache = npas.KvCache(*(x.to(_td(torch, dt)).cuda() for x in pages), table, dt)
+    starts, n = torch.arange(S + 1, dtype=torch.int32, device="cuda") * T, torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    need = npas.chunk_attention_workspace_bytes(cache, S * T, H, max(lengths))
+    ws = torch.full((max(need, 16) // 4 + 1,), float("nan"), device="cuda")
+    y = torch.full((S * T, H, D), float("nan"), dtype=_td(torch, dt), device="cuda")
+    lse = torch.full((S * T, H), float("nan"), device="cuda")
+    npas.chunk_attention(cache, q.to(_td(torch, dt)).reshape(S * T, H, D).cuda(), y, S * T, H, starts, n, max(lengths), scale, window=window, lse=lse,
+                         workspace=ws, workspace_bytes=need)
+    return y.double().cpu().reshape(S, T, H, D), lse.double().cpu().reshape(S, T, H)
+
+
+def _weights(torch, dt, T, D, where, steps):
+    S, H = 4, 8
+    x, v3, ref, w = _cancelling(torch, dt, S, H, D, 1)
+    n = where[-1] + 1 + T
+    k, v = torch.zeros((S, n, H, D), dtype=torch.float64), torch.zeros((S, n, H, D), dtype=torch.float64)
+    k[..., 0] = -200.0                                   # the other tokens: exp(-200) is zero in fp32
+    for i, j in enumerate(where):
+        k[:, j, :, 0], v[:, j] = x[:, i], v3[:, i]
+    q = torch.zeros((S, T, H, D), dtype=torch.float64)
+    q[..., 0] = 1
+    y, _ = _runs(torch, dt, q, k, v, 16, [n] * S, 1.0)
+    bad = _outside(y, ref[:, None], w[:, None], dt, steps + MORE[dt])
+    assert int(bad.sum()) == 0, f"{int(bad.sum())} of {bad.numel()} off, worst {float(((y - ref[:, None]).abs() / w[:, None]).max() / u)} steps"
+
+
+WHERE = [(64, (0, 1, 2), 12), (96, (0, 1, 2), 12), (128, (0, 1, 2), 12), (256, (0, 1, 2), 12), (80, (5, 40, 90), 12), (64, (3, 2500, 5990), 24),
+         (128, (100, 1000, 4999), 24), (256, (100, 1000, 4999), 24)]
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("D,where,steps", WHERE)
+@pytest.mark.parametrize("T", [40, 150])
+def test_weights_keep_the_bits_of_fp32_in_tiles(torch, dt, T, D, where, steps):
+    _weights(torch, dt, T, D, where, steps)
+
+
+def _strict(torch, ref, y, lse, dt, most, untouched=None):
+    """_check without an allowance for a weight's rounding to the storage type: 320 u for sums as in test_attention_weights (a lane's sums in turn, of up to some
+    2500 weights here, are off by the root of their number), the fp16 parts' 4 u, and what is lost below 2^-36 of the largest weight."""
+    ry, rl, w, ds = ref
+    rows = ~torch.isnan(rl[:, 0])
+    got, le = y.double().cpu(), lse.double().cpu()
+    if untouched is not None:
+        assert bool((got[~rows] == untouched).all()) and bool((le[~rows] == untouched).all()), "rows of no sequence were written"
+    got, le, ry, rl, w, ds = (t[rows] for t in (got, le, ry, rl, w, ds))
+    none = rl == -float("inf")
+    assert bool((got[none] == 0).all()) and bool((le[none] == -float("inf")).all())
+    assert bool(torch.isfinite(ry).all())
+    steps = 2 * ds[..., None] + (320 + MORE[dt]) * u + (most * 2.0 ** -36 if dt == npas.F16 else 0.0)
+    bad = ~((got - ry).abs() <= U[dt] * ry.abs() + TINY[dt] + steps * w)
+    assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()} off, worst {float((got - ry).abs().max())}"
+    assert bool(((le - rl).abs()[~none] <= ds[~none] + 320 * u + 4 * u * rl[~none].abs()).all())
+
+
+def _is_short(case):
+    """Whether a case of runs.RUNS goes through the kernel of short runs."""
+    H, KV, D, _, new = case[:5]
+    mean = -(-sum(n for n, _ in new) * (H // KV) // len(new))
+    return mean <= (16 if D > 128 else 32)
+
+
+@gpu
+@pytest.mark.parametrize("case", [c for c in runs.RUNS if not _is_short(c)], ids=str)
+def test_runs_in_tiles_without_an_allowance_for_rounded_weights(torch, monkeypatch, case):
+    monkeypatch.setattr(runs, "_check", _strict)
+    runs._run(torch, case)
