@@ -355,8 +355,8 @@ int npas_paged_attention8(const npas_kv_cache *cache, const npas_kv_scales *scal
  *   y = sum_j p_j v_j,  p = softmax_j(scale * q . k_j),  max(0, p + 1 - window) <= j <= p, j in the cache;  window 0: no window.
  * Where no j is left (p < 0 among them), y is zero.  Rows of q before start_dev[0] or from start_dev[sequences] on: their y and lse stay as they were.
  * q: row t at q + t * q_stride, heads * head_dim long; y [T][heads][head_dim]; lse_dev (nullable) fp32 [T][heads], as npas_paged_attention's.
- * A fp16 weight keeps 22 bits, at least 2^-36 of the row's largest; a bf16 weight all of its 24, in calls whose runs are some 32 rows on average or shorter, a row a
- * query head of a key head, 17.  An infinite v_j counts as npas_paged_attention says.
+ * A bf16 weight keeps its 24 bits, a fp16 one 22, at least 2^-36 of the row's largest.  An infinite v_j makes its element of y infinite, or NaN beside one of the other
+ * sign or where p_j is below 2^-12 (fp16; bf16: 2^-70) of the row's largest.
  * Where there are few rows, long sequences are cut over workgroups whose partial results are joined through the workspace (16-byte aligned;
  * npas_chunk_attention_workspace_bytes, which may be 0, is enough for any window, any lengths up to max_length and any parting of T).  Calls whose
  * work may overlap in time, on two streams or in two graphs, need a workspace each. */

@@ -14,7 +14,7 @@ SOURCES = ["pack.cpp", "api.cpp", "kernels.hip", "spatial_direct_kernel.hip", "s
            "inverted_residual_kernel.hip", "pointwise_stream_kernel.hip", "bottleneck_tail_kernel.hip", "noalloc.hip",
            "decoder.cpp", "decoder_kernels.hip", "paged_attention_kernel.hip", "kv_cache.cpp", "kv_write_kernel.hip", "chunk_attention_kernel.hip", "short_runs_kernel.hip",
            "mxfp4.cpp", "mxfp4_kernels.hip"]
-HEADERS = ["npas_internal.h", "device_util.h", "decoder_internal.h", "mxfp4_internal.h", "row_vectors.h", "cache8.h", "run_tiles.h", "join_cuts.h", "paged_attention_kernel.h"]
+HEADERS = ["npas_internal.h", "device_util.h", "decoder_internal.h", "mxfp4_internal.h", "row_vectors.h", "cache8.h", "run_tiles.h", "join_cuts.h", "weight_parts.h", "paged_attention_kernel.h"]
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "npas.h")
 
 F32, BF16, F16 = 0, 1, 2

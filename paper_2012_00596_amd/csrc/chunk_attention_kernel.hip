@@ -7,6 +7,7 @@
 #include "device_util.h"
 #include "join_cuts.h"
 #include "run_tiles.h"
+#include "weight_parts.h"
 
 namespace npas {
 
@@ -27,26 +28,6 @@ __device__ __forceinline__ uint2 read_columns(const uint8_t *p)
 {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
-}
-
-// The first 16-bit part of two weights, below them or equal, and what is left of them in their place: never zero where the weight is not (of fp16 weights, down
-// to 2^-14), as an infinite value times a part of zero would be NaN.
-template <int DT> __device__ __forceinline__ uint32_t part_below2(float &a, float &b)
-{
-    if constexpr (DT == NPAS_BF16) {
-        // (what is taken away is smaller than the part by 2^-24 of it: the weight counts as larger by that, in the one instruction that the difference takes)
-        const uint32_t u = __float_as_uint(a), w = __float_as_uint(b);
-        constexpr float c = 1.f - 0x1p-24f;
-        a = fmaf(__uint_as_float(u & 0xffff0000u), -c, a);
-        b = fmaf(__uint_as_float(w & 0xffff0000u), -c, b);
-        return __builtin_amdgcn_perm(w, u, 0x07060302u);
-    } else {
-        const uint32_t u = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u), w = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);
-        const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(u), __uint_as_float(w)));
-        a -= from_storage<DT>((uint16_t)x);
-        b -= from_storage<DT>((uint16_t)(x >> 16));
-        return x;
-    }
 }
 
 // Whether one of the two numbers is an infinity or a NaN.

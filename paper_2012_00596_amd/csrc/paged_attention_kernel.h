@@ -9,18 +9,11 @@
 #include "run_tiles.h"
 #include "device_util.h"
 #include "join_cuts.h"
+#include "weight_parts.h"
 
 namespace npas {
 
 constexpr int kRows = 2048; // tokens whose cache rows are looked up at once
-
-// Two 16-bit numbers below the weights a and b, next to them or nearly so; zero for zero.
-template <int DT> __device__ __forceinline__ uint32_t below2(float a, float b)
-{
-    const uint32_t u = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u), w = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);
-    if constexpr (DT == NPAS_BF16) return __builtin_amdgcn_perm(w, u, 0x07060302u);
-    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(u), __uint_as_float(w)));
-}
 
 // One workgroup a (sequence, key head, 16 of its query heads, cut): its four waves take tiles of 32 tokens in turn.
 // Both products run on 16 x 16 x 32 matrix instructions with the query heads as columns, so that a key or value is read once for all
@@ -41,15 +34,15 @@ template <int DT> __device__ __forceinline__ uint32_t below2(float a, float b)
 // (4.2 TB/s).
 // RUNS: columns are the rows (token, query head of the key head) of a run of new tokens, 16 in each of RUNS groups (0: one token a sequence): a key or value is read
 // once for all of them.  Where not every row sees every token of a tile, scores are left out by their positions, and values that are infinite or NaN, which a
-// weight of zero would spread, are added one by one to the rows that see them.  A weight goes in as two 16-bit numbers, as the products of two groups take the
-// time that one group left free (163 tokens over 32 sequences, three numbers 71 us, two 60).  32 sequences, 163 new tokens, 8 key heads of 128, up to 4096
-// tokens before them in 8 bits (0.15 GB): 57 us and 6 for the join; bound by the instructions between the loads, 4000 to 6000 cycles a wave and tile, in two rounds of
-// workgroups that the registers of two groups allow.
+// weight of zero would spread, are added one by one to the rows that see them.  A bf16 weight goes in as three 16-bit numbers here too, a fp16 one as two (22 bits).
+// 32 sequences, 163 new tokens, 8 key heads of 128, up to 4096 tokens before them in 8 bits (0.15 GB): 58 us and 6 for the join (with bf16 weights of
+// 17 bits, two numbers, 55).  Two groups of rows at head_dim up to 64: three waves a SIMD with some 6 registers in memory (32 sequences of 5 tokens on 4000, 4
+// key heads, in 8 bits 35 us, in 16 35; 64 of 6 on 2000, 8 key heads, 53 and 58) for two without (42, 38; 61 and 62).
 template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ __launch_bounds__(64 * NW, RUNS ? (NC == 2 ? 3 : NC == 4 ? 2 : 1) : NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
 {
     constexpr int G = RUNS ? RUNS : 1; // groups of 16 columns
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
-    constexpr int PITCH = DP + 4, PARTS = RUNS ? 2 : 3;
+    constexpr int PITCH = DP + 4, PARTS = RUNS && DT == NPAS_F16 ? 2 : 3;
     constexpr float GROW = !RUNS ? 0.f : DT == NPAS_BF16 ? 8.f : 4.f; // the maximum in use follows a row's scores where one exceeds it by 2^GROW
     constexpr float TOP = DT == NPAS_BF16 ? 1.f : RUNS ? 2048.f : 32768.f; // the largest weight is TOP 2^GROW
     __shared__ __align__(16) uint32_t rows[kRows];
@@ -312,9 +305,12 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
                 l[g] += p0 + p1;
 #pragma unroll
                 for (int n = 0; n < PARTS; ++n) {
-                    part[g][n][i] = n < PARTS - 1 ? below2<DT>(p0, p1) : pack2<DT>(p0, p1);
-                    p0 -= from_storage<DT>((uint16_t)part[g][n][i]);
-                    p1 -= from_storage<DT>((uint16_t)(part[g][n][i] >> 16));
+                    if constexpr (RUNS) part[g][n][i] = n < PARTS - 1 ? part_below2<DT>(p0, p1) : pack2<DT>(p0, p1);
+                    else {
+                        part[g][n][i] = n < PARTS - 1 ? below2<DT>(p0, p1) : pack2<DT>(p0, p1);
+                        p0 -= from_storage<DT>((uint16_t)part[g][n][i]);
+                        p1 -= from_storage<DT>((uint16_t)(part[g][n][i] >> 16));
+                    }
                 }
             }
         }

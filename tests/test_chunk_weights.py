@@ -73,6 +73,14 @@ def test_weights_keep_the_bits_of_fp32_in_tiles(torch, dt, T, D, where, steps):
     _weights(torch, dt, T, D, where, steps)
 
 
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("D,where,steps", WHERE)
+@pytest.mark.parametrize("T", [2, 20])
+def test_weights_keep_the_bits_of_fp32_in_short_runs(torch, dt, T, D, where, steps):
+    _weights(torch, dt, T if D <= 128 else T // 2, D, where, steps)
+
+
 def _strict(torch, ref, y, lse, dt, most, untouched=None):
     """_check without an allowance for a weight's rounding to the storage type: 320 u for sums as in test_attention_weights (a lane's sums in turn, of up to some
     2500 weights here, are off by the root of their number), the fp16 parts' 4 u, and what is lost below 2^-36 of the largest weight."""
@@ -101,5 +109,12 @@ def _is_short(case):
 @gpu
 @pytest.mark.parametrize("case", [c for c in runs.RUNS if not _is_short(c)], ids=str)
 def test_runs_in_tiles_without_an_allowance_for_rounded_weights(torch, monkeypatch, case):
+    monkeypatch.setattr(runs, "_check", _strict)
+    runs._run(torch, case)
+
+
+@gpu
+@pytest.mark.parametrize("case", [c for c in runs.RUNS if _is_short(c)], ids=str)
+def test_short_runs_without_an_allowance_for_rounded_weights(torch, monkeypatch, case):
     monkeypatch.setattr(runs, "_check", _strict)
     runs._run(torch, case)
