@@ -69,7 +69,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
 {
     constexpr int DP = 32 * ND, BM = 32 * WAVES, BN = 32 * NSUB, THREADS = 64 * WAVES, PIECES = DP / 8, STRIDE = DP * 2;
     constexpr int UNITS = E8 ? BN * PIECES / 2 : BN * PIECES, PER = (UNITS + THREADS - 1) / THREADS, IN_ROW = E8 ? PIECES / 2 : PIECES;
-    constexpr float GROW = DT == NPAS_BF16 ? 8.f : 4.f, TOP = DT == NPAS_BF16 ? 0.f : 11.f; // a weight is at most 2^(TOP + GROW)
+    constexpr float GROW = RunWeight<DT>::grow, UNIT = RunWeight<DT>::unit;
     constexpr int PARTS = DT == NPAS_BF16 ? 3 : 2; // 16-bit numbers that a weight is taken apart into
     __shared__ __align__(16) uint8_t kbuf[2][BN * STRIDE], vbuf[2][BN * STRIDE];
     constexpr int AHEAD = THREADS / BN; // steps whose tokens are looked up at once, one a thread
@@ -296,7 +296,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] *= c;
         }
-        const float base = m == -INFINITY ? 0.f : m - TOP;
+        const float base = m == -INFINITY ? 0.f : m;
         // 16 tokens at a time; between the products of one such part the next one's weights are formed, and its values read as soon as these have been multiplied
         constexpr int STRETCHES = 2 * NSUB;
         uint32_t pf[2][PARTS][4];
@@ -306,7 +306,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
         auto weigh = [&](int x, int pair) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 2 * pair; k < 2 * pair + 2; ++k) {
-                rest[k] = __builtin_amdgcn_exp2f(fmaf(sc[x >> 1][8 * (x & 1) + k], mul, -base));
+                rest[k] = __builtin_amdgcn_exp2f(fmaf(sc[x >> 1][8 * (x & 1) + k], mul, -base)) * UNIT;
                 l += rest[k];
             }
         };
@@ -412,7 +412,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
                     const int d = 32 * dt + 8 * g + 4 * h;
                     if (d < D) *reinterpret_cast<float4 *>(part + d) = make_float4(o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]);
                 }
-        if (h == 0) a.part_stat[out_row * a.splits + cut] = make_float2(m - TOP, l);
+        if (h == 0) a.part_stat[out_row * a.splits + cut] = make_float2(m, l);
         return;
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -426,7 +426,7 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
                 *reinterpret_cast<Words *>(reinterpret_cast<uint16_t *>(a.y) + out_row * D + d) =
                     Words{{pack2<DT>(o[dt][4 * g] * inv, o[dt][4 * g + 1] * inv), pack2<DT>(o[dt][4 * g + 2] * inv, o[dt][4 * g + 3] * inv)}};
         }
-    if (h == 0 && a.lse) a.lse[out_row] = l != 0.f ? (m - TOP + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (h == 0 && a.lse) a.lse[out_row] = l != 0.f ? (m + log2f(l * (1.f / UNIT))) * 0.6931471805599453f : -INFINITY;
 }
 
 // One wave a row, for up to 16 cuts: their sums, rescaled to the largest maximum and added in their order (64 tokens of 32 heads in 4 to 11 cuts: the whole call
@@ -468,7 +468,7 @@ template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_ke
     struct __attribute__((packed, aligned(2))) Words { uint32_t w[2]; };
     if (lane * 4 < D)
         *reinterpret_cast<Words *>(reinterpret_cast<uint16_t *>(a.y) + row * D + lane * 4) = Words{{pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv)}};
-    if (lane == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (lane == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l * (1.f / RunWeight<DT>::unit))) * 0.6931471805599453f : -INFINITY;
 }
 
 int launch_chunk_attention(int dt, const ChunkArgs &a, void *stream)

@@ -4,6 +4,7 @@
 
 #include "decoder_internal.h"
 #include "device_util.h"
+#include "weight_parts.h"
 
 namespace npas {
 
@@ -73,6 +74,7 @@ template <int DT, int LANES, int THREADS, typename Args> __global__ __launch_bou
         for (int k = 0; k < SIDE; ++k) sum += so[k][i];
         reinterpret_cast<uint16_t *>(a.y)[row * D + i] = to_storage<DT>(l != 0.f ? sum / l : 0.f);
     }
+    if constexpr (RUNS) l *= 1.f / RunWeight<DT>::unit;
     if (tid == 0 && a.lse) a.lse[row] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 

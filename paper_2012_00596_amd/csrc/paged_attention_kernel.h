@@ -43,8 +43,9 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
     constexpr int G = RUNS ? RUNS : 1; // groups of 16 columns
     constexpr int DP = 32 * NC, VW = DP / 16, VP = VW < 8 ? 1 : VW / 8, VD = VW / VP / 2; // a lane's value row: VP pieces of VD words
     constexpr int PITCH = DP + 4, PARTS = RUNS && DT == NPAS_F16 ? 2 : 3;
-    constexpr float GROW = !RUNS ? 0.f : DT == NPAS_BF16 ? 8.f : 4.f; // the maximum in use follows a row's scores where one exceeds it by 2^GROW
-    constexpr float TOP = DT == NPAS_BF16 ? 1.f : RUNS ? 2048.f : 32768.f; // the largest weight is TOP 2^GROW
+    constexpr float GROW = RUNS ? RunWeight<DT>::grow : 0.f; // the maximum in use follows a row's scores where one exceeds it by 2^GROW
+    constexpr float TOP = RUNS ? RunWeight<DT>::unit : DT == NPAS_BF16 ? 1.f : 32768.f; // the largest weight is TOP 2^GROW
+    constexpr float LEAVE = RUNS ? 1.f : 1.f / TOP, UNIT = RUNS ? TOP : 1.f; // factor of the sums that leave the kernel, and of the weights in them
     __shared__ __align__(16) uint32_t rows[kRows];
     __shared__ float sm[NW][16], sl[NW][16];
     __shared__ __align__(16) float so[NW * 16 * PITCH];
@@ -401,7 +402,7 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const float c = sm[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][n] - top) * (1.f / TOP);
+                const float c = sm[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][n] - top) * LEAVE;
                 const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + n) * PITCH + d);
                 sum += c * sl[w][n];
                 y.x += c * v.x, y.y += c * v.y, y.z += c * v.z, y.w += c * v.w;
@@ -415,7 +416,7 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
                 const float v[4] = {y.x * inv, y.y * inv, y.z * inv, y.w * inv};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) out[k] = to_storage<DT>(v[k]);
-                if (d == 0 && a.lse) a.lse[row] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                if (d == 0 && a.lse) a.lse[row] = sum != 0.f ? (top + log2f(sum * (1.f / UNIT))) * 0.6931471805599453f : -INFINITY;
             }
         }
     }

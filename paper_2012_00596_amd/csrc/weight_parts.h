@@ -4,6 +4,13 @@
 
 namespace npas {
 
+// Attention of runs: a row's weight is UNIT of exp(score - the maximum in use), which follows the scores only where one exceeds it by 2^GROW.  bf16 weights are
+// 1 at the most, so that sums of large values pass the end of fp32 no sooner than those of the attention of one token; fp16 ones, whose type ends at 2^-24
+// below, 2^15.  (A factor of the exponential: an exponent moved by 8 or 11 would be rounded more coarsely.)
+template <int DT> struct RunWeight {
+    static constexpr float unit = DT == NPAS_BF16 ? 0x1p-8f : 0x1p11f, grow = DT == NPAS_BF16 ? 8.f : 4.f;
+};
+
 // Two 16-bit numbers below the weights a and b, next to them or nearly so; zero for zero.
 template <int DT> __device__ __forceinline__ uint32_t below2(float a, float b)
 {

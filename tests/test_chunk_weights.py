@@ -118,3 +118,27 @@ def test_runs_in_tiles_without_an_allowance_for_rounded_weights(torch, monkeypat
 def test_short_runs_without_an_allowance_for_rounded_weights(torch, monkeypatch, case):
     monkeypatch.setattr(runs, "_check", _strict)
     runs._run(torch, case)
+
+
+@gpu
+@pytest.mark.parametrize("T,D", [(2, 64), (20, 128), (2, 256), (40, 64), (150, 128), (30, 256)])
+@pytest.mark.parametrize("n,e8", [(600, False), (600, True), (6000, False)])
+def test_large_bf16_values_beside_scores_that_grow(torch, T, D, n, e8):
+    """Values of 2^114 to 2^115 whose weights sum to their number at most: 2^13 2^115 is a number of fp32.  Scores grow by 5.5 halfway, a factor of 245 that a maximum
+    need not follow.  An exponent is off by 2.44 u and u 8, a sum's roundings are as many as test_attention_weights' 320 u has."""
+    S, H = 2, 2
+    g = torch.Generator().manual_seed(4)
+    k, v = torch.zeros((S, n, H, D), dtype=torch.float64), 2.0 ** 114 * (1 + _round(torch, torch.rand((S, n, H, D), generator=g, dtype=torch.float64), npas.BF16))
+    v = _round(torch, v, npas.BF16)
+    if e8:
+        v = c8.dequantise(*c8.quantise(v, npas.BF16))
+    k[:, n // 2:, :, 0] = 5.5
+    q = torch.zeros((S, T, H, D), dtype=torch.float64)
+    q[..., 0] = 1
+    y, lse = _runs(torch, npas.BF16, q, k, v, 16, [n] * S, 1.0, e8=e8)
+    for t in range(T):
+        seen = n - T + t + 1
+        p = torch.softmax(k[:, :seen, :, 0], 1)[..., None]
+        ref = (p * v[:, :seen]).sum(1)
+        assert not bool(_outside(y[:, t], ref, ref, npas.BF16, 320).any()), t
+        assert float((lse[:, t] - torch.logsumexp(k[:, :seen, :, 0], 1)).abs().max()) <= 320 * u
