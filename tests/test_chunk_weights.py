@@ -142,3 +142,49 @@ def test_large_bf16_values_beside_scores_that_grow(torch, T, D, n, e8):
         ref = (p * v[:, :seen]).sum(1)
         assert not bool(_outside(y[:, t], ref, ref, npas.BF16, 320).any()), t
         assert float((lse[:, t] - torch.logsumexp(k[:, :seen, :, 0], 1)).abs().max()) <= 320 * u
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("H,KV,D,T,n,window", [
+    (4, 2, 64, 2, 40, 0), (8, 2, 128, 3, 300, 0), (2, 1, 96, 10, 3000, 0), (4, 2, 64, 14, 2500, 700), (4, 2, 256, 3, 300, 0), (2, 1, 256, 7, 2500, 0),
+    (4, 4, 64, 60, 60, 0), (8, 2, 128, 40, 300, 0), (2, 1, 96, 70, 3000, 0), (4, 2, 256, 33, 500, 0), (2, 1, 80, 90, 600, 100), (1, 1, 128, 130, 2500, 0)])
+@pytest.mark.parametrize("scores", ["spread", "same", "low"])
+def test_infinite_values_come_out_as_they_are_where_they_are_seen(torch, scores, dt, H, KV, D, T, n, window):
+    """Two of three elements of a head have an infinite value of one token, of the prefix or the run; the last two have one of each sign or a NaN.  Rows that see it
+    have it, of its sign; all else is what it is without.  Weights of every size down to where the library promises it: by scores within 7; all the same, exact
+    16-bit numbers; and all but the first 2^-11.7 of it (bf16: 2^-69.3) or some more."""
+    S = 3
+    g = torch.Generator().manual_seed(H + D + T)
+    q, k, v = (torch.randn(shape, generator=g, dtype=torch.float64) for shape in ((S, T, H, D), (S, n, KV, D), (S, n, KV, D)))
+    q[..., 1:] = 0
+    if scores == "low":
+        q[..., 0] = 1
+        k[..., 0] = 0.2 * torch.rand((S, n, KV), generator=g)
+        k[:, 0, :, 0] = 8.1 if dt == npas.F16 else 48
+    else:
+        q, k = (q * (scores == "spread")).clamp(-1, 1), k.clamp(-3.5, 3.5)
+    clean, lse = _runs(torch, dt, q, k, v, 16, [n] * S, 1.0, window)
+    bad, token = v.clone(), torch.randint(max(0, n - T - 40), n, (S, KV, D), generator=g)
+    far = torch.rand((S, KV, D), generator=g) < 0.3
+    token = torch.where(far, torch.randint(0, n, (S, KV, D), generator=g), token)
+    sign = torch.where(torch.rand((S, KV, D), generator=g) < 0.5, -1.0, 1.0).double()
+    at = torch.arange(n - T, n)
+    want = clean.clone()
+    for s in range(S):
+        for h in range(KV):
+            for d in range(D):
+                if d % 3 == 2 and d < D - 2:
+                    continue
+                odd = [(int(token[s, h, d]), float(sign[s, h, d]) * float("inf"))]
+                if d >= D - 2:
+                    odd.append(((odd[0][0] + 1) % n, -odd[0][1] if s % 2 else float("nan")))
+                for j, value in odd:
+                    bad[s, j, h, d] = value
+                    see = (j <= at) & ((j > at - window) if window else True)
+                    before = want[s, see, h * (H // KV):(h + 1) * (H // KV), d]
+                    want[s, see, h * (H // KV):(h + 1) * (H // KV), d] = torch.where(torch.isfinite(before), value, before + value)
+    y, again = _runs(torch, dt, q, k, bad, 16, [n] * S, 1.0, window)
+    assert torch.equal(again, lse)
+    same = (y == want) | ((y != y) & (want != want))
+    assert int((~same).sum()) == 0, f"{int((~same).sum())} of {y.numel()}, first {torch.nonzero(~same)[0].tolist()}"
