@@ -320,7 +320,8 @@ int npas_paged_attention(const npas_kv_cache *cache, const void *q_dev, int64_t 
  * as the byte e + 127 in k_scale and v_scale [pages][kv_heads][page_size][ceil(head_dim / 32)], 16-byte aligned, and per element the NPAS_E4M3
  * number nearest to x / 2^e, ties to the even code.  e is the least of -15 .. 8 (dtype NPAS_F16; NPAS_BF16: -110 .. 120) with magnitudes up to
  * 448 * 2^e; at the largest e they stop at 240 * 2^e (61440, or 3.19e38).  So every number that a cache written here stands for is one of dtype's.  A block
- * that holds an infinity or a NaN has byte 255 and stands for NaN throughout.  head_dim: a multiple of 16.  dtype is the storage type of the rows outside: queries, keys,
+ * that holds an infinity or a NaN has byte 255 and stands for NaN throughout, whatever its codes.  A cache may be filled elsewhere: with bytes of those e
+ * or 255, at the largest e no magnitude above 240 * 2^e; a NaN code is NaN alone.  What other bytes and numbers stand for is undefined.  head_dim: a multiple of 16.  dtype is the storage type of the rows outside: queries, keys,
  * values, results.  The calls above refuse such a cache; those below take scales == NULL for a cache of 16 bits. */
 typedef struct {
     void *k_scale_dev, *v_scale_dev;

@@ -23,6 +23,13 @@ template <int DT> __device__ __forceinline__ uint4 from_e4m3x8(uint2 codes, uint
                       from_e4m3x2<DT, true>(codes.y, byte));
 }
 
+// The top bits of those of a word's four codes that stand for NaN: by the code or by the scale byte.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t codes, uint32_t byte)
+{
+    const uint32_t n = ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return byte == 255 ? 0x80808080u : n;
+}
+
 // The scale byte of a block whose largest magnitude has the bits `top` (of fp32 without the sign; a NaN's are the largest).
 template <int DT> __device__ __forceinline__ uint32_t scale8_of(uint32_t top)
 {

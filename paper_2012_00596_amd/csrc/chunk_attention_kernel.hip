@@ -179,7 +179,11 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
         if (parted(i)) {
             bool bad = false;
 #pragma unroll
-            for (int u = 0; u < PER; ++u) bad = bad || scale8[1][u] == 255;
+            for (int u = 0; u < PER; ++u) {
+                const uint4 w = in[1][u];
+                const uint32_t byte = scale8[1][u];
+                bad = bad || (nan_codes(w.x, byte) | nan_codes(w.y, byte) | nan_codes(w.z, byte) | nan_codes(w.w, byte)) != 0;
+            }
             if (bad) odd[i & 1] = 1;
         }
 #pragma unroll

@@ -203,12 +203,9 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
         auto odd16 = [](uint32_t v) __attribute__((always_inline)) { return (v & e) == e; };
         bool odd = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (E8) odd = odd || vs[i] == 255;
-            else
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int w = 0; w < VR; ++w) odd = odd || odd16(vt[i][w]) || odd16(vt[i][w] >> 16);
-        }
+            for (int w = 0; w < VR; ++w) odd = odd || (E8 ? nan_codes(vt[i][w], vs[E8 ? i : 0]) != 0 : odd16(vt[i][w]) || odd16(vt[i][w] >> 16));
         if (!__any(odd)) return;
         // the tile's values by token, in the wave's part of LDS; a lane reads those of its results
         uint16_t *tile = reinterpret_cast<uint16_t *>(so + wave * 16 * PITCH);
@@ -216,7 +213,11 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int w = 0; w < VW / 2; ++w) {
-                const uint32_t mine = E8 ? (vs[E8 ? i : 0] == 255 ? 0xffffffffu : 0u) : vt[i][E8 ? 0 : w];
+                uint32_t mine = vt[i][E8 ? w >> 1 : w]; // (8 bits: the NaN alone)
+                if constexpr (E8) {
+                    const uint32_t n = nan_codes(mine, vs[i]) >> 16 * (w & 1);
+                    mine = (n & 0x80u ? 0xffffu : 0u) | (n & 0x8000u ? 0xffff0000u : 0u);
+                }
                 *reinterpret_cast<uint32_t *>(tile + (16 * (i >> 2) + 4 * q + (i & 3)) * DP + VW * r + 2 * w) = mine;
             }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -238,10 +239,9 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if constexpr (E8) {
-                const bool none = vs[i] == 255;
 #pragma unroll
-                for (int w = 0; w < VR; ++w) vt[i][w] = none ? 0u : vt[i][w];
-                vs[i] = none ? 127u : vs[i];
+                for (int w = 0; w < VR; ++w) vt[i][w] &= ~((nan_codes(vt[i][w], vs[i]) >> 7) * 255u);
+                vs[i] = vs[i] == 255 ? 127u : vs[i]; // (its codes are zero now)
             } else
 #pragma unroll
                 for (int w = 0; w < VR; ++w) vt[i][w] &= (odd16(vt[i][w]) ? 0xffff0000u : ~0u) & (odd16(vt[i][w] >> 16) ? 0xffffu : ~0u);
