@@ -116,7 +116,9 @@ template <int DT, bool E8, int ROT, int P> __global__ __launch_bounds__(256) voi
                 float s = 0.f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) s = fmaf(x[j][k], x[j][k], s);
-                const float r = __builtin_amdgcn_rsqf(fmaf(lanes_sum<P>(s), a.inv_d, a.eps)); // (an ulp; what lies behind the head is zero and stays so)
+                const float mean = fmaf(lanes_sum<P>(s), a.inv_d, a.eps);
+                const bool small = mean < 0x1p-100f; // (the instruction takes a subnormal number for zero)
+                const float r = __builtin_amdgcn_rsqf(small ? mean * 0x1p64f : mean) * (small ? 0x1p32f : 1.f); // (an ulp; what lies behind the head is zero and stays so)
                 if (is_q) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) x[j][k] *= r * wq[k];
