@@ -188,3 +188,37 @@ def test_infinite_values_come_out_as_they_are_where_they_are_seen(torch, scores,
     assert torch.equal(again, lse)
     same = (y == want) | ((y != y) & (want != want))
     assert int((~same).sum()) == 0, f"{int((~same).sum())} of {y.numel()}, first {torch.nonzero(~same)[0].tolist()}"
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("H,KV,D,T,n", [(4, 2, 64, 3, 300), (8, 2, 128, 2, 3000), (4, 2, 64, 40, 90), (8, 2, 128, 40, 3000), (2, 1, 96, 130, 500), (2, 1, 256, 30, 300)])
+def test_infinite_and_nan_scores_of_runs(torch, dt, H, KV, D, T, n):
+    """By sequence: a score of inf; one of -inf; only -inf; one of inf and one NaN; none of these.  The odd keys stand among the run, so that some rows do not see them."""
+    S, a = 5, n - T // 2 - 1
+    g = torch.Generator().manual_seed(H + D + 1)
+    k, v, q = (torch.randn(shape, generator=g, dtype=torch.float64) for shape in ((S, n, KV, D), (S, n, KV, D), (S, T, H, D)))
+    q[..., 0] = 1
+    q, k, v = (_round(torch, x, dt) for x in (q, k, v))
+    k[0, a, :, 0] = k[3, a, :, 0] = float("inf")
+    k[1, a, :, 0] = k[2, :, :, 0] = -float("inf")
+    k[3, n - 1, :, 0] = float("nan")
+    y, lse = _runs(torch, dt, q, k, v, 16, [n] * S, 0.125)
+    sees = torch.arange(n - T, n) >= a
+    assert bool(sees.any())
+    assert bool((y[0, sees] != y[0, sees]).all()) and bool((lse[0, sees] == float("inf")).all())
+    assert bool((y[3, sees] != y[3, sees]).all()) and bool((lse[3, sees][:-1] == float("inf")).all()) and bool((lse[3, -1] != lse[3, -1]).all())
+    assert bool((y[2] == 0).all()) and bool((lse[2] == -float("inf")).all())
+    for s in (0, 1, 3, 4):
+        for t in range(T):
+            if s in (0, 3) and bool(sees[t]):
+                continue
+            j = [i for i in range(n - T + t + 1) if not (s == 1 and i == a)]
+            for h in range(H):
+                keys = k[s, j, h // (H // KV)]
+                x = keys @ q[s, t, h] * 0.125
+                off = D * u * float((keys.abs() @ q[s, t, h].abs()).max()) * 0.125
+                p, value = torch.softmax(x, 0), v[s, j, h // (H // KV)]
+                lost = n * 2.0 ** -36 / u if dt == npas.F16 else 0
+                assert not bool(_outside(y[s, t, h], p @ value, p @ value.abs(), dt, 2 * off / u + 320 + MORE[dt] + lost).any()), (s, t, h)
+                assert abs(float(lse[s, t, h] - torch.logsumexp(x, 0))) <= off + 320 * u
