@@ -56,14 +56,14 @@ __device__ __forceinline__ float over_halves(float x)
 // 16-bit numbers straight from memory, 8-bit floats through registers, where they become 16-bit numbers.  Loads are issued a part at a time between the
 // products.  The cache rows of 4 or 8 steps' tokens are looked up at once, a token a thread, in the step before they are needed.
 // The maximum in use follows a row's scores only where one exceeds it by 2^GROW, so that sums are hardly ever rescaled.  A weight enters the second product as
-// 16-bit numbers whose sum it is, three in bf16 and two in fp16 (22 bits), so that results are those of fp32 weights; one rounded number took 162 us for
-// the prompts below, 76 and 2280 for the other cases of its kind.  Masks, absent tokens and values that are not finite are branches that the steps which every
+// 16-bit numbers whose sum it is, three in bf16 and two in fp16 (22 bits), so that results are those of fp32 weights (one rounded number: 160 us for the
+// prompts below, 2.33 ms for the long sequence).  Masks, absent tokens and values that are not finite are branches that the steps which every
 // row sees whole do not have.
 // (Measured with one number a weight: the banks, 2048 tokens on 63000 2.41 -> 2.34 ms; loads by parts, 8191 prompt tokens 182 -> 172 us; branches for selects,
 // 343 -> 183.)
-// Bound by the matrix cores: one sequence's 2048 tokens on 63000, 32 query and 8 key heads of 128 in 8 bits: 3.71 ms, its instructions at 1160 TFLOP/s (a large
-// library product 1250); 8191 tokens of five prompts in 16 bits 236 us (930 TFLOP/s), where the diagonal's half-empty steps and the last, partial round of
-// workgroups count.
+// Bound by the matrix cores: one sequence's 2048 tokens on 63000, 32 query and 8 key heads of 128 in 8 bits: 3.65 to 3.86 ms, its instructions at 1110 to 1180 TFLOP/s
+// (a large library product 1250); 8191 tokens of five prompts in 16 bits 245 to 275 us (800 to 900 TFLOP/s), where the diagonal's half-empty steps and the order
+// and the last, partial round of workgroups count.
 // BN is 64 tokens for heads of up to 128, two workgroups a compute unit; 32 for longer ones, whose tiles fill LDS and registers.
 template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __global__ __launch_bounds__(64 * WAVES, OCC) void chunk_attention_kernel(ChunkArgs a)
 {
@@ -433,8 +433,9 @@ template <int DT, bool E8, int ND, int NSUB, int WAVES, int OCC, bool FULL> __gl
     if (h == 0 && a.lse) a.lse[out_row] = l != 0.f ? (m + log2f(l * (1.f / UNIT))) * 0.6931471805599453f : -INFINITY;
 }
 
-// One wave a row, for up to 16 cuts: their sums, rescaled to the largest maximum and added in their order (64 tokens of 32 heads in 4 to 11 cuts: the whole call
-// 18 to 22 us, with a workgroup a row as more cuts have it 20 to 25; in 118 cuts, read in this way, 61, in that 28).  The bytes of the sums bound it.
+// One wave a row, for up to 16 cuts: their sums, rescaled to the largest maximum and added in their order (64 tokens of 32 heads in 4 to 11 cuts: the whole call,
+// with weights of one number, 18 to 22 us, with a workgroup a row as more cuts have it 20 to 25; in 118 cuts, read in this way, 61, in that 28).  The bytes of the
+// sums bound it.
 template <int DT> __global__ __launch_bounds__(256) void chunk_attention_join_kernel(ChunkArgs a)
 {
     const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);

@@ -48,11 +48,11 @@ int check_cache(const npas_kv_cache *c, const npas_kv_scales *scales, int heads,
 //     pairs of 777 tokens, head_dim 64, 8.0 us in one cut, 9.3 in seven; replayed from a graph 8.2 and 7.1; 128 pairs of 300 tokens,
 //     head_dim 128, in a graph 7.2 and 9.9).
 //   - In that case eight waves where every workgroup has a compute unit to itself (16 pairs of 777 tokens 8.7 us, with four 9.4); otherwise four,
-//     two or three workgroups on a compute unit (512 pairs of up to 8192 tokens in one cut 227 us, with eight waves 244).
+//     two or three workgroups on a compute unit (512 pairs of up to 8192 tokens in one cut, in their order, 227 us, with eight waves 244).
 //   - Longer ones in 512 workgroups (131071 tokens of 4 pairs 54 us, in 1024 workgroups 56), at least 128 tokens each (4096 tokens of 8 pairs
 //     8.6 us, 256 each 10.3); and at most 2048, so that a long sequence in a ragged batch does not run alone at the end (512 pairs of
-//     up to 8192 tokens 227 us, in one cut 225, before the cuts met the compute units in turn, which made it 210); in 8-bit caches, whose cuts are
-//     read in half the time, at most 1024 (163 new tokens over 32 sequences of some 4096 59 to 64 us, 2048 each 64 to 68, 512 each 68; the pairs 116 to 122 all the same).
+//     up to 8192 tokens 205 us, at most 1024 each 198 to 202); in 8-bit caches, whose cuts are read in half the time, at most 1024 (the same pairs 116 us, 2048
+//     each 122, 512 each 118; 163 new tokens over 32 sequences of some 4096 65 us, 2048 each 67, 512 each 69).
 // Cuts follow max_length, not the lengths, which are on the device: a launch for much longer sequences than it meets leaves compute units idle
 // (8 pairs of 4096 tokens, head_dim 128, 8.7 us at max_length 4096, 11.7 at 32768, 25.5 at 131072; 128 pairs of 2048 26 us, 65 at 32768).
 Cuts plan_cuts(const CacheArgs &c, long pairs, size_t rows, int max_length, int window)

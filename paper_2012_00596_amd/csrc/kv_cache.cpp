@@ -10,14 +10,15 @@ namespace {
 
 // How a launch takes the rows and cuts the tokens.  Rows: (token, query head) of a key head.
 //   - Runs of up to 32 rows on average (of heads longer than 128: 16, and up to 32 in tiles of 16, which is all that the registers hold): the kernel of single
-//     tokens with one or two groups of 16 rows, cut as that is.  32 sequences of 5 tokens, 4 query heads a key head, in 8 bits 62 us, in tiles of kChunkRows
-//     86; 5 tokens of one sequence 9.3 and 11.2; in 16 bits, which tiles take straight from memory, both are near alike (16 sequences of 8 tokens on 4000
-//     54 and 54, 64 of 3 on 2000 59 and 53).
+//     tokens with one or two groups of 16 rows, cut as that is.  32 sequences of 5 tokens on 4000, 4 query heads a key head, head_dim 128, in 8 bits 71 us,
+//     in tiles of kChunkRows 126; 16 of 8 40 and 61, in 16 bits 54 and 67; 5 tokens of one sequence 9.5 and 12.6; 4 of each of 32 at head_dim 256 251 and 325.
+//     (7 tokens of one sequence on 8000 19.4 and 18.5.)
 //   - Longer ones: tiles of kChunkRows.  Where they do not fill the card, a tile's tokens are cut for kWorkgroups in all, two a compute unit (256 tokens on 30000,
-//     4 key heads and 8 query heads each: 149 us; for 1024 163, for 256 168).
+//     4 key heads and 8 query heads each: 236 us; for 1024 245, for 256 245).
 //   - A cut more costs each row head_dim floats written and read, a token more in a cut its walk: their sum is least at a length that goes with the root of
-//     rows and tokens (64 tokens of 32 heads on 8192: 32 cuts of 256 35 us, 16 of 512 30, 8 of 1024 36; on 30000, 8 heads, 256 each 28 to 31, 512 28), and
-//     kLeast at the least (on 1000: 256 each 18 us, 512 22).
+//     rows and tokens (64 tokens of 32 heads on 8192: 16 cuts of 512 35 us, half as long 37, twice 40; on 30000, 8 heads, 512 32, 256 each 34, 1024 38), and
+//     kLeast at the least (on 1000: 256 each 20 us, 512 26).
+// The mean decides for all runs of a call: one of 500 tokens beside 63 single tokens on 4096 takes 347 us in 16 bits and 344 in 8, in two calls 79 + 189 and 76 + 112.
 struct ChunkPlan {
     int groups; // of 16 rows; 0: tiles of kChunkRows
     long places;

@@ -56,8 +56,10 @@ enum { PAIRS, FAR_HALF, LANES, LDS };
 // The sum of squares is a tree over the P lanes, of lane patterns where 16 lanes hold a head (through LDS 49.6 us of the prompt below, so 47.5).  A block of
 // 8-bit floats is four lanes.
 // Bound by memory for long calls: 8191 tokens of 32 query and 8 key heads of 128, 206 MB, 46 us between other launches (4.4 TB/s; a large copy 5.0), 34 where
-// the caches still hold what it reads.  5003 tokens of 80 elements into 8 bits 17 us (the instructions of the conversion; 2.5 TB/s).  For single
-// tokens a launch and a chain of latencies, position, page, row: 24 tokens 10 us from call to call.
+// the caches still hold what it reads.  5003 tokens of 20 query and 5 key heads of 80 elements into 8 bits 15.8 us of a row of calls (2.5 TB/s), into 16 15.4, keys and
+// values alone 11.3 and 11.0: what 8 bits save in bytes, and what their conversion costs, hardly show.  Vector instructions take 60 % of that time, 40000 tokens go
+// at 3.7 TB/s; what bounds the short call beside its latencies is not known.  For single tokens a launch and a chain of latencies, position, page, row: 24 tokens
+// 10 us from call to call.
 template <int DT, bool E8, int ROT, int P> __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a)
 {
     constexpr int SIDE = 4; // heads of a lane on their way
@@ -225,7 +227,7 @@ int launch_kv_write(int dt, const WriteArgs &a, void *stream)
 }
 
 // One workgroup a token; a thread has eight elements of a key or value: a code is its value times a power of two, so nothing is rounded.
-// Bound by memory and, in one round of workgroups, by the chain position, page, row: 5003 tokens of 5 key heads of 80 5 us.
+// 5003 tokens of 5 key heads of 80 5 us, 2.4 TB/s: one round of workgroups, the chain position, page, row; 40000 tokens 27 us, 3.6 TB/s.
 template <int DT> __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a)
 {
     const int t = blockIdx.x, D = a.c.head_dim, vectors = D >> 3, heads = a.c.kv_heads, blocks = (D + 31) >> 5;

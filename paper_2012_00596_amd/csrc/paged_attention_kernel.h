@@ -25,18 +25,19 @@ constexpr int kRows = 2048; // tokens whose cache rows are looked up at once
 // A weight goes in as three 16-bit numbers whose sum it is: the matrix cores have time for them (the kernel waits for memory).  The first two
 // are taken below what there is to represent, so that all three are positive and an infinite value comes out as itself.  fp16 reaches
 // down to 2^-24 only, so there the largest weight is 2^15: what is below 2^-39 of it is lost.
-// Memory bound: 64 sequences of up to 8192 tokens, 8 key heads of 128, 1.07 GB in 210 us with the join (5.1 TB/s); one of 131071, 4 key heads, 55 us
+// Memory bound: 64 sequences of up to 8192 tokens, 8 key heads of 128, 1.07 GB in 205 us with the join (5.2 TB/s); one of 131071, 4 key heads, 55 us
 // (4.9 TB/s).  Few short sequences are a chain of latencies: a launch, the length, the pages, then 1.1-1.8 us a round of tiles.
 // E8: the cache holds 8-bit floats with a power of two for 32 elements.  A lane keeps the bytes and the scales of its next tile and makes 16-bit numbers of
 // them, exactly, when they are multiplied: keys as the first product's operand (where head_dim is DP a lane takes 16 consecutive elements of 64, so that a load
 // has 16 bytes; the query's elements are taken in the same order), values before they are turned round.  Half the bytes for more instructions, still bound by
-// memory where there is enough of it: the 64 sequences, 0.55 GB, 119 us with the join (4.7 TB/s; of one length 5.4 to 5.6), the one of 131071 33 us
+// memory where there is enough of it: the 64 sequences, 0.55 GB, 116 to 123 us with the join (4.5 to 4.8 TB/s), the one of 131071 33 us
 // (4.2 TB/s).
 // RUNS: columns are the rows (token, query head of the key head) of a run of new tokens, 16 in each of RUNS groups (0: one token a sequence): a key or value is read
 // once for all of them.  Where not every row sees every token of a tile, scores are left out by their positions, and values that are infinite or NaN, which a
 // weight of zero would spread, are added one by one to the rows that see them.  A bf16 weight goes in as three 16-bit numbers here too, a fp16 one as two (22 bits).
-// 32 sequences, 163 new tokens, 8 key heads of 128, up to 4096 tokens before them in 8 bits (0.15 GB): 58 us and 6 for the join (with bf16 weights of
-// 17 bits, two numbers, 55).  Two groups of rows at head_dim up to 64: three waves a SIMD with some 6 registers in memory (32 sequences of 5 tokens on 4000, 4
+// 32 sequences, 163 new tokens, 8 key heads of 128, up to 4096 tokens before them in 8 bits (0.15 GB): 65 us with the join (with bf16 weights of 17 bits, two
+// numbers, 61; the same tokens over 16 bits, 0.28 GB, 69 to 78).  Not bound by memory: some 650 workgroups have work and 512 fit at once, so that the last ones
+// run alone.  Two groups of rows at head_dim up to 64: three waves a SIMD with some 6 registers in memory (32 sequences of 5 tokens on 4000, 4
 // key heads, in 8 bits 35 us, in 16 35; 64 of 6 on 2000, 8 key heads, 53 and 58) for two without (42, 38; 61 and 62).
 template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ __launch_bounds__(64 * NW, RUNS ? (NC == 2 ? 3 : NC == 4 ? 2 : 1) : NC == 2 ? 4 : NC == 4 ? (NW == 4 && FULL ? 3 : 2) : 1) void paged_attention_kernel(AttentionArgs a)
 {
@@ -56,7 +57,8 @@ template <int DT, int NC, bool FULL, int NW, bool E8, int RUNS = 0> __global__ _
     id /= a.c.kv_heads;
     // Workgroups go to the compute units in turn, so the cuts of a sequence start at one or another: in their order, the last, often empty ones would all meet
     // the same units
-    // (64 sequences of up to 8192 tokens, 8 key heads of 128, a launch without its join: 143 us in their order and 112 so in 8 bits, 210 and 185 in 16).
+    // (64 sequences of up to 8192 tokens, 8 key heads of 128, two ragged batches, a launch without its join: in their order 129 and 122 us and so 116 and 106 in 8
+    // bits, 229 and 213, 209 and 194 in 16).
     auto turned = [&](uint32_t n) { return (int)((id % a.splits + (n * 0x9e3779b1u >> 16)) % a.splits); };
     int h0 = 0, split, s, first, count; // h0: first of the group's heads here
     RunTile tile_of_run{};
