@@ -101,9 +101,9 @@ def _strict(torch, ref, y, lse, dt, most, untouched=None):
 
 def _is_short(case):
     """Whether a case of runs.RUNS goes through the kernel of short runs."""
-    H, KV, D, _, new = case[:5]
+    H, KV, _, _, new = case[:5]
     mean = -(-sum(n for n, _ in new) * (H // KV) // len(new))
-    return mean <= (16 if D > 128 else 32)
+    return mean <= 32
 
 
 @gpu
@@ -222,3 +222,16 @@ def test_infinite_and_nan_scores_of_runs(torch, dt, H, KV, D, T, n):
                 lost = n * 2.0 ** -36 / u if dt == npas.F16 else 0
                 assert not bool(_outside(y[s, t, h], p @ value, p @ value.abs(), dt, 2 * off / u + 320 + MORE[dt] + lost).any()), (s, t, h)
                 assert abs(float(lse[s, t, h] - torch.logsumexp(x, 0))) <= off + 320 * u
+
+
+@gpu
+@pytest.mark.parametrize("case", [
+    (8, 2, 64, 16, [(300, 300)] + [(1, 50 + 7 * i) for i in range(40)] + [(0, 9)] * 5, 0, npas.BF16, False, False),     # by the mean in tiles of 32 rows
+    (4, 4, 128, 16, [(1, 90)] * 20 + [(0, 0)] * 11 + [(260, 700), (2, 2)], 0, npas.BF16, True, False),                    # of 16
+    (4, 2, 256, 16, [(0, 5)] * 9 + [(100, 140), (1, 33)], 0, npas.F16, False, False),
+    (8, 1, 64, 16, [(1, 40)] * 30 + [(500, 800)], 100, npas.F16, True, False),                                            # of 128
+    (16, 2, 96, 24, [(700, 700), (0, 3), (1, 2000), (1, 1), (3, 64)], 0, npas.BF16, False, False)], ids=lambda c: str(c[:4]))
+def test_a_long_run_among_single_tokens_and_idle_sequences(torch, monkeypatch, case):
+    """The mean run decides how all of them go; results are those of each by itself."""
+    monkeypatch.setattr(runs, "_check", _strict)
+    runs._run(torch, case)
