@@ -235,3 +235,23 @@ def test_a_long_run_among_single_tokens_and_idle_sequences(torch, monkeypatch, c
     """The mean run decides how all of them go; results are those of each by itself."""
     monkeypatch.setattr(runs, "_check", _strict)
     runs._run(torch, case)
+
+
+@gpu
+@pytest.mark.parametrize("dt", [npas.BF16, npas.F16])
+@pytest.mark.parametrize("H,KV,D,page,T,lengths,window", [
+    (4, 1, 128, 16, 3, [9000], 0), (8, 8, 64, 16, 7, [6000, 70, 2047, 7], 0), (2, 2, 256, 64, 5, [5000, 129], 0), (16, 2, 80, 7, 4, [2600, 2049, 33], 1000),
+    (4, 1, 128, 16, 40, [9000], 0), (8, 8, 64, 16, 50, [6000, 70, 2047, 50], 0), (2, 2, 256, 64, 65, [5000, 129], 0), (16, 2, 80, 7, 33, [2600, 2049, 33], 1000),
+    (1, 1, 24, 3, 130, [1400, 131], 0), (32, 8, 128, 16, 64, [2047, 4097], 63)])
+def test_every_token_of_a_run_counts_once(torch, dt, H, KV, D, page, T, lengths, window):
+    S, top = len(lengths), max(lengths)
+    v = torch.zeros((S, top, KV, D), dtype=torch.float64)
+    for s, n in enumerate(lengths):
+        v[s, :n] = _counts(torch, n, 0, D)[0][:, None]
+        v[s, n:] = 100                                    # must not come in
+    y, lse = _runs(torch, dt, torch.zeros((S, T, H, D), dtype=torch.float64), torch.ones_like(v), v, page, lengths, 0.125, window)
+    for s, n in enumerate(lengths):
+        for t in range(T):
+            seen = n - T + t + 1
+            first = max(0, seen - window) if window else 0
+            assert _counts_hold(y[s, t], lse[s, t], _counts(torch, seen, first, D)[1], seen - first, dt), (s, t)
